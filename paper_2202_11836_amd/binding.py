@@ -1,5 +1,6 @@
 """Thin ctypes binding of the C ABI of libskystage.so: the encoder stage
-(include/stage.h) and the host-side layer allocator (include/alloc.h).
+(include/stage.h), the attention operators (include/attn.h) and the host-side
+layer allocator (include/alloc.h).
 
 Argument marshalling only: torch tensors supply device memory and the HIP
 stream (torch.cuda.current_stream()); every step of the stage runs in the
@@ -36,6 +37,9 @@ EXPORTED = ("alloc_coarse", "alloc_fine", "alloc_workloads", "stage_init", "stag
             "stage_backward_noalloc",
             "stage_last_error", "stage_destroy")
 
+EXPORTED_ATTN = ("attn_relpos_init", "attn_relpos_bucket", "attn_workspace", "attn_forward",
+                 "attn_backward", "attn_last_error")
+
 _lib = None
 
 
@@ -50,6 +54,19 @@ class StageError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
         self.status = status
+
+
+class _RelPos(ctypes.Structure):  # attn_relpos
+    _fields_ = [("num_buckets", ctypes.c_int), ("max_distance", ctypes.c_int),
+                ("bidirectional", ctypes.c_int), ("reach", ctypes.c_int),
+                ("n_borders", ctypes.c_int), ("border", ctypes.c_int * 128)]
+
+
+class _AttnShape(ctypes.Structure):  # attn_shape
+    _fields_ = [("dtype", ctypes.c_int), ("batch", ctypes.c_int), ("seq_q", ctypes.c_int),
+                ("seq_k", ctypes.c_int), ("heads", ctypes.c_int), ("kv_heads", ctypes.c_int),
+                ("causal", ctypes.c_int), ("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_int64 * 3) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
 
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -121,6 +138,19 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.alloc_fine.restype = i32
     lib.alloc_workloads.argtypes = [i32, i32, dp, dp, dp, ip, i32, dp]
     lib.alloc_workloads.restype = i32
+    rp, sh = ctypes.POINTER(_RelPos), ctypes.POINTER(_AttnShape)
+    lib.attn_relpos_init.argtypes = [i32, i32, i32, rp]
+    lib.attn_relpos_init.restype = i32
+    lib.attn_relpos_bucket.argtypes = [rp, i64]
+    lib.attn_relpos_bucket.restype = i32
+    lib.attn_workspace.argtypes = [sh, rp, i32, ctypes.POINTER(sz)]
+    lib.attn_workspace.restype = i32
+    lib.attn_forward.argtypes = [sh, rp] + [vp] * 9 + [sz, vp]
+    lib.attn_forward.restype = i32
+    lib.attn_backward.argtypes = [sh, rp] + [vp] * 14 + [sz, vp]
+    lib.attn_backward.restype = i32
+    lib.attn_last_error.argtypes = []
+    lib.attn_last_error.restype = ctypes.c_char_p
     _lib = lib
     return lib
 
@@ -423,6 +453,167 @@ class Stage:
             self.close()
         except Exception:
             pass
+
+
+# ---------------------------------------------------------------------------
+# Attention operators (include/attn.h)
+# ---------------------------------------------------------------------------
+def _attn_check(status: int) -> None:
+    if status != STAGE_OK:
+        raise StageError(status, (load_library().attn_last_error() or b"").decode())
+
+
+def _refuse(msg: str):
+    raise StageError(STAGE_EINVAL, msg)
+
+
+class RelPos:
+    """Buckets of a relative position bias (attn_relpos): num_buckets over both
+    directions (bidirectional), or for the keys at or before a query only;
+    distances from max_distance on share the last one."""
+
+    def __init__(self, num_buckets: int = 32, max_distance: int = 128, bidirectional: bool = True):
+        self.num_buckets, self.max_distance = int(num_buckets), int(max_distance)
+        self.bidirectional = bool(bidirectional)
+        self.c = _RelPos()
+        _attn_check(load_library().attn_relpos_init(self.num_buckets, self.max_distance,
+                                                    int(self.bidirectional), ctypes.byref(self.c)))
+
+    def bucket(self, distance: int) -> int:
+        """Bucket of key position - query position."""
+        return load_library().attn_relpos_bucket(ctypes.byref(self.c), int(distance))
+
+
+class _AttnCall:
+    """Checks and marshalling shared by attn_forward and attn_backward."""
+
+    def __init__(self, q, k, v, key_mask, scale, causal, q_pos, relpos, table):
+        import torch
+        code = {torch.bfloat16: STAGE_BF16, torch.float32: STAGE_F32}.get(q.dtype)
+        if code is None:
+            _refuse("q must be bfloat16 or float32")
+        if q.dim() != 4 or k.dim() != 4:
+            _refuse("q, k, v must be [batch, length, heads, 64]")
+        B, Sq, H, D = q.shape
+        Sk, G = k.shape[1], k.shape[2]
+        self.dev, self.dtype = q.device, q.dtype
+        self.q_shape, self.kv_shape = (B, Sq, H, D), (B, Sk, G, D)
+        if D != 64 or not q.is_cuda:
+            _refuse("q must be [batch, length, heads, 64] on a GPU")
+        s = self.s = _AttnShape()
+        s.dtype, s.batch, s.seq_q, s.seq_k, s.heads, s.kv_heads = code, B, Sq, Sk, H, G
+        s.causal, s.scale = int(bool(causal)), 0.125 if scale is None else scale
+        self.put("q", q, self.q_shape)
+        self.put("k", k, self.kv_shape)
+        self.put("v", v, self.kv_shape)
+        if key_mask is not None:
+            self.plain("key_mask", key_mask, torch.uint8, (B, Sk))
+        if q_pos is not None:
+            self.plain("q_pos", q_pos, torch.int32, (B,))
+        if (relpos is None) != (table is None):
+            _refuse("relpos and table go together")
+        self.rp = None
+        if relpos is not None:
+            self.plain("table", table, torch.float32, (relpos.num_buckets, H))
+            self.rp = ctypes.byref(relpos.c)
+        self.head = (ctypes.byref(s), self.rp, _ptr(table), q.data_ptr(), k.data_ptr(),
+                     v.data_ptr(), _ptr(key_mask), _ptr(q_pos))
+
+    def put(self, name, t, shape):
+        """An operand of the call's type and device: its strides go into the shape."""
+        if t.shape != shape or t.dtype != self.dtype or t.device != self.dev:
+            _refuse(f"{name} must be {self.dtype} {tuple(shape)} on {self.dev}")
+        st = t.stride()
+        if st[3] != 1:
+            _refuse(f"the 64 values of a head of {name} must lie side by side")
+        setattr(self.s, name, st[:3])
+
+    def plain(self, name, t, dtype, shape):
+        if t.shape != shape or t.dtype != dtype or t.device != self.dev or not t.is_contiguous():
+            _refuse(f"{name} must be contiguous {dtype} {tuple(shape)} on {self.dev}")
+
+    def made(self, name, t, shape):
+        """The operand given for an output, or a new one."""
+        import torch
+        if t is None:
+            t = torch.empty(shape, dtype=self.dtype, device=self.dev)
+        self.put(name, t, shape)
+        return t
+
+    def run(self, fn, tail, backward):
+        """fn(head..., tail..., workspace, its bytes, stream) on the operands' device
+        and that device's current stream.  The workspace comes from torch's
+        allocator, which gives no memory of a stream (or of a captured graph) away
+        while work on it may still use it."""
+        import torch
+        n = ctypes.c_size_t()
+        lib = load_library()
+
+        def go():
+            _attn_check(lib.attn_workspace(self.head[0], self.rp, backward, ctypes.byref(n)))
+            ws = torch.empty(n.value, dtype=torch.uint8, device=self.dev) if n.value else None
+            _attn_check(fn(*self.head, *tail, _ptr(ws), n.value,
+                           torch.cuda.current_stream(self.dev).cuda_stream))
+
+        if torch.cuda.current_device() == self.dev.index:
+            go()
+        else:
+            with torch.cuda.device(self.dev):
+                go()
+
+
+def attn_forward(q, k, v, key_mask=None, scale=None, causal=False, q_pos=None, relpos=None,
+                 table=None, out=None, lse=None):
+    """Attention of q [batch, seq_q, heads, 64] over k, v [batch, seq_k, kv_heads, 64]
+    (fp32 or bf16, any strides that leave a head's 64 values side by side):
+    returns out, shaped like q, and lse [batch, heads, seq_q] fp32, which
+    attn_backward takes.
+
+    key_mask   uint8 [batch, seq_k], 1 = attend (None: every key)
+    scale      of the scores (None: 1 / 8)
+    causal     query i sees the keys at positions up to i + q_pos
+    q_pos      int32 [batch], position of query 0 on the key axis (None: 0)
+    relpos, table   a RelPos and its fp32 [num_buckets, heads] biases
+    out, lse   where to write
+
+    A query without a key gets zeros and lse = -inf.  Runs on the current stream
+    of q's device."""
+    import torch
+    c = _AttnCall(q, k, v, key_mask, scale, causal, q_pos, relpos, table)
+    out = c.made("out", out, c.q_shape)
+    B, Sq, H, _ = c.q_shape
+    if lse is None:
+        lse = torch.empty((B, H, Sq), dtype=torch.float32, device=c.dev)
+    else:
+        c.plain("lse", lse, torch.float32, (B, H, Sq))
+    c.run(load_library().attn_forward, (out.data_ptr(), lse.data_ptr()), 0)
+    return out, lse
+
+
+def attn_backward(q, k, v, out, lse, dout, key_mask=None, scale=None, causal=False, q_pos=None,
+                  relpos=None, table=None, dq=None, dk=None, dv=None, dtable=None):
+    """Gradients of <out, dout> for attn_forward's arguments, out and lse: returns
+    dq, dk, dv and dtable (None without a table), written where given."""
+    import torch
+    c = _AttnCall(q, k, v, key_mask, scale, causal, q_pos, relpos, table)
+    B, Sq, H, _ = c.q_shape
+    c.put("out", out, c.q_shape)
+    c.put("dout", dout, c.q_shape)
+    c.plain("lse", lse, torch.float32, (B, H, Sq))
+    dq = c.made("dq", dq, c.q_shape)
+    dk = c.made("dk", dk, c.kv_shape)
+    dv = c.made("dv", dv, c.kv_shape)
+    if table is None:
+        if dtable is not None:
+            _refuse("dtable without a table")
+    elif dtable is None:
+        dtable = torch.empty_like(table)
+    else:
+        c.plain("dtable", dtable, torch.float32, tuple(table.shape))
+    c.run(load_library().attn_backward,
+          (out.data_ptr(), lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+           dv.data_ptr(), _ptr(dtable)), 1)
+    return dq, dk, dv, dtable
 
 
 # ---------------------------------------------------------------------------

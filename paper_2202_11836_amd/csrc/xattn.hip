@@ -1,0 +1,588 @@
+// Attention over the keys of another sequence, with a relative position bias by
+// buckets (include/attn.h has the formulas).  The kernels are those of the stage's
+// self attention (attn.hip) in structure: a wavefront owns 32 queries (forward,
+// dQ) or 32 keys (dK, dV), a work-group of 4 shares 64-row blocks of the streamed
+// operand in a two-stage LDS ring filled by direct-to-LDS loads, scores are
+// produced transposed where a row's statistics are wanted per lane, and
+// accumulators go back into the next product as its B operand.  What is added:
+//   - fp32 tiles beside the bf16 ones (XT), on v_mfma_f32_32x32x2_f32;
+//   - the keys that a mask leaves, as bits (KeyBlocks): blocks without one are
+//     skipped, and a block that holds hidden keys has their K and V rows cleared
+//     in LDS, so that whatever they hold stays out of the products;
+//   - the bias: distances from `reach` on share one value on either side, so a
+//     32 x 32 tile that is further adds one scalar inside the exponent; a nearer
+//     tile reads a table of the bias by distance that the work-group spread out
+//     in LDS (two reads for four scores);
+//   - the bias gradient: far tiles sum their dS in a register; a near tile adds
+//     its dS along the diagonals in LDS (per half wavefront, where the 32 lanes
+//     of one instruction hit 32 distances), then sums diagonals of one bucket
+//     with a segmented scan over the lanes.  One row of sums per work-group goes
+//     to memory; all in a fixed order.
+
+#include "xattn.h"
+
+namespace {
+
+constexpr int XQB = 128;  // rows (queries or keys) of a work-group
+
+// Work-groups in an order that starts the long ones first under `causal`.
+__device__ __forceinline__ void x_block(const XAttnArgs& a, int nrow, bool last_first, int& rb,
+                                        int& bh) {
+  attn_block(blockIdx.x, gridDim.x, nrow, rb, bh);
+  if (last_first) rb = nrow - 1 - rb;
+}
+
+__device__ __forceinline__ int x_dist_n(const XAttnArgs& a) { return 2 * (a.reach + XPAD) + 1; }
+
+// The bias of head h by distance, -(reach + XPAD) .. reach + XPAD, in units of
+// log2.
+__device__ __forceinline__ void x_fill_dist(const XAttnArgs& a, int h, float* dist) {
+  const int n = x_dist_n(a), mid = n >> 1;
+  for (int e = threadIdx.x; e < n; e += 256)
+    dist[e] = a.table[(int64_t)x_bucket(a, e - mid) * a.H + h] * XLOG2E;
+}
+
+// Clears the rows of a block's K and V tiles whose key is hidden (word: the keys
+// that are not).
+template <typename T>
+__device__ __forceinline__ void x_clear_hidden(char* kv, uint64_t word) {
+  constexpr int CPR = XT<T>::CPR, N = 2 * XKT * CPR;
+#pragma unroll
+  for (int i = 0; i < N / 256; ++i) {
+    const int ch = threadIdx.x + 256 * i;
+    if (!((word >> ((ch / CPR) & (XKT - 1))) & 1)) *(u32x4_t*)(kv + 16 * ch) = zero4();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Forward
+// ---------------------------------------------------------------------------
+template <typename T, bool BIAS>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(XAttnArgs a) {
+  constexpr int TILE = XKT * XT<T>::ROWB;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];  // [2][K, V], dist
+  float* dist = (float*)(lds + 4 * TILE);
+
+  int qb, bh;
+  x_block(a, (a.Sq + XQB - 1) / XQB, a.causal, qb, bh);
+  const int b = bh / a.H, h = bh % a.H, g = h / a.rep;
+  const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int q0 = qb * XQB + wave * 32;
+  const int qp = x_q_pos(a, b);
+  const int p0 = q0 + qp;  // position of the wavefront's first query
+  const T* K = (const T*)a.k + b * a.sk[0] + g * a.sk[2];
+  const T* V = (const T*)a.v + b * a.sv[0] + g * a.sv[2];
+  const int lim =
+      a.causal ? max(0, min(a.Sk, min(qb * XQB + XQB, a.Sq) + qp)) : a.Sk;
+
+  const typename XT<T>::Frag qf =
+      x_frag((const T*)a.q + b * a.sq[0] + (int64_t)(q0 + rr) * a.sq[1] + h * a.sq[2],
+             q0 + rr < a.Sq, hf);
+  KeyBlocks<XKT> blocks;
+  blocks.init(a.mask ? a.mask + (int64_t)b * a.Sk : nullptr, lim, 0, (lim + XKT - 1) / XKT, lane);
+  int kb = blocks.next(0);
+  if (kb < blocks.nblk) {
+    x_dma<T, XKT, 4>(K, a.sk[1], kb * XKT, lim, lds, wave, lane);
+    x_dma<T, XKT, 4>(V, a.sv[1], kb * XKT, lim, lds + TILE, wave, lane);
+  }
+  float far_l = 0.0f, far_r = 0.0f;
+  const int mid = a.reach + XPAD;
+  if constexpr (BIAS) {
+    x_fill_dist(a, h, dist);
+    far_l = a.table[(int64_t)x_bucket(a, -a.reach) * a.H + h] * XLOG2E;
+    far_r = a.table[(int64_t)x_bucket(a, a.reach) * a.H + h] * XLOG2E;
+  }
+
+  float m = -INFINITY, lsum = 0.0f;
+  f32x16_t acc[2] = {zero16(), zero16()};
+  for (int st = 0; kb < blocks.nblk; st ^= 1) {
+    const uint64_t word = blocks.word(kb);
+    const uint64_t hidden = blocks.in_range(kb) & ~word;
+    const int kn = blocks.next(kb + 1);
+    wait_all();
+    __syncthreads();
+    char* kv = lds + st * 2 * TILE;
+    if (kn < blocks.nblk) {
+      char* nkv = lds + (st ^ 1) * 2 * TILE;
+      x_dma<T, XKT, 4>(K, a.sk[1], kn * XKT, lim, nkv, wave, lane);
+      x_dma<T, XKT, 4>(V, a.sv[1], kn * XKT, lim, nkv + TILE, wave, lane);
+    }
+    if (hidden) {
+      x_clear_hidden<T>(kv, word);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      const int k0 = kb * XKT + 32 * sub;
+      const uint32_t rows = (uint32_t)(word >> (32 * sub));
+      if (rows == 0 || (a.causal && k0 > p0 + 31)) continue;
+      f32x16_t s = x_mma_rows(kv, 32 * sub, qf, zero16(), lane);
+      const bool full = rows == 0xffffffffu && (!a.causal || k0 + 31 <= p0);
+      const bool near = BIAS && k0 + 31 - p0 > -a.reach && k0 - p0 - 31 < a.reach;
+      const float far = !BIAS ? 0.0f : k0 > p0 ? far_r : far_l;  // (of a tile that is not near)
+      // Scores in units of log2: s * mul + add, masked; either in one step inside
+      // the exponent (a tile with one bias and no hidden key) or here.
+      float mul = a.c, add = far, mblk = -INFINITY;
+      if (full && !near) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mblk = fmaxf(mblk, s[r]);
+        mblk = fmaf(mblk, mul, add);
+      } else {
+        uint32_t bits = x_lane_bits(rows, hf);
+        if (a.causal) bits &= x_upto(p0 + rr - k0 - 4 * hf);
+        if (near) {
+          const float* d = dist + (k0 + 4 * hf - p0 - rr + mid);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], mul, d[8 * (r >> 2) + (r & 3)]);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], mul, add);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = x_bit(bits, r) ? s[r] : -INFINITY;
+          mblk = fmaxf(mblk, s[r]);
+        }
+        mul = 1.0f;
+        add = 0.0f;
+      }
+      {
+        const HalfPair pr = half_pair(mblk);
+        mblk = fmaxf(pr.x, pr.y);
+      }
+      // The offset of the exponents moves only when a tile's maximum exceeds it
+      // by more than 8, so most tiles leave the output accumulators alone.
+      const bool grow = mblk > m + 8.0f;
+      if (__any(grow)) {
+        const float mn = grow ? mblk : m;
+        const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+        lsum *= alpha;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[t][r] *= alpha;
+        m = mn;
+      }
+      add -= m == -INFINITY ? 0.0f : m;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add));
+      float ps = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) ps += s[r];
+      lsum += ps;
+      x_mma_cols<T>(kv + TILE, 32 * sub, s, acc, lane);
+    }
+    kb = kn;
+  }
+  const HalfPair lp = half_pair(lsum);
+  const float ltot = lp.x + lp.y;
+  if (a.lse && hf == 0 && q0 + rr < a.Sq)
+    a.lse[((int64_t)b * a.H + h) * a.Sq + q0 + rr] =
+        ltot == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(ltot)) * XLN2;
+  __syncthreads();  // the ring becomes the output staging area
+  x_store<T>(acc, ltot == 0.0f ? 0.0f : 1.0f / ltot, (T*)lds + wave * 32 * XT<T>::LD,
+             (T*)a.out + b * a.so[0] + h * a.so[2], a.so[1], q0, a.Sq);
+}
+
+// ---------------------------------------------------------------------------
+// Backward, dQ and the bias gradient.  RED: D is formed from P and dP in a pass of
+// its own over the keys; else it is rowsum(dO * out).
+// ---------------------------------------------------------------------------
+template <typename T, bool BIAS, bool RED>
+__global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
+  constexpr int TILE = XKT * XT<T>::ROWB;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  // [2][K, V]; with a bias: dist, the wavefronts' diagonal sums [4][2][64] and
+  // bucket sums [4][nb]
+  float* dist = (float*)(lds + 4 * TILE);
+  const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  float* diag = nullptr;
+  float* bsum = nullptr;
+  if constexpr (BIAS) {
+    float* p = dist + ((x_dist_n(a) + 3) & ~3);
+    diag = p + wave * 128;
+    bsum = p + 512 + wave * a.nb;
+  }
+
+  int qb, bh;
+  const int nq = (a.Sq + XQB - 1) / XQB;
+  x_block(a, nq, a.causal, qb, bh);
+  const int b = bh / a.H, h = bh % a.H, g = h / a.rep;
+  const int q0 = qb * XQB + wave * 32, q = q0 + rr;
+  const bool qv = q < a.Sq;
+  const int qp = x_q_pos(a, b);
+  const int p0 = q0 + qp;
+  const T* K = (const T*)a.k + b * a.sk[0] + g * a.sk[2];
+  const T* V = (const T*)a.v + b * a.sv[0] + g * a.sv[2];
+  const int lim =
+      a.causal ? max(0, min(a.Sk, min(qb * XQB + XQB, a.Sq) + qp)) : a.Sk;
+
+  const typename XT<T>::Frag qf = x_frag(
+      (const T*)a.q + b * a.sq[0] + (int64_t)q * a.sq[1] + h * a.sq[2], qv, hf);
+  const typename XT<T>::Frag dof = x_frag(
+      (const T*)a.dout + b * a.sdo[0] + (int64_t)q * a.sdo[1] + h * a.sdo[2], qv, hf);
+  const int64_t row = ((int64_t)b * a.H + h) * a.Sq + q;
+  float lse2 = qv ? a.lse[row] * XLOG2E : 0.0f;
+  if (lse2 == -INFINITY) lse2 = INFINITY;  // no key: P = exp2(s - inf) = 0
+  float D = 0.0f;
+  if constexpr (!RED) {
+    const typename XT<T>::Frag of = x_frag(
+        (const T*)a.o + b * a.so[0] + (int64_t)q * a.so[1] + h * a.so[2], qv, hf);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(of) / 16); ++i)
+#pragma unroll
+      for (int e = 0; e < 16 / (int)sizeof(T); ++e) D += (float)dof.f[i][e] * (float)of.f[i][e];
+    const HalfPair pr = half_pair(D);
+    D = pr.x + pr.y;
+  }
+  float far_l = 0.0f, far_r = 0.0f;      // far bias
+  float gfar_l = 0.0f, gfar_r = 0.0f;    // far sums of dS
+  const int mid = a.reach + XPAD;
+  if constexpr (BIAS) {
+    x_fill_dist(a, h, dist);
+    far_l = a.table[(int64_t)x_bucket(a, -a.reach) * a.H + h] * XLOG2E;
+    far_r = a.table[(int64_t)x_bucket(a, a.reach) * a.H + h] * XLOG2E;
+    diag[lane] = diag[64 + lane] = 0.0f;
+    for (int i = lane; i < a.nb; i += 64) bsum[i] = 0.0f;
+  }
+
+  f32x16_t dq[2] = {zero16(), zero16()};
+  auto sweep = [&](auto first) {
+    constexpr bool SUM_D = decltype(first)::value;
+    KeyBlocks<XKT> blocks;
+    blocks.init(a.mask ? a.mask + (int64_t)b * a.Sk : nullptr, lim, 0, (lim + XKT - 1) / XKT, lane);
+    int kb = blocks.next(0);
+    if (kb < blocks.nblk) {
+      x_dma<T, XKT, 4>(K, a.sk[1], kb * XKT, lim, lds, wave, lane);
+      x_dma<T, XKT, 4>(V, a.sv[1], kb * XKT, lim, lds + TILE, wave, lane);
+    }
+    for (int st = 0; kb < blocks.nblk; st ^= 1) {
+      const uint64_t word = blocks.word(kb);
+      const uint64_t hidden = blocks.in_range(kb) & ~word;
+      const int kn = blocks.next(kb + 1);
+      wait_all();
+      __syncthreads();
+      char* kv = lds + st * 2 * TILE;
+      if (kn < blocks.nblk) {
+        char* nkv = lds + (st ^ 1) * 2 * TILE;
+        x_dma<T, XKT, 4>(K, a.sk[1], kn * XKT, lim, nkv, wave, lane);
+        x_dma<T, XKT, 4>(V, a.sv[1], kn * XKT, lim, nkv + TILE, wave, lane);
+      }
+      if (hidden) {
+        x_clear_hidden<T>(kv, word);
+        __syncthreads();
+      }
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const int k0 = kb * XKT + 32 * sub;
+        const uint32_t rows = (uint32_t)(word >> (32 * sub));
+        if (rows == 0 || (a.causal && k0 > p0 + 31)) continue;
+        f32x16_t s = x_mma_rows(kv, 32 * sub, qf, zero16(), lane);
+        f32x16_t dp = x_mma_rows(kv + TILE, 32 * sub, dof, splat16(SUM_D ? 0.0f : -D), lane);
+        const bool full = rows == 0xffffffffu && (!a.causal || k0 + 31 <= p0);
+        const bool near = BIAS && k0 + 31 - p0 > -a.reach && k0 - p0 - 31 < a.reach;
+        if (near) {
+          const float* d = dist + (k0 + 4 * hf - p0 - rr + mid);
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, d[8 * (r >> 2) + (r & 3)]) - lse2);
+        } else {
+          const float add = (!BIAS ? 0.0f : k0 > p0 ? far_r : far_l) - lse2;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, add));
+        }
+        if (!full) {
+          uint32_t bits = x_lane_bits(rows, hf);
+          if (a.causal) bits &= x_upto(p0 + rr - k0 - 4 * hf);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = x_bit(bits, r) ? s[r] : 0.0f;
+        }
+        if constexpr (SUM_D) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) D = fmaf(s[r], dp[r], D);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] *= dp[r];  // dS
+          if constexpr (BIAS) {
+            if (a.dtable && near) {
+              // lane (query) rr, register r (key): distance k0 - p0 - 31 + e with
+              // e = key - rr + 31; one instruction's 32 lanes of a half have 32
+              // distances
+              float* e = diag + 64 * hf + 4 * hf - rr + 31;
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                __hip_atomic_fetch_add(e + 8 * (r >> 2) + (r & 3), s[r], __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_WAVEFRONT);
+              lds_wait();
+              __builtin_amdgcn_wave_barrier();
+              float v = diag[lane] + diag[64 + lane];
+              lds_wait();
+              __builtin_amdgcn_wave_barrier();
+              diag[lane] = diag[64 + lane] = 0.0f;
+              // Buckets are runs of distances: sum each run into its last lane.
+              // Lane 63 has none.
+              const int bk = lane < 63 ? x_bucket(a, k0 - p0 - 31 + lane) : -1;
+#pragma unroll
+              for (int o = 1; o < 64; o <<= 1) {
+                const float u = __shfl_up(v, o, 64);
+                const int ub = __shfl_up(bk, o, 64);
+                if (lane >= o && ub == bk) v += u;
+              }
+              const int nb = __shfl_down(bk, 1, 64);
+              if (lane < 63 && nb != bk) bsum[bk] += v;
+              lds_wait();
+              __builtin_amdgcn_wave_barrier();
+            } else if (a.dtable) {
+              float t = s[0];
+#pragma unroll
+              for (int r = 1; r < 16; ++r) t += s[r];
+              if (k0 > p0) gfar_r += t;
+              else gfar_l += t;
+            }
+          }
+          x_mma_cols<T>(kv, 32 * sub, s, dq, lane);
+        }
+      }
+      kb = kn;
+    }
+    __syncthreads();  // (the next pass, or the output, takes the ring)
+  };
+  if constexpr (RED) {
+    sweep(std::true_type());
+    const HalfPair pr = half_pair(D);
+    D = pr.x + pr.y;
+  }
+  if (hf == 0 && qv) a.dsum[row] = D;
+  sweep(std::false_type());
+  if constexpr (BIAS) {
+    if (a.dtable) {
+      gfar_l = wave_sum(gfar_l);
+      gfar_r = wave_sum(gfar_r);
+      if (lane == 0) {
+        bsum[x_bucket(a, -a.reach)] += gfar_l;
+        bsum[x_bucket(a, a.reach)] += gfar_r;
+      }
+      __syncthreads();
+      const float* p = bsum - wave * a.nb;
+      for (int i = tid; i < a.nb; i += 256)
+        a.tpart[(((int64_t)b * a.H + h) * nq + qb) * a.nb + i] =
+            (p[i] + p[a.nb + i]) + (p[2 * a.nb + i] + p[3 * a.nb + i]);
+    }
+  }
+  x_store<T>(dq, a.scale, (T*)lds + wave * 32 * XT<T>::LD,
+             (T*)a.dq + b * a.sdq[0] + h * a.sdq[2], a.sdq[1], q0, a.Sq);
+}
+
+// ---------------------------------------------------------------------------
+// Backward, dK and dV: wavefront = 32 keys, loops over blocks of QB queries of
+// every query head that shares the keys.  Work-groups from n_kv on sum the bias
+// gradient: one per bucket and head.
+// ---------------------------------------------------------------------------
+template <typename T> constexpr int x_qb() { return sizeof(T) == 2 ? 128 : 64; }
+
+__device__ __forceinline__ void x_dtable_sum(const XAttnArgs& a, int w, float* red) {
+  const int c = w % a.nb, h = w / a.nb, nq = (a.Sq + XQB - 1) / XQB;
+  float t = 0.0f;
+  for (int64_t i = threadIdx.x; i < (int64_t)a.B * nq; i += 256)
+    t += a.tpart[((i / nq * a.H + h) * nq + i % nq) * a.nb + c];
+  t = wave_sum(t);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = t;
+  __syncthreads();
+  if (threadIdx.x == 0) a.dtable[(int64_t)c * a.H + h] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+template <typename T, bool BIAS>
+__global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_kv) {
+  constexpr int QB = x_qb<T>(), TILE = QB * XT<T>::ROWB;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  // [2][Q, dO]; per stage lse and -D of QB rows; with a bias: dist
+  float* rowv = (float*)(lds + 4 * TILE);
+  float* dist = rowv + 4 * QB;
+  if ((int)blockIdx.x >= n_kv) {
+    x_dtable_sum(a, blockIdx.x - n_kv, rowv);
+    return;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int kblk, bg;
+  attn_block(blockIdx.x, n_kv, (a.Sk + XQB - 1) / XQB, kblk, bg);
+  const int b = bg / a.G, g = bg % a.G;
+  const int k0 = kblk * XQB + wave * 32, key = k0 + rr;
+  const int qp = x_q_pos(a, b);
+  // Queries from q_first on see a key of this work-group, those before it none.
+  const int q_first = a.causal ? max(0, kblk * XQB - qp) : 0;
+  const int qb0 = q_first / QB, nqb = max(0, (a.Sq + QB - 1) / QB - qb0), n_it = nqb * a.rep;
+  // A key that the mask hides, or no query sees, may hold anything.
+  const bool kvalid = key < a.Sk && (!a.causal || key - qp < a.Sq) &&
+                      (!a.mask || a.mask[(int64_t)b * a.Sk + key] != 0);
+  const bool all_valid = __all(kvalid);
+  const uint32_t kbits = kvalid ? 0xffffffffu : 0u;
+  const typename XT<T>::Frag kf = x_frag(
+      (const T*)a.k + b * a.sk[0] + (int64_t)key * a.sk[1] + g * a.sk[2], kvalid, hf);
+  const typename XT<T>::Frag vf = x_frag(
+      (const T*)a.v + b * a.sv[0] + (int64_t)key * a.sv[1] + g * a.sv[2], kvalid, hf);
+  const T* Q = (const T*)a.q + b * a.sq[0];
+  const T* dO = (const T*)a.dout + b * a.sdo[0];
+
+  auto head = [&](int it) { return g * a.rep + it / nqb; };
+  auto qrow = [&](int it) { return (qb0 + it % nqb) * QB; };
+  auto dma = [&](int it, char* to) {
+    const int h = head(it), r = qrow(it);
+    x_dma<T, QB, 4>(Q + h * a.sq[2], a.sq[1], r, a.Sq, to, wave, lane);
+    x_dma<T, QB, 4>(dO + h * a.sdo[2], a.sdo[1], r, a.Sq, to + TILE, wave, lane);
+  };
+  // Thread t < QB carries lse (in log2 units) of row t of a block, the next QB
+  // threads -D; rows that are not there have P = exp2(s - inf) = 0.
+  const bool row_thread = tid < 2 * QB;
+  auto row_raw = [&](int it) {
+    const int r = qrow(it) + (tid & (QB - 1));
+    if (!row_thread || r >= a.Sq) return tid < QB ? INFINITY : 0.0f;
+    return (tid < QB ? a.lse : a.dsum)[((int64_t)b * a.H + head(it)) * a.Sq + r];
+  };
+  auto row_store = [&](float raw, int st) {
+    if (row_thread)
+      rowv[st * 2 * QB + tid] = tid >= QB ? -raw : raw == -INFINITY ? INFINITY : raw * XLOG2E;
+  };
+  float raw = 0.0f;
+  if (n_it > 0) {
+    dma(0, lds);
+    row_store(row_raw(0), 0);
+    if (n_it > 1) raw = row_raw(1);
+  }
+  const int mid = a.reach + XPAD;
+  float far_l = 0.0f, far_r = 0.0f;
+  f32x16_t dv[2] = {zero16(), zero16()}, dk[2] = {zero16(), zero16()};
+  int cur_h = -1;
+  for (int it = 0; it < n_it; ++it) {
+    const int st = it & 1;
+    const int h = head(it), qr = qrow(it);
+    wait_all();
+    __syncthreads();
+    if constexpr (BIAS) {
+      if (h != cur_h) {
+        // (every wavefront is past its last use of the previous head's table)
+        cur_h = h;
+        x_fill_dist(a, h, dist);
+        far_l = a.table[(int64_t)x_bucket(a, -a.reach) * a.H + h] * XLOG2E;
+        far_r = a.table[(int64_t)x_bucket(a, a.reach) * a.H + h] * XLOG2E;
+        __syncthreads();
+      }
+    }
+    if (it + 1 < n_it) dma(it + 1, lds + (st ^ 1) * 2 * TILE);
+    const float raw2 = it + 2 < n_it ? row_raw(it + 2) : 0.0f;
+    const char* Qs = lds + st * 2 * TILE;
+    const char* dOs = Qs + TILE;
+    const float* lv = rowv + st * 2 * QB;
+#pragma unroll
+    for (int sub = 0; sub < QB / 32; ++sub) {
+      const int r0 = qr + 32 * sub;   // first query
+      const int p0 = r0 + qp;         // its position
+      if (r0 >= a.Sq || (a.causal && k0 > p0 + 31)) continue;
+      f32x16_t dp;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4_t d4 = *(const f32x4_t*)(lv + QB + 32 * sub + 8 * i + 4 * hf);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dp[4 * i + e] = d4[e];
+      }
+      f32x16_t s = x_mma_rows(Qs, 32 * sub, kf, zero16(), lane);
+      dp = x_mma_rows(dOs, 32 * sub, vf, dp, lane);
+      const bool full = all_valid && (!a.causal || k0 + 31 <= p0);
+      const bool near = BIAS && k0 + 31 - p0 > -a.reach && k0 - p0 - 31 < a.reach;
+      const float far = !BIAS ? 0.0f : k0 > p0 ? far_r : far_l;
+      const float* d = dist + (k0 + rr - p0 - 4 * hf + mid);
+      // Key rr is seen by the queries from rr + k0 - p0 on.
+      uint32_t bits = kbits;
+      if (a.causal) bits &= ~x_upto(k0 + rr - p0 - 4 * hf - 1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4_t l4 = *(const f32x4_t*)(lv + 32 * sub + 8 * i + 4 * hf);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * i + e;
+          float x;
+          if (near) x = fmaf(s[r], a.c, d[-(8 * i + e)]) - l4[e];
+          else x = fmaf(s[r], a.c, BIAS ? far - l4[e] : -l4[e]);
+          s[r] = __builtin_amdgcn_exp2f(x);
+        }
+      }
+      if (!full) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = x_bit(bits, r) ? s[r] : 0.0f;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[r] *= s[r];  // dS
+      x_mma_cols<T>(dOs, 32 * sub, s, dv, lane);
+      x_mma_cols<T>(Qs, 32 * sub, dp, dk, lane);
+    }
+    if (it + 1 < n_it) row_store(raw, st ^ 1);
+    raw = raw2;
+  }
+  __syncthreads();  // the ring becomes the output staging area
+  T* stage = (T*)lds + wave * 32 * XT<T>::LD;
+  x_store<T>(dk, a.scale, stage, (T*)a.dk + b * a.sdk[0] + g * a.sdk[2], a.sdk[1], k0, a.Sk);
+  lds_wait();
+  __builtin_amdgcn_wave_barrier();
+  x_store<T>(dv, 1.0f, stage, (T*)a.dv + b * a.sdv[0] + g * a.sdv[2], a.sdv[1], k0, a.Sk);
+}
+
+template <typename K>
+hipError_t launch(K kernel, int64_t grid, size_t lds, hipStream_t st, const XAttnArgs& a) {
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), lds, st, a);
+  return hipGetLastError();
+}
+
+size_t dist_bytes(const XAttnArgs& a) {
+  return a.table ? (size_t)((2 * (a.reach + XPAD) + 1 + 3) & ~3) * 4 : 0;
+}
+
+template <typename T>
+hipError_t forward_t(const XAttnArgs& a, hipStream_t st) {
+  const int64_t grid = (int64_t)a.B * a.H * ((a.Sq + XQB - 1) / XQB);
+  const size_t lds = 4 * XKT * XT<T>::ROWB + dist_bytes(a);
+  if (grid == 0) return hipSuccess;
+  return a.table ? launch(xattn_fwd_kernel<T, true>, grid, lds, st, a)
+                 : launch(xattn_fwd_kernel<T, false>, grid, lds, st, a);
+}
+
+template <typename T>
+hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
+  hipError_t e = hipSuccess;
+  const int64_t gq = (int64_t)a.B * a.H * ((a.Sq + XQB - 1) / XQB);
+  if (gq > 0) {
+    size_t lds = 4 * XKT * XT<T>::ROWB;
+    if (!a.table) {
+      e = launch(xattn_dq_kernel<T, false, false>, gq, lds, st, a);
+    } else {
+      lds += dist_bytes(a) + (512 + 4 * (size_t)a.nb) * 4;
+      // The bias gradient is a sum of many dS that nearly cancel, in fp32: with
+      // D from a bf16 out it would be off by out's rounding.
+      if (sizeof(T) == 2 && a.dtable)
+        e = launch(xattn_dq_kernel<T, true, sizeof(T) == 2>, gq, lds, st, a);
+      else
+        e = launch(xattn_dq_kernel<T, true, false>, gq, lds, st, a);
+    }
+    if (e != hipSuccess) return e;
+  }
+  const int64_t n_kv = (int64_t)a.B * a.G * ((a.Sk + XQB - 1) / XQB);
+  const int64_t n_red = a.dtable ? (int64_t)a.nb * a.H : 0;
+  if (n_kv + n_red == 0) return e;
+  const size_t lds = 4 * x_qb<T>() * XT<T>::ROWB + 4 * x_qb<T>() * 4 + dist_bytes(a);
+  const dim3 grid((unsigned)(n_kv + n_red));
+  if (a.table)
+    hipLaunchKernelGGL((xattn_dkdv_kernel<T, true>), grid, dim3(256), lds, st, a, (int)n_kv);
+  else
+    hipLaunchKernelGGL((xattn_dkdv_kernel<T, false>), grid, dim3(256), lds, st, a, (int)n_kv);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t xattn_forward(const XAttnArgs& a, stage_dtype dt, hipStream_t st) {
+  return dt == STAGE_BF16 ? forward_t<bf16_t>(a, st) : forward_t<float>(a, st);
+}
+hipError_t xattn_backward(const XAttnArgs& a, stage_dtype dt, hipStream_t st) {
+  return dt == STAGE_BF16 ? backward_t<bf16_t>(a, st) : backward_t<float>(a, st);
+}
