@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -62,11 +63,9 @@ class _RelPos(ctypes.Structure):  # attn_relpos
                 ("n_borders", ctypes.c_int), ("border", ctypes.c_int * 128)]
 
 
-class _AttnShape(ctypes.Structure):  # attn_shape
-    _fields_ = [("dtype", ctypes.c_int), ("batch", ctypes.c_int), ("seq_q", ctypes.c_int),
-                ("seq_k", ctypes.c_int), ("heads", ctypes.c_int), ("kv_heads", ctypes.c_int),
-                ("causal", ctypes.c_int), ("scale", ctypes.c_float)] + \
-               [(n, ctypes.c_int64 * 3) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+# attn_shape: dtype, batch, seq_q, seq_k, heads, kv_heads, causal, scale and the
+# strides of q, k, v, out, dout, dq, dk, dv
+_ATTN_SHAPE = struct.Struct("@7if24q")
 
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -138,7 +137,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.alloc_fine.restype = i32
     lib.alloc_workloads.argtypes = [i32, i32, dp, dp, dp, ip, i32, dp]
     lib.alloc_workloads.restype = i32
-    rp, sh = ctypes.POINTER(_RelPos), ctypes.POINTER(_AttnShape)
+    rp, sh = ctypes.POINTER(_RelPos), ctypes.c_char_p  # (attn_shape: packed bytes)
     lib.attn_relpos_init.argtypes = [i32, i32, i32, rp]
     lib.attn_relpos_init.restype = i32
     lib.attn_relpos_bucket.argtypes = [rp, i64]
@@ -478,88 +477,75 @@ class RelPos:
         self.c = _RelPos()
         _attn_check(load_library().attn_relpos_init(self.num_buckets, self.max_distance,
                                                     int(self.bidirectional), ctypes.byref(self.c)))
+        self.ref = ctypes.byref(self.c)
 
     def bucket(self, distance: int) -> int:
         """Bucket of key position - query position."""
         return load_library().attn_relpos_bucket(ctypes.byref(self.c), int(distance))
 
 
-class _AttnCall:
-    """Checks and marshalling shared by attn_forward and attn_backward."""
+def _attn_strides(name, t, shape, dtype, dev):
+    """Batch, position and head stride of an operand of this shape, type and device."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
+        _refuse(f"{name} must be {dtype} {tuple(shape)} on cuda:{dev}")
+    b, p, h, one = t.stride()
+    if one != 1:
+        _refuse(f"the 64 values of a head of {name} must lie side by side")
+    return b, p, h
 
-    def __init__(self, q, k, v, key_mask, scale, causal, q_pos, relpos, table):
-        import torch
-        code = {torch.bfloat16: STAGE_BF16, torch.float32: STAGE_F32}.get(q.dtype)
-        if code is None:
-            _refuse("q must be bfloat16 or float32")
-        if q.dim() != 4 or k.dim() != 4:
-            _refuse("q, k, v must be [batch, length, heads, 64]")
-        B, Sq, H, D = q.shape
-        Sk, G = k.shape[1], k.shape[2]
-        self.dev, self.dtype = q.device, q.dtype
-        self.q_shape, self.kv_shape = (B, Sq, H, D), (B, Sk, G, D)
-        if D != 64 or not q.is_cuda:
-            _refuse("q must be [batch, length, heads, 64] on a GPU")
-        s = self.s = _AttnShape()
-        s.dtype, s.batch, s.seq_q, s.seq_k, s.heads, s.kv_heads = code, B, Sq, Sk, H, G
-        s.causal, s.scale = int(bool(causal)), 0.125 if scale is None else scale
-        self.put("q", q, self.q_shape)
-        self.put("k", k, self.kv_shape)
-        self.put("v", v, self.kv_shape)
-        if key_mask is not None:
-            self.plain("key_mask", key_mask, torch.uint8, (B, Sk))
-        if q_pos is not None:
-            self.plain("q_pos", q_pos, torch.int32, (B,))
-        if (relpos is None) != (table is None):
-            _refuse("relpos and table go together")
-        self.rp = None
-        if relpos is not None:
-            self.plain("table", table, torch.float32, (relpos.num_buckets, H))
-            self.rp = ctypes.byref(relpos.c)
-        self.head = (ctypes.byref(s), self.rp, _ptr(table), q.data_ptr(), k.data_ptr(),
-                     v.data_ptr(), _ptr(key_mask), _ptr(q_pos))
 
-    def put(self, name, t, shape):
-        """An operand of the call's type and device: its strides go into the shape."""
-        if t.shape != shape or t.dtype != self.dtype or t.device != self.dev:
-            _refuse(f"{name} must be {self.dtype} {tuple(shape)} on {self.dev}")
-        st = t.stride()
-        if st[3] != 1:
-            _refuse(f"the 64 values of a head of {name} must lie side by side")
-        setattr(self.s, name, st[:3])
+def _attn_plain(name, t, shape, dtype, dev):
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
+        _refuse(f"{name} must be contiguous {dtype} {tuple(shape)} on cuda:{dev}")
+    return t.data_ptr()
 
-    def plain(self, name, t, dtype, shape):
-        if t.shape != shape or t.dtype != dtype or t.device != self.dev or not t.is_contiguous():
-            _refuse(f"{name} must be contiguous {dtype} {tuple(shape)} on {self.dev}")
 
-    def made(self, name, t, shape):
-        """The operand given for an output, or a new one."""
-        import torch
-        if t is None:
-            t = torch.empty(shape, dtype=self.dtype, device=self.dev)
-        self.put(name, t, shape)
-        return t
+def _attn_inputs(q, k, v, key_mask, scale, causal, q_pos, relpos, table):
+    """Checks of what both calls take.  Returns the shapes of q and of k, the device,
+    the head of the packed attn_shape (up to the strides of v) and the arguments from
+    rp to q_pos."""
+    import torch
+    dtype = q.dtype
+    code = STAGE_BF16 if dtype == torch.bfloat16 else STAGE_F32
+    dev = q.get_device()
+    if code == STAGE_F32 and dtype != torch.float32:
+        _refuse("q must be bfloat16 or float32")
+    if q.dim() != 4 or k.dim() != 4 or q.shape[3] != 64 or dev < 0:
+        _refuse("q, k, v must be [batch, length, heads, 64] on a GPU")
+    B, Sq, H, _ = q_shape = q.shape
+    Sk, G = k.shape[1], k.shape[2]
+    kv_shape = (B, Sk, G, 64)
+    if (relpos is None) != (table is None):
+        _refuse("relpos and table go together")
+    rp = tab = mask = pos = None
+    if relpos is not None:
+        rp, tab = relpos.ref, _attn_plain("table", table, (relpos.num_buckets, H), torch.float32, dev)
+    if key_mask is not None:
+        mask = _attn_plain("key_mask", key_mask, (B, Sk), torch.uint8, dev)
+    if q_pos is not None:
+        pos = _attn_plain("q_pos", q_pos, (B,), torch.int32, dev)
+    head = (code, B, Sq, Sk, H, G, 1 if causal else 0, 0.125 if scale is None else scale,
+            *_attn_strides("q", q, q_shape, dtype, dev),
+            *_attn_strides("k", k, kv_shape, dtype, dev),
+            *_attn_strides("v", v, kv_shape, dtype, dev))
+    return q_shape, kv_shape, dev, head, (rp, tab, q.data_ptr(), k.data_ptr(), v.data_ptr(), mask,
+                                          pos)
 
-    def run(self, fn, tail, backward):
-        """fn(head..., tail..., workspace, its bytes, stream) on the operands' device
-        and that device's current stream.  The workspace comes from torch's
-        allocator, which gives no memory of a stream (or of a captured graph) away
-        while work on it may still use it."""
-        import torch
-        n = ctypes.c_size_t()
-        lib = load_library()
 
-        def go():
-            _attn_check(lib.attn_workspace(self.head[0], self.rp, backward, ctypes.byref(n)))
-            ws = torch.empty(n.value, dtype=torch.uint8, device=self.dev) if n.value else None
-            _attn_check(fn(*self.head, *tail, _ptr(ws), n.value,
-                           torch.cuda.current_stream(self.dev).cuda_stream))
-
-        if torch.cuda.current_device() == self.dev.index:
-            go()
-        else:
-            with torch.cuda.device(self.dev):
-                go()
+def _attn_call(fn, shape, args, backward, dev):
+    """fn(shape, args..., workspace, its bytes, stream) on device dev and its current
+    stream.  The workspace comes from torch's allocator, which gives no memory of a
+    stream (or of a captured graph) away while work on it may still use it."""
+    import torch
+    lib = load_library()
+    n = ctypes.c_size_t()
+    if torch.cuda.current_device() != dev:
+        with torch.cuda.device(dev):
+            return _attn_call(fn, shape, args, backward, dev)
+    _attn_check(lib.attn_workspace(shape, args[0], backward, ctypes.byref(n)))
+    ws = torch.empty(n.value, dtype=torch.uint8, device=dev) if n.value else None
+    stream = torch._C._cuda_getCurrentRawStream(dev)
+    _attn_check(fn(shape, *args, None if ws is None else ws.data_ptr(), n.value, stream))
 
 
 def attn_forward(q, k, v, key_mask=None, scale=None, causal=False, q_pos=None, relpos=None,
@@ -579,14 +565,16 @@ def attn_forward(q, k, v, key_mask=None, scale=None, causal=False, q_pos=None, r
     A query without a key gets zeros and lse = -inf.  Runs on the current stream
     of q's device."""
     import torch
-    c = _AttnCall(q, k, v, key_mask, scale, causal, q_pos, relpos, table)
-    out = c.made("out", out, c.q_shape)
-    B, Sq, H, _ = c.q_shape
+    shape, _, dev, head, args = _attn_inputs(q, k, v, key_mask, scale, causal, q_pos, relpos, table)
+    B, Sq, H, _ = shape
+    if out is None:
+        out = torch.empty(shape, dtype=q.dtype, device=q.device)
     if lse is None:
-        lse = torch.empty((B, H, Sq), dtype=torch.float32, device=c.dev)
-    else:
-        c.plain("lse", lse, torch.float32, (B, H, Sq))
-    c.run(load_library().attn_forward, (out.data_ptr(), lse.data_ptr()), 0)
+        lse = torch.empty((B, H, Sq), dtype=torch.float32, device=q.device)
+    packed = _ATTN_SHAPE.pack(*head, *_attn_strides("out", out, shape, q.dtype, dev), *(0,) * 12)
+    _attn_call(load_library().attn_forward, packed,
+               (*args, out.data_ptr(), _attn_plain("lse", lse, (B, H, Sq), torch.float32, dev)), 0,
+               dev)
     return out, lse
 
 
@@ -595,24 +583,29 @@ def attn_backward(q, k, v, out, lse, dout, key_mask=None, scale=None, causal=Fal
     """Gradients of <out, dout> for attn_forward's arguments, out and lse: returns
     dq, dk, dv and dtable (None without a table), written where given."""
     import torch
-    c = _AttnCall(q, k, v, key_mask, scale, causal, q_pos, relpos, table)
-    B, Sq, H, _ = c.q_shape
-    c.put("out", out, c.q_shape)
-    c.put("dout", dout, c.q_shape)
-    c.plain("lse", lse, torch.float32, (B, H, Sq))
-    dq = c.made("dq", dq, c.q_shape)
-    dk = c.made("dk", dk, c.kv_shape)
-    dv = c.made("dv", dv, c.kv_shape)
-    if table is None:
-        if dtable is not None:
-            _refuse("dtable without a table")
-    elif dtable is None:
+    q_shape, kv_shape, dev, head, args = _attn_inputs(q, k, v, key_mask, scale, causal, q_pos,
+                                                      relpos, table)
+    B, Sq, H, _ = q_shape
+    dtype = q.dtype
+    if dq is None:
+        dq = torch.empty(q_shape, dtype=dtype, device=q.device)
+    if dk is None:
+        dk = torch.empty(kv_shape, dtype=dtype, device=q.device)
+    if dv is None:
+        dv = torch.empty(kv_shape, dtype=dtype, device=q.device)
+    if table is None and dtable is not None:
+        _refuse("dtable without a table")
+    if table is not None and dtable is None:
         dtable = torch.empty_like(table)
-    else:
-        c.plain("dtable", dtable, torch.float32, tuple(table.shape))
-    c.run(load_library().attn_backward,
-          (out.data_ptr(), lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(),
-           dv.data_ptr(), _ptr(dtable)), 1)
+    packed = _ATTN_SHAPE.pack(*head, *_attn_strides("out", out, q_shape, dtype, dev),
+                              *_attn_strides("dout", dout, q_shape, dtype, dev),
+                              *_attn_strides("dq", dq, q_shape, dtype, dev),
+                              *_attn_strides("dk", dk, kv_shape, dtype, dev),
+                              *_attn_strides("dv", dv, kv_shape, dtype, dev))
+    to = None if dtable is None else _attn_plain("dtable", dtable, table.shape, torch.float32, dev)
+    _attn_call(load_library().attn_backward, packed,
+               (*args, out.data_ptr(), _attn_plain("lse", lse, (B, H, Sq), torch.float32, dev),
+                dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), to), 1, dev)
     return dq, dk, dv, dtable
 
 

@@ -221,13 +221,12 @@ struct KeyBlocks {
   Word w;
   uint64_t live;
 
-  __device__ __forceinline__ void init(const uint8_t* mask_row, int lim_, int first, int last,
-                                       int lane_) {
+  // (load(first) comes before the first next())
+  __device__ __forceinline__ void init(const uint8_t* mask_row, int lim_, int last, int lane_) {
     m = mask_row;
     lim = lim_;
     nblk = last;
     lane = lane_;
-    load(first);
   }
   // Bits of the keys of block b that are below lim.
   __device__ __forceinline__ Word in_range(int b) const {

@@ -14,10 +14,10 @@
 //     tile reads a table of the bias by distance that the work-group spread out
 //     in LDS (two reads for four scores);
 //   - the bias gradient: far tiles sum their dS in a register; a near tile adds
-//     its dS along the diagonals in LDS (per half wavefront, where the 32 lanes
-//     of one instruction hit 32 distances), then sums diagonals of one bucket
-//     with a segmented scan over the lanes.  One row of sums per work-group goes
-//     to memory; all in a fixed order.
+//     its dS along the diagonals (x_diagonals) to the wavefront's sums by distance
+//     in LDS; at the end distances of one bucket are summed with a segmented scan
+//     over the lanes.  One row of sums per work-group goes to memory; all in a
+//     fixed order.
 
 #include "xattn.h"
 
@@ -54,6 +54,27 @@ __device__ __forceinline__ void x_clear_hidden(char* kv, uint64_t word) {
   }
 }
 
+// The blocks of a pass over the keys, with the first of them on its way into stage
+// 0: block 0 is requested before the mask says whether it holds a key (it nearly
+// always does), so that the two latencies overlap.  Returns the first block.
+template <typename T>
+__device__ __forceinline__ int x_start(const XAttnArgs& a, int b, const T* K, const T* V, int lim,
+                                       char* kv, int wave, int lane, KeyBlocks<XKT>& blocks) {
+  constexpr int TILE = XKT * XT<T>::ROWB;
+  blocks.init(a.mask ? a.mask + (int64_t)b * a.Sk : nullptr, lim, (lim + XKT - 1) / XKT, lane);
+  if (blocks.nblk == 0) return 0;
+  x_dma<T, XKT, 4>(K, a.sk[1], 0, lim, kv, wave, lane);
+  x_dma<T, XKT, 4>(V, a.sv[1], 0, lim, kv + TILE, wave, lane);
+  blocks.load(0);
+  const int kb = blocks.next(0);
+  if (kb > 0) wait_all();  // (each wavefront writes its own rows of the tiles)
+  if (kb > 0 && kb < blocks.nblk) {
+    x_dma<T, XKT, 4>(K, a.sk[1], kb * XKT, lim, kv, wave, lane);
+    x_dma<T, XKT, 4>(V, a.sv[1], kb * XKT, lim, kv + TILE, wave, lane);
+  }
+  return kb;
+}
+
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
@@ -80,12 +101,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(
       x_frag((const T*)a.q + b * a.sq[0] + (int64_t)(q0 + rr) * a.sq[1] + h * a.sq[2],
              q0 + rr < a.Sq, hf);
   KeyBlocks<XKT> blocks;
-  blocks.init(a.mask ? a.mask + (int64_t)b * a.Sk : nullptr, lim, 0, (lim + XKT - 1) / XKT, lane);
-  int kb = blocks.next(0);
-  if (kb < blocks.nblk) {
-    x_dma<T, XKT, 4>(K, a.sk[1], kb * XKT, lim, lds, wave, lane);
-    x_dma<T, XKT, 4>(V, a.sv[1], kb * XKT, lim, lds + TILE, wave, lane);
-  }
+  int kb = x_start(a, b, K, V, lim, lds, wave, lane, blocks);
   float far_l = 0.0f, far_r = 0.0f;
   const int mid = a.reach + XPAD;
   if constexpr (BIAS) {
@@ -187,23 +203,75 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(
 
 // ---------------------------------------------------------------------------
 // Backward, dQ and the bias gradient.  RED: D is formed from P and dP in a pass of
-// its own over the keys; else it is rowsum(dO * out).
+// its own over the keys.  Else it starts as D' = rowsum(dO * out); on bf16 out's
+// rounding makes the rows of P (dP - D') sum to D - D' instead of zero, which is of
+// the size of dS where few keys take most of P: that sum and P K are kept as well,
+// and dQ and D corrected at the end.
 // ---------------------------------------------------------------------------
+
+// The sums of a 32 x 32 accumulator along its diagonals (lane = query, registers =
+// keys, x_acc order): lane l gets the sum over all (key, query) with key - query =
+// 31 - l, lane 63 zero.  Going through the keys upwards, the running sums move one
+// lane up per key, as the diagonals do; half a register at a time with zeros above,
+// so that diagonals which leave query 31 go on in the upper lanes.  96 vector
+// instructions and no LDS: adding the 1024 values to 63 sums in LDS took 190 cycles
+// per atomic of a wavefront (the dQ kernel of 32 x 512 tokens and 12 heads 315 us).
+__device__ __forceinline__ float x_diagonals(const f32x16_t& s) {
+  float d = 0.0f;
+  auto step = [&](uint32_t v) {
+    const float up = __uint_as_float(
+        __builtin_amdgcn_update_dpp(0, __float_as_uint(d), 0x138 /* wave_shr:1 */, 0xf, 0xf, true));
+    d = up + __uint_as_float(v);
+  };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t hi[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[4 * i + e]), 0u, false, false);
+      step(r[0]);
+      hi[e] = r[1];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) step(hi[e]);
+  }
+  return d;
+}
+
+// Adds v of lane l, the sum at distance rel0 + l (lanes from n on have none), to
+// its bucket.  Buckets are runs of distances: each run is summed into its last lane.
+__device__ __forceinline__ void x_add_buckets(const XAttnArgs& a, float v, int rel0, int n, int lane,
+                                              float* bsum) {
+  const int bk = lane < n ? x_bucket(a, rel0 + lane) : -1;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const float u = __shfl_up(v, o, 64);
+    const int ub = __shfl_up(bk, o, 64);
+    if (lane >= o && ub == bk) v += u;
+  }
+  const int nb = __shfl_down(bk, 1, 64);
+  if (bk >= 0 && (lane == 63 || nb != bk)) bsum[bk] += v;
+  lds_wait();
+  __builtin_amdgcn_wave_barrier();
+}
+
 template <typename T, bool BIAS, bool RED>
 __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
   constexpr int TILE = XKT * XT<T>::ROWB;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  // [2][K, V]; with a bias: dist, the wavefronts' diagonal sums [4][2][64] and
-  // bucket sums [4][nb]
+  // [2][K, V]; with a bias: dist, the wavefronts' sums by distance [4][nd] and by
+  // bucket [4][nb]
+  constexpr bool FIX = sizeof(T) == 2 && !RED;
   float* dist = (float*)(lds + 4 * TILE);
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   float* diag = nullptr;
   float* bsum = nullptr;
+  const int nd = x_dist_n(a);
   if constexpr (BIAS) {
     float* p = dist + ((x_dist_n(a) + 3) & ~3);
-    diag = p + wave * 128;
-    bsum = p + 512 + wave * a.nb;
+    diag = p + wave * nd;
+    bsum = p + 4 * nd + wave * a.nb;
   }
 
   int qb, bh;
@@ -244,20 +312,17 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
     x_fill_dist(a, h, dist);
     far_l = a.table[(int64_t)x_bucket(a, -a.reach) * a.H + h] * XLOG2E;
     far_r = a.table[(int64_t)x_bucket(a, a.reach) * a.H + h] * XLOG2E;
-    diag[lane] = diag[64 + lane] = 0.0f;
+    for (int i = lane; i < nd; i += 64) diag[i] = 0.0f;
     for (int i = lane; i < a.nb; i += 64) bsum[i] = 0.0f;
   }
 
   f32x16_t dq[2] = {zero16(), zero16()};
+  f32x16_t pk[2] = {zero16(), zero16()};  // FIX: P K
+  float rsum = 0.0f;                      // FIX: row sum of dS; RED: of P
   auto sweep = [&](auto first) {
     constexpr bool SUM_D = decltype(first)::value;
     KeyBlocks<XKT> blocks;
-    blocks.init(a.mask ? a.mask + (int64_t)b * a.Sk : nullptr, lim, 0, (lim + XKT - 1) / XKT, lane);
-    int kb = blocks.next(0);
-    if (kb < blocks.nblk) {
-      x_dma<T, XKT, 4>(K, a.sk[1], kb * XKT, lim, lds, wave, lane);
-      x_dma<T, XKT, 4>(V, a.sv[1], kb * XKT, lim, lds + TILE, wave, lane);
-    }
+    int kb = x_start(a, b, K, V, lim, lds, wave, lane, blocks);
     for (int st = 0; kb < blocks.nblk; st ^= 1) {
       const uint64_t word = blocks.word(kb);
       const uint64_t hidden = blocks.in_range(kb) & ~word;
@@ -280,7 +345,10 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
         const uint32_t rows = (uint32_t)(word >> (32 * sub));
         if (rows == 0 || (a.causal && k0 > p0 + 31)) continue;
         f32x16_t s = x_mma_rows(kv, 32 * sub, qf, zero16(), lane);
-        f32x16_t dp = x_mma_rows(kv + TILE, 32 * sub, dof, splat16(SUM_D ? 0.0f : -D), lane);
+        // (RED: both passes form the same dP, so that the matrix core's rounding,
+        // which is one-sided, cancels in dP - D; from an accumulator that starts at
+        // -D the sums over a bucket of 3 million pairs were off by 1e-6)
+        f32x16_t dp = x_mma_rows(kv + TILE, 32 * sub, dof, splat16(RED ? 0.0f : -D), lane);
         const bool full = rows == 0xffffffffu && (!a.causal || k0 + 31 <= p0);
         const bool near = BIAS && k0 + 31 - p0 > -a.reach && k0 - p0 - 31 < a.reach;
         if (near) {
@@ -301,39 +369,21 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
         }
         if constexpr (SUM_D) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) D = fmaf(s[r], dp[r], D);
+          for (int r = 0; r < 16; ++r) {
+            D = fmaf(s[r], dp[r], D);
+            rsum += s[r];
+          }
         } else {
+          if constexpr (FIX) x_mma_cols<T>(kv, 32 * sub, s, pk, lane);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] *= dp[r];  // dS
+          for (int r = 0; r < 16; ++r) {
+            s[r] *= RED ? dp[r] - D : dp[r];  // dS
+            if constexpr (FIX) rsum += s[r];
+          }
           if constexpr (BIAS) {
             if (a.dtable && near) {
-              // lane (query) rr, register r (key): distance k0 - p0 - 31 + e with
-              // e = key - rr + 31; one instruction's 32 lanes of a half have 32
-              // distances
-              float* e = diag + 64 * hf + 4 * hf - rr + 31;
-#pragma unroll
-              for (int r = 0; r < 16; ++r)
-                __hip_atomic_fetch_add(e + 8 * (r >> 2) + (r & 3), s[r], __ATOMIC_RELAXED,
-                                       __HIP_MEMORY_SCOPE_WAVEFRONT);
-              lds_wait();
-              __builtin_amdgcn_wave_barrier();
-              float v = diag[lane] + diag[64 + lane];
-              lds_wait();
-              __builtin_amdgcn_wave_barrier();
-              diag[lane] = diag[64 + lane] = 0.0f;
-              // Buckets are runs of distances: sum each run into its last lane.
-              // Lane 63 has none.
-              const int bk = lane < 63 ? x_bucket(a, k0 - p0 - 31 + lane) : -1;
-#pragma unroll
-              for (int o = 1; o < 64; o <<= 1) {
-                const float u = __shfl_up(v, o, 64);
-                const int ub = __shfl_up(bk, o, 64);
-                if (lane >= o && ub == bk) v += u;
-              }
-              const int nb = __shfl_down(bk, 1, 64);
-              if (lane < 63 && nb != bk) bsum[bk] += v;
-              lds_wait();
-              __builtin_amdgcn_wave_barrier();
+              const float v = x_diagonals(s);
+              if (lane < 63) diag[k0 - p0 + 31 - lane + mid] += v;
             } else if (a.dtable) {
               float t = s[0];
 #pragma unroll
@@ -351,13 +401,33 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
   };
   if constexpr (RED) {
     sweep(std::true_type());
-    const HalfPair pr = half_pair(D);
-    D = pr.x + pr.y;
+    // Over the sum of these P, which the log-sum-exp's rounding leaves off 1: the
+    // rows of dS then sum to zero to the last bits, as far buckets of long rows
+    // need.
+    const HalfPair pr = half_pair(D), ps = half_pair(rsum);
+    const float total = ps.x + ps.y;
+    D = total == 0.0f ? 0.0f : (pr.x + pr.y) / total;
+  }
+  sweep(std::false_type());
+  if constexpr (FIX) {
+    const HalfPair pr = half_pair(rsum);
+    const float off = pr.x + pr.y;
+    D += off;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq[t][r] = fmaf(-off, pk[t][r], dq[t][r]);
   }
   if (hf == 0 && qv) a.dsum[row] = D;
-  sweep(std::false_type());
   if constexpr (BIAS) {
     if (a.dtable) {
+      const float* all = diag - wave * nd;  // (after the pass's last barrier)
+      for (int e0 = 64 * wave; e0 < nd; e0 += 256) {
+        const int e = e0 + lane;
+        const float v =
+            e < nd ? (all[e] + all[nd + e]) + (all[2 * nd + e] + all[3 * nd + e]) : 0.0f;
+        x_add_buckets(a, v, e0 - mid, nd - e0, lane, bsum);
+      }
       gfar_l = wave_sum(gfar_l);
       gfar_r = wave_sum(gfar_r);
       if (lane == 0) {
@@ -414,15 +484,14 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
   // Queries from q_first on see a key of this work-group, those before it none.
   const int q_first = a.causal ? max(0, kblk * XQB - qp) : 0;
   const int qb0 = q_first / QB, nqb = max(0, (a.Sq + QB - 1) / QB - qb0), n_it = nqb * a.rep;
-  // A key that the mask hides, or no query sees, may hold anything.
+  typename XT<T>::Frag kf = x_frag(
+      (const T*)a.k + b * a.sk[0] + (int64_t)key * a.sk[1] + g * a.sk[2], key < a.Sk, hf);
+  typename XT<T>::Frag vf = x_frag(
+      (const T*)a.v + b * a.sv[0] + (int64_t)key * a.sv[1] + g * a.sv[2], key < a.Sk, hf);
   const bool kvalid = key < a.Sk && (!a.causal || key - qp < a.Sq) &&
                       (!a.mask || a.mask[(int64_t)b * a.Sk + key] != 0);
   const bool all_valid = __all(kvalid);
   const uint32_t kbits = kvalid ? 0xffffffffu : 0u;
-  const typename XT<T>::Frag kf = x_frag(
-      (const T*)a.k + b * a.sk[0] + (int64_t)key * a.sk[1] + g * a.sk[2], kvalid, hf);
-  const typename XT<T>::Frag vf = x_frag(
-      (const T*)a.v + b * a.sv[0] + (int64_t)key * a.sv[1] + g * a.sv[2], kvalid, hf);
   const T* Q = (const T*)a.q + b * a.sq[0];
   const T* dO = (const T*)a.dout + b * a.sdo[0];
 
@@ -450,6 +519,15 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
     dma(0, lds);
     row_store(row_raw(0), 0);
     if (n_it > 1) raw = row_raw(1);
+  }
+  // A key that the mask hides, or no query sees, may hold anything.  (After the
+  // first loads, so that the rows do not wait for the mask.)
+  if (!all_valid) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(kf) / 16); ++i) {
+      kf.f[i] = kvalid ? kf.f[i] : __builtin_bit_cast(decltype(kf.f[0] + kf.f[0]), zero4());
+      vf.f[i] = kvalid ? vf.f[i] : __builtin_bit_cast(decltype(vf.f[0] + vf.f[0]), zero4());
+    }
   }
   const int mid = a.reach + XPAD;
   float far_l = 0.0f, far_r = 0.0f;
@@ -556,7 +634,7 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
     if (!a.table) {
       e = launch(xattn_dq_kernel<T, false, false>, gq, lds, st, a);
     } else {
-      lds += dist_bytes(a) + (512 + 4 * (size_t)a.nb) * 4;
+      lds += dist_bytes(a) + 4 * (size_t)(2 * (a.reach + XPAD) + 1 + a.nb) * 4;
       // The bias gradient is a sum of many dS that nearly cancel, in fp32: with
       // D from a bf16 out it would be off by out's rounding.
       if (sizeof(T) == 2 && a.dtable)

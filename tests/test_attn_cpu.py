@@ -58,15 +58,14 @@ def test_bucket_refusals(num, far, both):
 
 
 def shape(**kw):
-    s = Bn._AttnShape()
-    s.dtype, s.batch, s.seq_q, s.seq_k, s.heads, s.kv_heads = 1, 2, 5, 7, 4, 2
-    s.causal, s.scale = 0, 0.125
+    d = dict(dtype=1, batch=2, seq_q=5, seq_k=7, heads=4, kv_heads=2, causal=0, scale=0.125)
     for n, S, H in (("q", 5, 4), ("k", 7, 2), ("v", 7, 2), ("out", 5, 4), ("dout", 5, 4),
                     ("dq", 5, 4), ("dk", 7, 2), ("dv", 7, 2)):
-        setattr(s, n, (S * H * 64, H * 64, 64))
-    for n, v in kw.items():
-        setattr(s, n, v)
-    return s
+        d[n] = (S * H * 64, H * 64, 64)
+    assert set(kw) <= set(d)
+    d.update(kw)
+    flat = [x for v in d.values() for x in (v if isinstance(v, tuple) else (v,))]
+    return Bn._ATTN_SHAPE.pack(*flat)
 
 
 # Addresses that are never read: every call below is refused.
@@ -80,7 +79,7 @@ def call(backward, s, rp=None, ws_bytes=1 << 20, **ptr):
     if rp is None:
         p["table"] = p["dtable"] = None
     p.update(ptr)
-    head = [ctypes.byref(s) if s is not None else None, ctypes.byref(rp) if rp is not None else None,
+    head = [s, ctypes.byref(rp) if rp is not None else None,
             p["table"], p["q"], p["k"], p["v"], p["mask"], p["q_pos"], p["out"], p["lse"]]
     if backward:
         st = lib.attn_backward(*head, p["dout"], p["dq"], p["dk"], p["dv"], p["dtable"], p["ws"],
@@ -156,17 +155,17 @@ def test_table_and_buckets_refused():
 def test_workspace():
     lib, n = P.load_library(), ctypes.c_size_t(7)
     s, rp = shape(), P.RelPos(32, 128).c
-    assert lib.attn_workspace(ctypes.byref(s), None, 1, ctypes.byref(n)) == 0
+    assert lib.attn_workspace(s, None, 1, ctypes.byref(n)) == 0
     need = n.value
     assert need >= 2 * 4 * 5 * 4
     assert call(1, s, ws_bytes=need - 1)[0] == 1
     assert call(1, s, ws=None)[0] == 1
     assert call(1, s, ws=PTR["ws"] + 8)[0] == 1
-    assert lib.attn_workspace(ctypes.byref(s), ctypes.byref(rp), 1, ctypes.byref(n)) == 0
+    assert lib.attn_workspace(s, ctypes.byref(rp), 1, ctypes.byref(n)) == 0
     assert n.value >= need + 2 * 4 * 32 * 4
     assert call(1, s, rp, ws_bytes=n.value - 1)[0] == 1
-    assert lib.attn_workspace(ctypes.byref(s), None, 2, ctypes.byref(n)) == 1
-    assert lib.attn_workspace(ctypes.byref(s), None, 0, None) == 1
+    assert lib.attn_workspace(s, None, 2, ctypes.byref(n)) == 1
+    assert lib.attn_workspace(s, None, 0, None) == 1
     assert lib.attn_workspace(None, None, 0, ctypes.byref(n)) == 1
     assert call(0, None)[0] == 1
 
