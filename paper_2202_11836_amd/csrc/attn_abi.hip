@@ -1,9 +1,9 @@
 // C ABI of the attention operators (include/attn.h): argument checks, the borders
 // of the relative position buckets, the workspace's layout.
+#include <climits>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
-#include <cstring>
 
 #include "xattn.h"
 
@@ -78,15 +78,29 @@ bool relpos_ok(const attn_relpos* rp) {
 int64_t row_blocks(int n) { return ((int64_t)n + 127) / 128; }
 
 struct Workspace {
-  int64_t dsum, tpart, total;  // bytes
+  int64_t dsum, tpart, part, total;  // bytes
+  XKvPlan kv;
+  XFewPlan few;
 };
 Workspace workspace_of(const attn_shape* s, const attn_relpos* rp, bool backward) {
   Workspace w{};
-  if (!backward) return w;
+  const int rep = s->heads / s->kv_heads;
+  if (!backward) {
+    w.few = xattn_few_plan(s->batch, s->kv_heads, rep, s->seq_q, s->seq_k, rp ? rp->num_buckets : 0,
+                           rp ? rp->reach : 0, s->dtype);
+    if (w.few.splits > 1)
+      w.part = (int64_t)w.few.splits * s->batch * s->kv_heads * xattn_few_tiles(rep, s->seq_q) * 32 *
+               XFEW_ROW * 4;
+    w.total = w.part;
+    return w;
+  }
   w.dsum = ((int64_t)s->batch * s->heads * s->seq_q * 4 + 15) / 16 * 16;
   if (rp)
     w.tpart = ((int64_t)s->batch * s->heads * row_blocks(s->seq_q) * rp->num_buckets * 4 + 15) / 16 * 16;
-  w.total = w.dsum + w.tpart;
+  w.kv = xattn_kv_plan(s->batch, s->kv_heads, rep, s->seq_q, s->seq_k, s->causal, s->dtype);
+  if (w.kv.splits > 1)
+    w.part = (int64_t)w.kv.splits * s->batch * s->kv_heads * s->seq_k * 2 * XHD * 4;
+  w.total = w.dsum + w.tpart + w.part;
   return w;
 }
 
@@ -163,7 +177,8 @@ void fill_common(XAttnArgs* a, const attn_shape* s, const attn_relpos* rp, const
     a->one = a->nbd / 2;
     a->reach = rp->reach;
     a->n_borders = rp->n_borders;
-    memcpy(a->border, rp->border, sizeof(a->border));
+    for (int i = 0; i < ATTN_MAX_BUCKETS / 2; ++i)
+      a->border[i] = i < rp->n_borders ? rp->border[i] : INT_MAX;
   }
 }
 
@@ -268,6 +283,9 @@ stage_status attn_forward(const attn_shape* s, const attn_relpos* rp, const floa
   a.q_pos = q_pos;
   a.out = out;
   a.lse = lse;
+  a.part = (float*)workspace;
+  a.few_waves = w.few.waves;
+  a.few_splits = w.few.splits;
   const hipError_t e = xattn_forward(a, s->dtype, (hipStream_t)hip_stream);
   if (e != hipSuccess) return bad(STAGE_EHIP, "attn_forward: %s", hipGetErrorString(e));
   return STAGE_OK;
@@ -323,6 +341,9 @@ stage_status attn_backward(const attn_shape* s, const attn_relpos* rp, const flo
   a.dtable = dtable;
   a.dsum = (float*)workspace;
   a.tpart = (float*)((char*)workspace + w.dsum);
+  a.part = (float*)((char*)workspace + w.dsum + w.tpart);
+  a.kv_chunk = w.kv.chunk;
+  a.kv_splits = w.kv.splits;
   const hipError_t e = xattn_backward(a, s->dtype, (hipStream_t)hip_stream);
   if (e != hipSuccess) return bad(STAGE_EHIP, "attn_backward: %s", hipGetErrorString(e));
   return STAGE_OK;

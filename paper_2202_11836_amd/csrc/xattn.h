@@ -26,14 +26,37 @@ struct XAttnArgs {
   int64_t sq[3], sk[3], sv[3], so[3], sdo[3], sdq[3], sdk[3], sdv[3];
   int B, Sq, Sk, H, G, rep;  // G key heads, rep = H / G query heads to each
   int causal;
-  int nsplit;
+  int kv_chunk, kv_splits;   // XKvPlan
+  int few_waves, few_splits; // XFewPlan
   float c;      // scale * log2(e)
   float scale;
   // Buckets (attn_relpos): nb in all, nbd to a direction, `one` of them with one
   // distance each.
   int nb, nbd, one, both, reach, n_borders;
-  int border[ATTN_MAX_BUCKETS / 2];
+  int border[ATTN_MAX_BUCKETS / 2];  // INT_MAX from n_borders on
 };
+
+// How the dK / dV kernel goes through the query blocks (of XKvPlan::rows queries of
+// one head) that a block of 128 keys meets: `chunk` of them to a work-group, and with
+// splits > 1 each chunk's fp32 sums go to the workspace, [split][B, G][Sk][dK | dV].
+struct XKvPlan {
+  int rows, chunk, splits;
+};
+XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_dtype dt);
+
+// The forward kernel that serves few queries (xattn_few.hip): wavefronts of a
+// work-group and splits of the keys, 0 splits where the other kernel is faster.  With
+// more than one split it leaves, in the workspace, per split and row (query and query
+// head of a key head, in tiles of 32) XFEW_ROW floats: 64 sums of P v, the exponents'
+// offset and the sum of P.  buckets, reach: of the bias, 0 without one.
+constexpr int XFEW_ROW = 68;
+struct XFewPlan {
+  int waves, splits;
+};
+XFewPlan xattn_few_plan(int B, int G, int rep, int Sq, int Sk, int buckets, int reach,
+                        stage_dtype dt);
+inline int64_t xattn_few_tiles(int rep, int Sq) { return ((int64_t)Sq * rep + 31) / 32; }
+hipError_t xattn_few(const XAttnArgs& a, stage_dtype dt, hipStream_t st);
 
 hipError_t xattn_forward(const XAttnArgs& a, stage_dtype dt, hipStream_t st);
 hipError_t xattn_backward(const XAttnArgs& a, stage_dtype dt, hipStream_t st);
@@ -55,7 +78,10 @@ __device__ __forceinline__ int x_bucket(const XAttnArgs& a, int rel) {
   const int n = rel <= 0 ? -rel : (a.both ? rel : 0);
   if (n < a.one) return base + n;
   int b = base + a.one;
-  for (int i = 0; i < a.n_borders; ++i) b += n >= a.border[i];
+  for (int i = 0; i < a.n_borders; i += 8) {  // (padded; eight to a scalar load)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b += n >= a.border[i + j];
+  }
   return b;
 }
 
@@ -207,6 +233,12 @@ __device__ __forceinline__ void x_store(const f32x16_t acc[2], float mul, T* sta
   }
 }
 
+// "At most N vector memory operations outstanding, no LDS operation" (gfx9 encoding).
+template <int N>
+__device__ __forceinline__ void x_wait_vm() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | 0x70 | (((N >> 4) & 3) << 14));
+}
+
 // The blocks of BK keys that a wavefront goes through: those of [0, nblk) that
 // hold a key below lim which the mask leaves.  A window of 64 blocks is held at a
 // time, lane i with the mask bits of its block base + i, so that a block's bits
@@ -283,11 +315,20 @@ struct KeyBlocks {
   }
 };
 
-// Bit r of a lane's word: whether register r's row of a 32 x 32 tile with bits
-// `rows` is set, moved so that the test of register r is of bit 8 (r / 4) + r % 4.
+// A lane's bits of a 32 x 32 tile whose rows have bits `rows`: that of register r is
+// bit 8 (r / 4) + r % 4.
 __device__ __forceinline__ uint32_t x_lane_bits(uint32_t rows, int hf) { return rows >> (4 * hf); }
-__device__ __forceinline__ bool x_bit(uint32_t bits, int r) {
-  return (bits >> (8 * (r >> 2) + (r & 3))) & 1;
+// All ones or zeros by the bit of register r, and v where it is set, else 0 or -inf
+// (one instruction each; a compare and a select would be three).
+__device__ __forceinline__ uint32_t x_mask(uint32_t bits, int r) {
+  return (uint32_t)__builtin_amdgcn_sbfe((int)bits, 8 * (r >> 2) + (r & 3), 1);
+}
+__device__ __forceinline__ float x_or_zero(float v, uint32_t bits, int r) {
+  return __uint_as_float(__float_as_uint(v) & x_mask(bits, r));
+}
+__device__ __forceinline__ float x_or_ninf(float v, uint32_t bits, int r) {
+  const uint32_t m = x_mask(bits, r);
+  return __uint_as_float((__float_as_uint(v) & m) | (0xff800000u & ~m));
 }
 // The low n + 1 bits (none for n < 0, all from 31 on).
 __device__ __forceinline__ uint32_t x_upto(int n) {

@@ -19,6 +19,8 @@
 //     over the lanes.  One row of sums per work-group goes to memory; all in a
 //     fixed order.
 
+#include <algorithm>
+
 #include "xattn.h"
 
 namespace {
@@ -157,7 +159,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = x_bit(bits, r) ? s[r] : -INFINITY;
+          s[r] = x_or_ninf(s[r], bits, r);
           mblk = fmaxf(mblk, s[r]);
         }
         mul = 1.0f;
@@ -365,7 +367,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
           uint32_t bits = x_lane_bits(rows, hf);
           if (a.causal) bits &= x_upto(p0 + rr - k0 - 4 * hf);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = x_bit(bits, r) ? s[r] : 0.0f;
+          for (int r = 0; r < 16; ++r) s[r] = x_or_zero(s[r], bits, r);
         }
         if constexpr (SUM_D) {
 #pragma unroll
@@ -451,6 +453,11 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
 // gradient: one per bucket and head.
 // ---------------------------------------------------------------------------
 template <typename T> constexpr int x_qb() { return sizeof(T) == 2 ? 128 : 64; }
+// LDS: [2][Q, dO], per stage lse and -D of QB rows, a word per wavefront; with a bias
+// its table by distance follows.
+template <typename T> constexpr int kv_lds() {
+  return 4 * x_qb<T>() * XT<T>::ROWB + 4 * x_qb<T>() * 4 + 16;
+}
 
 __device__ __forceinline__ void x_dtable_sum(const XAttnArgs& a, int w, float* red) {
   const int c = w % a.nb, h = w / a.nb, nq = (a.Sq + XQB - 1) / XQB;
@@ -467,9 +474,8 @@ template <typename T, bool BIAS>
 __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_kv) {
   constexpr int QB = x_qb<T>(), TILE = QB * XT<T>::ROWB;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  // [2][Q, dO]; per stage lse and -D of QB rows; with a bias: dist
   float* rowv = (float*)(lds + 4 * TILE);
-  float* dist = rowv + 4 * QB;
+  float* dist = (float*)(lds + kv_lds<T>());
   if ((int)blockIdx.x >= n_kv) {
     x_dtable_sum(a, blockIdx.x - n_kv, rowv);
     return;
@@ -477,21 +483,32 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int kblk, bg;
-  attn_block(blockIdx.x, n_kv, (a.Sk + XQB - 1) / XQB, kblk, bg);
+  attn_block(blockIdx.x, n_kv, (a.Sk + XQB - 1) / XQB * a.kv_splits, kblk, bg);
+  const int split = kblk % a.kv_splits;
+  kblk /= a.kv_splits;
   const int b = bg / a.G, g = bg % a.G;
   const int k0 = kblk * XQB + wave * 32, key = k0 + rr;
   const int qp = x_q_pos(a, b);
   // Queries from q_first on see a key of this work-group, those before it none.
   const int q_first = a.causal ? max(0, kblk * XQB - qp) : 0;
-  const int qb0 = q_first / QB, nqb = max(0, (a.Sq + QB - 1) / QB - qb0), n_it = nqb * a.rep;
-  typename XT<T>::Frag kf = x_frag(
-      (const T*)a.k + b * a.sk[0] + (int64_t)key * a.sk[1] + g * a.sk[2], key < a.Sk, hf);
-  typename XT<T>::Frag vf = x_frag(
-      (const T*)a.v + b * a.sv[0] + (int64_t)key * a.sv[1] + g * a.sv[2], key < a.Sk, hf);
+  const int qb0 = q_first / QB, nqb = max(0, (a.Sq + QB - 1) / QB - qb0);
+  const int it0 = split * a.kv_chunk;
+  int n_it = min(nqb * a.rep, it0 + a.kv_chunk);
+  if (split > 0 && it0 >= n_it) return;  // (the sum knows which splits there are)
+  // A key that the mask hides, or no query sees, may hold anything: its rows are not
+  // read, and a work-group without another key only writes zeros.  (The rows wait for
+  // the mask this way; but few queries make this a copy of K and V to dK and dV: 32 x
+  // 16 heads of 128 queries and 512 keys, half of them hidden, 40 -> 36 us.)
   const bool kvalid = key < a.Sk && (!a.causal || key - qp < a.Sq) &&
                       (!a.mask || a.mask[(int64_t)b * a.Sk + key] != 0);
-  const bool all_valid = __all(kvalid);
+  const bool all_valid = __all(kvalid), any_valid = __any(kvalid);
   const uint32_t kbits = kvalid ? 0xffffffffu : 0u;
+  if (a.mask) {
+    int* any = (int*)(lds + kv_lds<T>() - 16);
+    any[wave] = any_valid;
+    __syncthreads();
+    if (!(any[0] | any[1] | any[2] | any[3])) n_it = it0;
+  }
   const T* Q = (const T*)a.q + b * a.sq[0];
   const T* dO = (const T*)a.dout + b * a.sdo[0];
 
@@ -515,26 +532,21 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
       rowv[st * 2 * QB + tid] = tid >= QB ? -raw : raw == -INFINITY ? INFINITY : raw * XLOG2E;
   };
   float raw = 0.0f;
-  if (n_it > 0) {
-    dma(0, lds);
-    row_store(row_raw(0), 0);
-    if (n_it > 1) raw = row_raw(1);
-  }
-  // A key that the mask hides, or no query sees, may hold anything.  (After the
-  // first loads, so that the rows do not wait for the mask.)
-  if (!all_valid) {
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(kf) / 16); ++i) {
-      kf.f[i] = kvalid ? kf.f[i] : __builtin_bit_cast(decltype(kf.f[0] + kf.f[0]), zero4());
-      vf.f[i] = kvalid ? vf.f[i] : __builtin_bit_cast(decltype(vf.f[0] + vf.f[0]), zero4());
-    }
+  const typename XT<T>::Frag kf = x_frag(
+      (const T*)a.k + b * a.sk[0] + (int64_t)key * a.sk[1] + g * a.sk[2], kvalid && it0 < n_it, hf);
+  const typename XT<T>::Frag vf = x_frag(
+      (const T*)a.v + b * a.sv[0] + (int64_t)key * a.sv[1] + g * a.sv[2], kvalid && it0 < n_it, hf);
+  if (it0 < n_it) {
+    dma(it0, lds);
+    row_store(row_raw(it0), 0);
+    if (it0 + 1 < n_it) raw = row_raw(it0 + 1);
   }
   const int mid = a.reach + XPAD;
   float far_l = 0.0f, far_r = 0.0f;
   f32x16_t dv[2] = {zero16(), zero16()}, dk[2] = {zero16(), zero16()};
   int cur_h = -1;
-  for (int it = 0; it < n_it; ++it) {
-    const int st = it & 1;
+  for (int it = it0; it < n_it; ++it) {
+    const int st = (it - it0) & 1;
     const int h = head(it), qr = qrow(it);
     wait_all();
     __syncthreads();
@@ -557,7 +569,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
     for (int sub = 0; sub < QB / 32; ++sub) {
       const int r0 = qr + 32 * sub;   // first query
       const int p0 = r0 + qp;         // its position
-      if (r0 >= a.Sq || (a.causal && k0 > p0 + 31)) continue;
+      if (!any_valid || r0 >= a.Sq || (a.causal && k0 > p0 + 31)) continue;
       f32x16_t dp;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -569,26 +581,31 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
       dp = x_mma_rows(dOs, 32 * sub, vf, dp, lane);
       const bool full = all_valid && (!a.causal || k0 + 31 <= p0);
       const bool near = BIAS && k0 + 31 - p0 > -a.reach && k0 - p0 - 31 < a.reach;
-      const float far = !BIAS ? 0.0f : k0 > p0 ? far_r : far_l;
-      const float* d = dist + (k0 + rr - p0 - 4 * hf + mid);
       // Key rr is seen by the queries from rr + k0 - p0 on.
       uint32_t bits = kbits;
       if (a.causal) bits &= ~x_upto(k0 + rr - p0 - 4 * hf - 1);
+      if constexpr (!BIAS) {
+      } else if (near) {
+        const float* d = dist + (k0 + rr - p0 - 4 * hf + mid);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, d[-(8 * (r >> 2) + (r & 3))]);
+      } else {
+        const float far = k0 > p0 ? far_r : far_l;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, far);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const f32x4_t l4 = *(const f32x4_t*)(lv + 32 * sub + 8 * i + 4 * hf);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int r = 4 * i + e;
-          float x;
-          if (near) x = fmaf(s[r], a.c, d[-(8 * i + e)]) - l4[e];
-          else x = fmaf(s[r], a.c, BIAS ? far - l4[e] : -l4[e]);
-          s[r] = __builtin_amdgcn_exp2f(x);
+          const float x = s[4 * i + e];
+          s[4 * i + e] = __builtin_amdgcn_exp2f(BIAS ? x - l4[e] : fmaf(x, a.c, -l4[e]));
         }
       }
       if (!full) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = x_bit(bits, r) ? s[r] : 0.0f;
+        for (int r = 0; r < 16; ++r) s[r] = x_or_zero(s[r], bits, r);
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) dp[r] *= s[r];  // dS
@@ -599,11 +616,43 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
     raw = raw2;
   }
   __syncthreads();  // the ring becomes the output staging area
+  if (a.kv_splits > 1) {
+    float* to = a.part + ((int64_t)split * a.B * a.G + bg) * a.Sk * 2 * XHD;
+    float* stage = (float*)lds + wave * 32 * XT<float>::LD;
+    x_store<float>(dk, a.scale, stage, to, 2 * XHD, k0, a.Sk);
+    lds_wait();
+    __builtin_amdgcn_wave_barrier();
+    x_store<float>(dv, 1.0f, stage, to + XHD, 2 * XHD, k0, a.Sk);
+    return;
+  }
   T* stage = (T*)lds + wave * 32 * XT<T>::LD;
   x_store<T>(dk, a.scale, stage, (T*)a.dk + b * a.sdk[0] + g * a.sdk[2], a.sdk[1], k0, a.Sk);
   lds_wait();
   __builtin_amdgcn_wave_barrier();
   x_store<T>(dv, 1.0f, stage, (T*)a.dv + b * a.sdv[0] + g * a.sdv[2], a.sdv[1], k0, a.Sk);
+}
+
+// dK and dV from their splits, in order: 32 threads to a key, 4 values each.
+template <typename T>
+__global__ __launch_bounds__(256) void xattn_kv_sum_kernel(XAttnArgs a) {
+  constexpr int QB = x_qb<T>();
+  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), n = (int64_t)a.B * a.G * a.Sk;
+  if (row >= n) return;
+  const int key = (int)(row % a.Sk), bg = (int)(row / a.Sk), b = bg / a.G, g = bg % a.G;
+  const int c = (threadIdx.x & 31) * 4;
+  const int qp = x_q_pos(a, b);
+  const int q_first = a.causal ? max(0, key / XQB * XQB - qp) : 0;
+  const int n_it = max(0, (a.Sq + QB - 1) / QB - q_first / QB) * a.rep;
+  const int splits = max(1, (n_it + a.kv_chunk - 1) / a.kv_chunk);
+  f32x4_t t = {0.0f, 0.0f, 0.0f, 0.0f};
+  const float* p = a.part + row * 2 * XHD + c;
+  for (int i = 0; i < splits; ++i) t += *(const f32x4_t*)(p + (int64_t)i * n * 2 * XHD);
+  T* to = c < XHD ? (T*)a.dk + b * a.sdk[0] + (int64_t)key * a.sdk[1] + g * a.sdk[2] + c
+                  : (T*)a.dv + b * a.sdv[0] + (int64_t)key * a.sdv[1] + g * a.sdv[2] + c - XHD;
+  if constexpr (sizeof(T) == 2)
+    *(u32x2_t*)to = u32x2_t{pack_bf16x2(t[0], t[1]), pack_bf16x2(t[2], t[3])};
+  else
+    *(f32x4_t*)to = t;
 }
 
 template <typename K>
@@ -618,6 +667,7 @@ size_t dist_bytes(const XAttnArgs& a) {
 
 template <typename T>
 hipError_t forward_t(const XAttnArgs& a, hipStream_t st) {
+  if (a.few_splits > 0) return xattn_few(a, sizeof(T) == 2 ? STAGE_BF16 : STAGE_F32, st);
   const int64_t grid = (int64_t)a.B * a.H * ((a.Sq + XQB - 1) / XQB);
   const size_t lds = 4 * XKT * XT<T>::ROWB + dist_bytes(a);
   if (grid == 0) return hipSuccess;
@@ -644,19 +694,35 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
     }
     if (e != hipSuccess) return e;
   }
-  const int64_t n_kv = (int64_t)a.B * a.G * ((a.Sk + XQB - 1) / XQB);
+  const int64_t n_kv = (int64_t)a.B * a.G * ((a.Sk + XQB - 1) / XQB) * a.kv_splits;
   const int64_t n_red = a.dtable ? (int64_t)a.nb * a.H : 0;
   if (n_kv + n_red == 0) return e;
-  const size_t lds = 4 * x_qb<T>() * XT<T>::ROWB + 4 * x_qb<T>() * 4 + dist_bytes(a);
+  const size_t lds = kv_lds<T>() + dist_bytes(a);
   const dim3 grid((unsigned)(n_kv + n_red));
   if (a.table)
     hipLaunchKernelGGL((xattn_dkdv_kernel<T, true>), grid, dim3(256), lds, st, a, (int)n_kv);
   else
     hipLaunchKernelGGL((xattn_dkdv_kernel<T, false>), grid, dim3(256), lds, st, a, (int)n_kv);
-  return hipGetLastError();
+  if ((e = hipGetLastError()) != hipSuccess || a.kv_splits == 1) return e;
+  return launch(xattn_kv_sum_kernel<T>, ((int64_t)a.B * a.G * a.Sk + 7) / 8, 0, st, a);
 }
 
 }  // namespace
+
+XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_dtype dt) {
+  const int rows = dt == STAGE_BF16 ? x_qb<bf16_t>() : x_qb<float>();
+  const int64_t its = (int64_t)((Sq + rows - 1) / rows) * rep;
+  const int64_t wgs = (int64_t)B * G * ((Sk + XQB - 1) / XQB);
+  const int64_t slots = 2 * device_cus();
+  // The sum of the splits is a launch and a pass over them (5 us and more), a block of
+  // queries 3 us: 1 x 4 key heads of 4 x 2500 queries and 2500 keys 369 us in one piece
+  // (80 work-groups), 96 + 8 in chunks; 8 x 12 heads of 128 (two blocks, fp32) 29 and
+  // 22 + 5.
+  if (wgs * 2 > slots || wgs == 0 || its < 4) return {rows, (int)std::max<int64_t>(its, 1), 1};
+  const int64_t all = wgs * its / (causal ? 2 : 1);
+  const int64_t chunk = std::max<int64_t>((all + slots - 1) / slots, 1);
+  return {rows, (int)chunk, (int)((its + chunk - 1) / chunk)};
+}
 
 hipError_t xattn_forward(const XAttnArgs& a, stage_dtype dt, hipStream_t st) {
   return dt == STAGE_BF16 ? forward_t<bf16_t>(a, st) : forward_t<float>(a, st);
