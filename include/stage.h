@@ -184,6 +184,45 @@ stage_status stage_backward(stage_t* s, const void* dy, void* dx);
 stage_status stage_backward_noalloc(stage_t* s, const void* dy, void* dx);
 
 /*
+ * Relative position bias of the stage's self attention (attn.h: buckets of the
+ * distance key - query in both directions): the scores of every attention half get
+ * table[bucket][head], one fp32 table [num_buckets, heads] for all layers of the
+ * stage, 0 at first.  num_buckets = 0 takes the bias out again; otherwise
+ * num_buckets and max_distance are those of attn_relpos_init.  Synchronises the
+ * stream, drops the saved context and any earlier table; the next stage_forward
+ * allocates anew.  stage_backward also overwrites the table's gradient, the sum over
+ * the stage's layers (a model that shares one table over several stages sums theirs).
+ * A sequence without a valid key attends to nothing, as without the bias.  The
+ * table, its gradient and the operators' workspace are held besides what
+ * stage_memory_model counts.  EINVAL for buckets attn_relpos_init rejects or a stage
+ * without an attention half.
+ */
+stage_status stage_set_relpos(stage_t* s, int num_buckets, int max_distance);
+/* Device pointers (fp32) of the table and of its gradient, and their element count;
+ * valid until the next stage_set_relpos or stage_destroy.  ESTATE without a bias. */
+stage_status stage_relpos(stage_t* s, float** table, float** grad, int64_t* numel);
+
+/*
+ * Cross attention (the decoder layers of an encoder-decoder model), on a stage that
+ * holds one attention half and no bias: queries from x [batch, seq, h], keys and
+ * values from memory [batch, mem_seq, h] (an encoder's output), with the half's
+ * parameters, W_qkv's row blocks applied to x, memory and memory:
+ *     y = LN(x + W_o attention(x W_q^T + b_q, memory W_k^T + b_k, memory W_v^T + b_v) + b_o)
+ * key_mask: uint8 [batch, mem_seq] or NULL.  x, memory and the mask are copied into
+ * the saved context; y may not be one of them.  Lengths of 0 are valid (a query
+ * without a key attends to nothing).  stage_backward_cross takes the gradient of y
+ * and writes those of x and of memory (dmemory: 16-byte aligned) and the half's
+ * parameter gradients; it consumes the context.  EINVAL, ESTATE and ENOMEM as
+ * stage_forward and stage_backward; a context of one kind is not taken by the other
+ * kind's backward (ESTATE).  STAGE_SAVED_QKV of such a context is Q alone, [T, h].
+ * The memory's copy, keys and values with their gradient are held besides what
+ * stage_memory_model counts.
+ */
+stage_status stage_forward_cross(stage_t* s, const void* x, const void* memory,
+                                 const uint8_t* key_mask, int batch, int seq, int mem_seq, void* y);
+stage_status stage_backward_cross(stage_t* s, const void* dy, void* dx, void* dmemory);
+
+/*
  * Device memory.  stage_device_bytes: bytes the library holds for s
  * (parameters, gradients, the saved-activation record and the workspace, as
  * requested from hipMalloc).  stage_memory_model: the same figure predicted

@@ -35,7 +35,8 @@ EXPORTED = ("alloc_coarse", "alloc_fine", "alloc_workloads", "stage_init", "stag
             "stage_trace_site", "stage_trace_mask", "stage_trace_read", "stage_site_count",
             "stage_site_name", "stage_device_bytes", "stage_memory_model",
             "stage_memory_model_units", "stage_mfma_peak", "stage_record_grads",
-            "stage_backward_noalloc",
+            "stage_backward_noalloc", "stage_set_relpos", "stage_relpos", "stage_forward_cross",
+            "stage_backward_cross",
             "stage_last_error", "stage_destroy")
 
 EXPORTED_ATTN = ("attn_relpos_init", "attn_relpos_bucket", "attn_workspace", "attn_forward",
@@ -130,6 +131,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.stage_mfma_peak.restype = i32
     lib.stage_record_grads.argtypes = [vp, i32]
     lib.stage_record_grads.restype = i32
+    lib.stage_set_relpos.argtypes = [vp, i32, i32]
+    lib.stage_set_relpos.restype = i32
+    lib.stage_relpos.argtypes = [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(i64)]
+    lib.stage_relpos.restype = i32
+    lib.stage_forward_cross.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp]
+    lib.stage_forward_cross.restype = i32
+    lib.stage_backward_cross.argtypes = [vp, vp, vp, vp]
+    lib.stage_backward_cross.restype = i32
     dp, ip = ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)
     lib.alloc_coarse.argtypes = [i32, i32, dp, dp, ip, ip]
     lib.alloc_coarse.restype = i32
@@ -213,6 +222,27 @@ def stage_backward(handle, dy, dx) -> None:
 
 def stage_backward_noalloc(handle, dy, dx) -> None:
     _check(handle, load_library().stage_backward_noalloc(handle, _ptr(dy), _ptr(dx)))
+
+
+def stage_set_relpos(handle, num_buckets: int, max_distance: int) -> None:
+    _check(handle, load_library().stage_set_relpos(handle, num_buckets, max_distance))
+
+
+def stage_relpos(handle):
+    """(table pointer, gradient pointer, elements) of the relative position bias."""
+    t, g, n = ctypes.c_void_p(), ctypes.c_void_p(), ctypes.c_int64()
+    _check(handle, load_library().stage_relpos(handle, ctypes.byref(t), ctypes.byref(g),
+                                               ctypes.byref(n)))
+    return t.value, g.value, n.value
+
+
+def stage_forward_cross(handle, x, memory, key_mask, batch: int, seq: int, mem_seq: int, y) -> None:
+    _check(handle, load_library().stage_forward_cross(handle, _ptr(x), _ptr(memory), _ptr(key_mask),
+                                                      batch, seq, mem_seq, _ptr(y)))
+
+
+def stage_backward_cross(handle, dy, dx, dmemory) -> None:
+    _check(handle, load_library().stage_backward_cross(handle, _ptr(dy), _ptr(dx), _ptr(dmemory)))
 
 
 def stage_param(handle, layer: int, which: int):
@@ -314,6 +344,15 @@ def stage_destroy(handle) -> None:
 # Convenience wrapper
 # ---------------------------------------------------------------------------
 
+class _DeviceFloats:
+    """fp32 memory of a stage for torch.as_tensor; the tensor keeps the stage alive."""
+
+    def __init__(self, stage, ptr, shape):
+        self.stage = stage
+        self.__cuda_array_interface__ = {"data": (ptr, False), "shape": shape, "typestr": "<f4",
+                                         "strides": None, "version": 2}
+
+
 class Stage:
     """One stage of L encoder layers on the current GPU, or, with
     first_unit / n_units, of the half-layer units [first_unit, first_unit +
@@ -367,6 +406,56 @@ class Stage:
         self._sync_stream()
         stage_backward_noalloc(self.handle, dy, out)
         return out
+
+    def set_relpos(self, num_buckets: int, max_distance: int = 128):
+        """Give the self attention of the stage's layers one relative position bias
+        (both directions; a table of zeros), or take it out (num_buckets 0)."""
+        self._sync_stream()
+        stage_set_relpos(self.handle, num_buckets, max_distance)
+
+    def _relpos_view(self, which: int):
+        import torch
+        t, g, n = stage_relpos(self.handle)
+        return torch.as_tensor(_DeviceFloats(self, (t, g)[which], (n // self.heads, self.heads)),
+                               device="cuda")
+
+    def relpos_table(self):
+        """The bias table [num_buckets, heads], fp32, in the stage's own memory (to read
+        and to update in place, until the next set_relpos)."""
+        return self._relpos_view(0)
+
+    def relpos_grad(self):
+        """Its gradient of the latest backward, in the stage's own memory."""
+        return self._relpos_view(1)
+
+    def forward_cross(self, x, memory, key_mask=None, out=None):
+        """Cross attention of x [batch, seq, hidden] over memory [batch, mem_seq,
+        hidden] (a stage of one attention half)."""
+        import torch
+        B, S, h = x.shape
+        assert h == self.hidden and x.dtype == self.torch_dtype and x.is_cuda and x.is_contiguous()
+        assert memory.dim() == 3 and memory.shape[0] == B and memory.shape[2] == h
+        assert memory.dtype == x.dtype and memory.device == x.device and memory.is_contiguous()
+        M = memory.shape[1]
+        if key_mask is not None:
+            assert key_mask.dtype == torch.uint8 and key_mask.shape == (B, M) and key_mask.is_contiguous()
+        y = torch.empty_like(x) if out is None else out
+        self._sync_stream()
+        stage_forward_cross(self.handle, x, memory, key_mask, B, S, M, y)
+        self._mem_shape = memory.shape
+        return y
+
+    def backward_cross(self, dy, out=None, out_memory=None):
+        """(dx, dmemory) of the latest forward_cross."""
+        import torch
+        assert dy.dtype == self.torch_dtype and dy.is_cuda and dy.is_contiguous()
+        dx = torch.empty_like(dy) if out is None else out
+        shape = getattr(self, "_mem_shape", (0, 0, self.hidden))
+        dmem = torch.empty(shape, dtype=dy.dtype, device=dy.device) if out_memory is None else out_memory
+        assert dmem.shape == shape and dmem.dtype == dy.dtype and dmem.is_contiguous()
+        self._sync_stream()
+        stage_backward_cross(self.handle, dy, dx, dmem)
+        return dx, dmem
 
     def _param_shape(self, which: int):
         h, f = self.hidden, self.ffn

@@ -663,6 +663,7 @@ template hipError_t add_ln_fwd<bf16_t, float>(const float*, int, const float*, c
                                               const bf16_t*, const float*, const float*, bf16_t*,
                                               bf16_t*, bf16_t*, float*, int, int, hipStream_t);
 template hipError_t col_partial<float>(const float*, int, int, float*, int, hipStream_t);
+template hipError_t col_partial<bf16_t>(const bf16_t*, int, int, float*, int, hipStream_t);
 template hipError_t softmax_fwd<float>(const float*, const uint8_t*, float*, int, int, int, int,
                                        float, hipStream_t);
 template hipError_t softmax_bwd<float>(const float*, const float*, float*, int, int, int, float,

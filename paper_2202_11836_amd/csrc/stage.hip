@@ -15,6 +15,7 @@
 #include <type_traits>
 #include <vector>
 
+#include "../../include/attn.h"
 #include "../../include/stage.h"
 #include "kernels.h"
 
@@ -78,6 +79,15 @@ __global__ void init_normal_kernel(T* out, int64_t n, uint64_t key, double stdv)
   double u2 = (double)(b >> 11) * (1.0 / 9007199254740992.0);          // [0, 1)
   double z = sqrt(-2.0 * log(u1)) * cos(6.283185307179586 * u2);
   st_f(out + i, (float)(z * stdv));
+}
+
+// out[i] = the sum over rows r < n of rows[r * numel + i], in order.
+__global__ void sum_rows_kernel(const float* rows, int n, int64_t numel, float* out) {
+  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= numel) return;
+  float t = 0.0f;
+  for (int r = 0; r < n; ++r) t += rows[r * numel + i];
+  out[i] = t;
 }
 
 __global__ void fill_kernel(float* out, int64_t n, float v) {
@@ -177,6 +187,23 @@ struct stage {
   bool record_grads = false;
   bool rec_valid = false;
   std::vector<float*> rec;
+
+  // Relative position bias of the attention halves (stage_set_relpos): its buckets,
+  // one table [num_buckets, H] and its gradient for all layers.
+  bool relpos = false;
+  attn_relpos rp = {};
+  float* rp_table = nullptr;
+  float* rp_grad = nullptr;
+  // Workspace of the attention operators (with a bias also the layers' table
+  // gradients) and, of a cross-attention pass, what belongs to the memory: its copy
+  // [Tm, h], K | V and their gradient [Tm, 2h], its mask and column partial sums.
+  float* attn_ws = nullptr;
+  size_t attn_ws_elems = 0, attn_ws_bytes = 0;
+  float* cross_buf = nullptr;
+  size_t cross_elems = 0, cross_bytes = 0;
+  bool masked = false;  // the latest forward had a key mask
+  bool cross = false;   // it was stage_forward_cross, over M positions
+  int M = 0;
 
   int device = 0;          // device current at stage_init
   bool no_alloc = false;   // inside stage_backward_noalloc: no event creation
@@ -307,9 +334,9 @@ void free_activations(stage_t* s) {
   s->rec.clear();
   s->rec_valid = false;
   s->bytes_act = 0;
-  s->splitk = s->scores = nullptr;
-  s->splitk_elems = s->scores_elems = 0;
-  s->splitk_bytes = s->scores_bytes = 0;
+  s->splitk = s->scores = s->attn_ws = s->cross_buf = nullptr;
+  s->splitk_elems = s->scores_elems = s->attn_ws_elems = s->cross_elems = 0;
+  s->splitk_bytes = s->scores_bytes = s->attn_ws_bytes = s->cross_bytes = 0;
   s->cap_T = s->cap_BSS = s->cap_B = s->cap_NQB = -1;
   s->have_ctx = false;
 }
@@ -404,7 +431,7 @@ stage_status ensure_activations(stage_t* s, int B, int S) {
   // Probabilities (and their gradient) are stored only on fp32 stages, scores
   // only where their rows do not stay on chip.
   const int64_t BSS = s->dtype == STAGE_F32 ? (int64_t)B * s->H * S * S : 0;
-  const size_t n_scores = S > ATTN_F32_MAX_S ? (size_t)BSS : 0;
+  const size_t n_scores = S > ATTN_F32_MAX_S && !s->relpos ? (size_t)BSS : 0;
   const int64_t BHS = (int64_t)B * s->H * S;
   const int64_t NQB = (int64_t)B * ((S + 31) / 32);
   const size_t need = splitk_need(s, T);
@@ -517,8 +544,7 @@ struct WgradJob {
 // the rounding of its dx: one launch that writes whole gradients, or a
 // stream-K launch over all their tiles (fp32 partials side by side in the
 // split-K buffer) and one of fixed-order reductions.
-stage_status wgrad_group(stage_t* s, const WgradJob* jobs, int n, const TailJobs& tail) {
-  const int Tn = s->B * s->S;
+stage_status wgrad_group(stage_t* s, const WgradJob* jobs, int n, const TailJobs& tail, int Tn) {
   GemmArgs gs[GEMM_GROUP_MAX];
   float* outs[GEMM_GROUP_MAX];
   int Ms[GEMM_GROUP_MAX], Ns[GEMM_GROUP_MAX];
@@ -549,8 +575,7 @@ stage_status wgrad_group(stage_t* s, const WgradJob* jobs, int n, const TailJobs
 
 // The same on fp32 stages.  Traced as the gradients and reductions it holds.
 stage_status wgrad_group_f32(stage_t* s, const WgradJob* jobs, int n, const TailJobs& tail, bool attn,
-                             bool ffn) {
-  const int Tn = s->B * s->S;
+                             bool ffn, int Tn) {
   GemmArgs gs[GEMM_GROUP_MAX];
   float* outs[GEMM_GROUP_MAX];
   const F32WgradPlan plan = gemm_f32_wgrad_plan(s->h, s->f, Tn);
@@ -600,6 +625,131 @@ AttnF32Args attn_f32_args(stage_t* s, const float* qkv, void* P, float* out, int
   a.h = s->h;
   a.scale = 1.0f / sqrtf((float)HEAD_DIM);
   return a;
+}
+
+// ---------------------------------------------------------------------------
+// The attention operators (attn.h) on a stage's tensors: self attention with the
+// relative position bias, from a packed QKV [T, 3h], and cross attention, from Q
+// [T, h] and the memory's K | V [Tm, 2h].
+// ---------------------------------------------------------------------------
+attn_shape attn_op_shape(const stage_t* s) {
+  attn_shape a{};
+  const int64_t h = s->h, S = s->S, M = s->cross ? s->M : S;
+  a.dtype = s->dtype;
+  a.batch = s->B;
+  a.seq_q = s->S;
+  a.seq_k = (int)M;
+  a.heads = a.kv_heads = s->H;
+  a.scale = 1.0f / sqrtf((float)HEAD_DIM);
+  auto set = [](int64_t* st, int64_t n, int64_t ld) {
+    st[0] = n * ld;
+    st[1] = ld;
+    st[2] = HEAD_DIM;
+  };
+  const int64_t ldq = s->cross ? h : 3 * h, ldk = s->cross ? 2 * h : 3 * h;
+  set(a.q, S, ldq);
+  set(a.dq, S, ldq);
+  for (int64_t* st : {a.k, a.v, a.dk, a.dv}) set(st, M, ldk);
+  set(a.out, S, h);
+  set(a.dout, S, h);
+  return a;
+}
+
+// Room for the workspaces of both passes, and with a bias for the layers' table
+// gradients behind it.
+stage_status ensure_attn_ws(stage_t* s, size_t* table_at) {
+  const attn_shape a = attn_op_shape(s);
+  const attn_relpos* rp = s->relpos ? &s->rp : nullptr;
+  size_t f = 0, b = 0;
+  stage_status st;
+  if ((st = attn_workspace(&a, rp, 0, &f)) || (st = attn_workspace(&a, rp, 1, &b)))
+    return fail(s, st, attn_last_error());
+  const size_t at = (std::max(f, b) + 255) / 256 * 64;  // floats
+  if (table_at) *table_at = at;
+  const size_t need = at + (rp ? (size_t)s->L * rp->num_buckets * s->H : 0);
+  return need > s->attn_ws_elems ? grow(s, &s->attn_ws, &s->attn_ws_elems, &s->attn_ws_bytes, need)
+                                 : STAGE_OK;
+}
+
+// The memory's part of a cross-attention pass in cross_buf.
+struct CrossBuf {
+  char *mem, *kv, *dkv;
+  uint8_t* mask;
+  float* part;
+  size_t elems;  // floats in all
+};
+CrossBuf cross_layout(const stage_t* s, int64_t Tm) {
+  CrossBuf c{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char* p = (char*)s->cross_buf + off;
+    off += (bytes + 255) / 256 * 256;
+    return p;
+  };
+  c.mem = take(Tm * s->h * s->esz);
+  c.kv = take(Tm * 2 * s->h * s->esz);
+  c.dkv = take(Tm * 2 * s->h * s->esz);
+  c.mask = (uint8_t*)take(Tm);
+  c.part = (float*)take((size_t)COL_PARTS * 3 * s->h * 4);
+  c.elems = off / 4;
+  return c;
+}
+
+stage_status attn_op_forward(stage_t* s, const void* q, const void* k, const void* v,
+                             const uint8_t* mask, const Saved& sv) {
+  const attn_shape a = attn_op_shape(s);
+  const int tr = trace_begin(s, site_set(SITE_ATTN_FWD));
+  const stage_status st =
+      attn_forward(&a, s->relpos ? &s->rp : nullptr, s->relpos ? s->rp_table : nullptr, q, k, v,
+                   s->masked ? mask : nullptr, nullptr, sv.C, sv.lse, s->attn_ws,
+                   s->attn_ws_elems * 4, s->stream);
+  trace_end(s, tr);
+  return st ? fail(s, st, attn_last_error()) : STAGE_OK;
+}
+stage_status attn_op_backward(stage_t* s, const void* q, const void* k, const void* v,
+                              const uint8_t* mask, const Saved& sv, void* dq, void* dk, void* dv,
+                              float* dtable, size_t ws_bytes) {
+  const attn_shape a = attn_op_shape(s);
+  const int tr = trace_begin(s, site_set(SITE_ATTN_BWD, SITE_ATTN_DQ, SITE_ATTN_DKDV));
+  const stage_status st =
+      attn_backward(&a, s->relpos ? &s->rp : nullptr, s->relpos ? s->rp_table : nullptr, q, k, v,
+                    s->masked ? mask : nullptr, nullptr, sv.C, sv.lse, s->dC, dq, dk, dv, dtable,
+                    s->attn_ws, ws_bytes, s->stream);
+  trace_end(s, tr);
+  return st ? fail(s, st, attn_last_error()) : STAGE_OK;
+}
+
+// Self attention's backward with the bias: dQKV, its column sums (*cj) and the
+// layer's table gradient.
+template <typename T>
+stage_status attn_relpos_backward(stage_t* s, int l, float* db, ColJob* cj) {
+  const int h = s->h, Tn = s->B * s->S;
+  const Saved& v = s->saved[l];
+  const T* qkv = (const T*)v.QKV;
+  T* d = (T*)s->dQKV;
+  size_t at = 0;
+  stage_status st = ensure_attn_ws(s, &at);
+  if (!st)
+    st = attn_op_backward(s, qkv, qkv + h, qkv + 2 * h, s->mask, v, d, d + h, d + 2 * h,
+                          s->attn_ws + at + (size_t)l * s->rp.num_buckets * s->H, at * 4);
+  if (st) return st;
+  const int nblk = std::min(COL_PARTS, s->B * ((s->S + 31) / 32));
+  SITE(BQKV_SUM, col_partial<T>(d, Tn, 3 * h, s->colpart_qkv, nblk, s->stream));
+  *cj = ColJob{s->colpart_qkv, nblk, 1, 3 * h, {db, nullptr, nullptr, nullptr}};
+  return STAGE_OK;
+}
+// The table's gradient from those of the layers (those with an attention half are all
+// but the first layer of a stage that starts at a feed-forward half).
+stage_status relpos_grad_sum(stage_t* s) {
+  size_t at = 0;
+  stage_status st = ensure_attn_ws(s, &at);
+  if (st) return st;
+  const int64_t n = (int64_t)s->rp.num_buckets * s->H;
+  const int first = s->ffn_first ? 1 : 0;
+  hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s->stream,
+                     s->attn_ws + at + first * n, s->L - first, n, s->rp_grad);
+  HIPCK(hipGetLastError());
+  return STAGE_OK;
 }
 
 // Whether kernels may read n bytes at p in place: device memory of this device,
@@ -678,7 +828,10 @@ stage_status forward_impl(stage_t* s, const T* x, const uint8_t* key_mask, T* y)
         g.bias = (const float*)p[STAGE_B_QKV];
         SITE_SET(SITE_QKV_FWD, l == 0 ? prep_site : 0, gemm_in(g, EPI_STORE, l == 0));
       }
-      if constexpr (std::is_same<T, bf16_t>::value) {
+      if (s->relpos) {
+        const stage_status r = attn_op_forward(s, QKV, QKV + h, QKV + 2 * h, s->mask, v);
+        if (r) return r;
+      } else if constexpr (std::is_same<T, bf16_t>::value) {
         // Fused attention: softmax(Q K^T / 8) V per (batch, head), P stays on chip.
         AttnArgs aa = attn_args(s, (const bf16_t*)QKV, (bf16_t*)v.C, v.lse);
         aa.out_lo = (bf16_t*)v.Clo;
@@ -840,7 +993,9 @@ stage_status backward_f32(stage_t* s, const float* dy, float* dx) {
         SITE(OUT_DGRAD, gemm_f32(g, true, false, EPI_STORE, 1, st));
       }
       const bool rows = S <= ATTN_F32_MAX_S;
-      if (rows) {
+      if (s->relpos) {
+        if ((r = attn_relpos_backward<T>(s, l, gr[STAGE_B_QKV], &tail.col[tail.ncol++]))) return r;
+      } else if (rows) {
         // dS, dQ and its column sums
         AttnF32Args aa = attn_f32_args(s, QKV, v.P, dQKV, 3 * h);
         aa.dC = dC;
@@ -867,7 +1022,7 @@ stage_status backward_f32(stage_t* s, const float* dy, float* dx) {
       // dV_bj = P_bj^T dC_bj, dK_bj = dS_bj^T Q_bj (and dQ_bj = dS_bj K_bj), and
       // their column sums per 32 rows of each sequence (db_qkv)
       const int nqb = (S + 31) / 32;
-      {
+      if (!s->relpos) {
         auto prob = [&](const void* a, const T* b, int64_t ldb, int64_t sb1, int block) {
           GemmArgs g = gemm_args(a, S, b, ldb, dQKV + (int64_t)block * h, 3 * h, S, HEAD_DIM, S);
           g.zdiv = H;
@@ -887,9 +1042,9 @@ stage_status backward_f32(stage_t* s, const float* dy, float* dx) {
         SITE_SET(SITE_DV_BWD, site_set(SITE_DK_BWD, SITE_BQKV_SUM, rows ? SITE_DV_BWD : SITE_DQ_BWD),
                  gemm_f32_attn_bwd(prob(v.P, dC, h, (int64_t)S * h, 2),
                                    prob(s->dS, QKV, 3 * h, sq, 1), rows ? nullptr : &dq, BH, st));
+        tail.col[tail.ncol++] = ColJob{s->colpart_qkv, B * nqb, 1, 3 * h,
+                             {gr[STAGE_B_QKV], nullptr, nullptr, nullptr}};
       }
-      tail.col[tail.ncol++] = ColJob{s->colpart_qkv, B * nqb, 1, 3 * h,
-                           {gr[STAGE_B_QKV], nullptr, nullptr, nullptr}};
       // dW_qkv = dQKV^T X
       wjobs[nw++] = {dQKV, 3 * h, v.X, h, 3 * h, h, gr[STAGE_W_QKV]};
       // dX = dZ1 + dQKV W_qkv  (the previous layer's dY, or the stage's dx)
@@ -902,9 +1057,9 @@ stage_status backward_f32(stage_t* s, const float* dy, float* dx) {
       }
       dYcur = dXout;
     }
-    if ((r = wgrad_group_f32(s, wjobs, nw, tail, attn, ffn))) return r;
+    if ((r = wgrad_group_f32(s, wjobs, nw, tail, attn, ffn, Tn))) return r;
   }
-  return STAGE_OK;
+  return s->relpos ? relpos_grad_sum(s) : STAGE_OK;
 }
 
 // A data-gradient product dX = dY W (W as stored: n-major B operand) that
@@ -1013,23 +1168,27 @@ stage_status backward_bf16(stage_t* s, const bf16_t* dy, bf16_t* dx) {
       g.ldaux = h;
       g.dsum = s->dsum;
       g.dsum_S = S;
-      const bool dsum = g.tile != GEMM_TILE_256x256;
+      const bool dsum = g.tile != GEMM_TILE_256x256 && !s->relpos;
       SITE(OUT_DGRAD, gemm_bf16(g, false, dsum ? EPI_DSUM : EPI_STORE, st));
       // Attention backward (recomputes P from the saved log-sum-exp): dQKV
       // and the column sums of db_qkv per 32-row block.
-      AttnArgs aa = attn_args(s, (const T*)v.QKV, dQKV, v.lse);
-      aa.o = (const T*)v.C;
-      aa.o_lo = (const T*)v.Clo;
-      aa.dout = dC;
-      aa.colpart = s->colpart_qkv;
-      if (dsum) {
-        SITE_SET(SITE_ATTN_BWD, site_set(SITE_ATTN_DQ, SITE_ATTN_DKDV), attn_backward(aa, st));
+      if (s->relpos) {
+        if ((r = attn_relpos_backward<T>(s, l, gr[STAGE_B_QKV], &tail.col[tail.ncol++]))) return r;
       } else {
-        SITE(ATTN_DQ, attn_backward_dq(aa, st));
-        SITE(ATTN_DKDV, attn_backward_dkdv(aa, st));
+        AttnArgs aa = attn_args(s, (const T*)v.QKV, dQKV, v.lse);
+        aa.o = (const T*)v.C;
+        aa.o_lo = (const T*)v.Clo;
+        aa.dout = dC;
+        aa.colpart = s->colpart_qkv;
+        if (dsum) {
+          SITE_SET(SITE_ATTN_BWD, site_set(SITE_ATTN_DQ, SITE_ATTN_DKDV), attn_backward(aa, st));
+        } else {
+          SITE(ATTN_DQ, attn_backward_dq(aa, st));
+          SITE(ATTN_DKDV, attn_backward_dkdv(aa, st));
+        }
+        tail.col[tail.ncol++] = ColJob{s->colpart_qkv, B * ((S + 31) / 32), 1, 3 * h,
+                             {gr[STAGE_B_QKV], nullptr, nullptr, nullptr}};
       }
-      tail.col[tail.ncol++] = ColJob{s->colpart_qkv, B * ((S + 31) / 32), 1, 3 * h,
-                           {gr[STAGE_B_QKV], nullptr, nullptr, nullptr}};
       // dW_qkv = dQKV^T X
       wjobs[nw++] = {dQKV, 3 * h, v.X, h, 3 * h, h, gr[STAGE_W_QKV]};
       // dX = dZ1 + dQKV W_qkv: summed in the previous layer's second
@@ -1044,9 +1203,158 @@ stage_status backward_bf16(stage_t* s, const bf16_t* dy, bf16_t* dx) {
         tail.gn = n;
       }
     }
-    if ((r = wgrad_group(s, wjobs, nw, tail))) return r;
+    if ((r = wgrad_group(s, wjobs, nw, tail, Tn))) return r;
   }
+  return s->relpos ? relpos_grad_sum(s) : STAGE_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Cross attention: an attention half whose keys and values come from a memory of
+// another length: Q = X W_q^T + b_q, K | V = memory W_kv^T + b_kv (the row blocks of
+// W_qkv), then as in self attention.
+// ---------------------------------------------------------------------------
+// Split-K elements of its two groups of weight gradients, over T and over Tm tokens.
+size_t cross_splitk_need(const stage_t* s, int64_t T, int64_t Tm) {
+  const int h = s->h, one[2] = {h, h}, two = 2 * h;
+  const int Tq = (int)std::max<int64_t>(T, 1), Tk = (int)std::max<int64_t>(Tm, 1);
+  const size_t hh = (size_t)h * h;
+  if (s->dtype == STAGE_BF16)
+    return std::max((size_t)wgrad_group_slots(one, one, 2, Tq), (size_t)wgrad_group_slots(&two, one, 1, Tk)) *
+           2 * hh;
+  const int ks = std::max(gemm_f32_wgrad_plan(h, s->f, Tq).ks, gemm_f32_wgrad_plan(h, s->f, Tk).ks);
+  return ks > 1 ? ks * 2 * hh : 0;
+}
+
+template <typename T>
+stage_status forward_cross_impl(stage_t* s, const T* x, const T* mem, const uint8_t* key_mask, T* y) {
+  const int B = s->B, S = s->S, M = s->M, h = s->h, Tn = B * S, Tm = B * M;
+  hipStream_t st = s->stream;
+  Saved& v = s->saved[0];
+  auto& p = s->param[0];
+  const CrossBuf c = cross_layout(s, Tm);
+  // Copies of x, the memory and its mask (s->mask, of the queries, is not used).
+  for (int i = 0; i < (Tm > 0 ? 2 : 1); ++i) {
+    const T* from = i ? mem : x;
+    PrepArgs a{from, i ? (void*)c.mem : v.X, (int64_t)(i ? Tm : Tn) * h * (int)sizeof(T),
+               i ? key_mask : nullptr, i ? c.mask : s->mask, B, i ? M : S, nullptr};
+    if (((uintptr_t)from & 15) != 0 || !reads_in_place(from, (size_t)a.nx, s->device)) {
+      HIPCK(hipMemcpyAsync(a.X, from, (size_t)a.nx, hipMemcpyDefault, st));
+      a.x = a.X;
+      a.nx = 0;
+    }
+    if (a.key_mask && !reads_in_place(a.key_mask, (size_t)Tm, s->device)) {
+      HIPCK(hipMemcpyAsync(a.mask, a.key_mask, (size_t)Tm, hipMemcpyDefault, st));
+      a.key_mask = a.mask;
+    }
+    SITE(KEXT, stage_prep(a, st));
+  }
+  const T* W = (const T*)p[STAGE_W_QKV];
+  const float* bias = (const float*)p[STAGE_B_QKV];
+  T* Q = (T*)v.QKV;
+  T* KV = (T*)c.kv;
+  {
+    GemmArgs g = gemm_args(v.X, h, W, h, Q, h, Tn, h, h);
+    g.bias = bias;
+    SITE(QKV_FWD, gemm_fwd(g, EPI_STORE, (T*)nullptr, st));
+  }
+  if (Tm > 0) {
+    GemmArgs g = gemm_args(c.mem, h, W + (int64_t)h * h, h, KV, 2 * h, Tm, 2 * h, h);
+    g.bias = bias + h;
+    SITE(QKV_FWD, gemm_fwd(g, EPI_STORE, (T*)nullptr, st));
+  }
+  const stage_status r = attn_op_forward(s, Q, KV, KV + h, c.mask, v);
+  if (r) return r;
+  int np = 1;
+  {
+    GemmArgs g = gemm_args(v.C, h, p[STAGE_W_O], h, s->tmp, h, Tn, h, h);
+    SITE(OUT_FWD, gemm_fwd_ln(g, &np, (T*)nullptr, st));
+  }
+  SITE(LN1_FWD, add_ln_fwd<T, float>(s->tmp, np, (const float*)p[STAGE_B_O], (const T*)v.X, nullptr,
+                                     (const float*)p[STAGE_G1], (const float*)p[STAGE_BE1], y, nullptr,
+                                     (T*)v.xhat1, v.rstd1, Tn, h, st));
   return STAGE_OK;
+}
+
+template <typename T>
+stage_status backward_cross_impl(stage_t* s, const T* dy, T* dx, T* dmem) {
+  constexpr bool BF = std::is_same<T, bf16_t>::value;
+  const int B = s->B, S = s->S, h = s->h, Tn = B * S, Tm = B * s->M;
+  hipStream_t st = s->stream;
+  Saved& v = s->saved[0];
+  auto& p = s->param[0];
+  auto& gr = s->grad[0];
+  const CrossBuf c = cross_layout(s, Tm);
+  T *dZ1 = (T*)s->dZ1, *dC = (T*)s->dC, *dQ = (T*)s->dQKV, *dKV = (T*)c.dkv;
+  const T* W = (const T*)p[STAGE_W_QKV];
+  const T* Wkv = W + (int64_t)h * h;
+  TailJobs tail{};
+  stage_status r;
+  // y = LN(Z1): dZ1, dgamma1, dbeta1, db_o;  dC = dZ1 W_o
+  if constexpr (BF) {
+    const GradIn gin{dy, nullptr, nullptr, nullptr, nullptr, 0};
+    if (recording(s)) HIPCK(grad_f32(gin, s->rec[0], (int64_t)Tn * h, st));
+    SITE(LN1_BWD, ln_bwd_bf16(gin, (const T*)v.xhat1, v.rstd1, (const float*)p[STAGE_G1], dZ1,
+                              (T*)s->dz1lo, s->part, Tn, h, st));
+  } else {
+    if (recording(s))
+      HIPCK(hipMemcpyAsync(s->rec[0], dy, (size_t)Tn * h * 4, hipMemcpyDeviceToDevice, st));
+    SITE(LN1_BWD, ln_bwd_f32(dy, (const T*)v.xhat1, v.rstd1, (const float*)p[STAGE_G1], dZ1, s->part,
+                             Tn, h, st));
+  }
+  tail.col[tail.ncol++] = ColJob{s->part, ln_bwd_blocks(Tn), 3, h,
+                       {gr[STAGE_G1], gr[STAGE_BE1], gr[STAGE_B_O], nullptr}};
+  {
+    GemmArgs g = gemm_args(dZ1, h, p[STAGE_W_O], h, dC, h, Tn, h, h);
+    if constexpr (BF) SITE(OUT_DGRAD, gemm_bf16(g, false, EPI_STORE, st));
+    else SITE(OUT_DGRAD, gemm_f32(g, true, false, EPI_STORE, 1, st));
+  }
+  if ((r = attn_op_backward(s, v.QKV, c.kv, (const T*)c.kv + h, c.mask, v, dQ, dKV, dKV + h, nullptr,
+                            s->attn_ws_elems * 4)))
+    return r;
+  // Column sums of dQ and dK | dV
+  float* part_kv = c.part + (size_t)COL_PARTS * h;
+  SITE(BQKV_SUM, col_partial<T>(dQ, Tn, h, c.part, COL_PARTS, st));
+  tail.col[tail.ncol++] = ColJob{c.part, COL_PARTS, 1, h, {gr[STAGE_B_QKV], nullptr, nullptr, nullptr}};
+  if (Tm > 0) {
+    SITE(BQKV_SUM, col_partial<T>(dKV, Tm, 2 * h, part_kv, COL_PARTS, st));
+    tail.col[tail.ncol++] =
+        ColJob{part_kv, COL_PARTS, 1, 2 * h, {gr[STAGE_B_QKV] + h, nullptr, nullptr, nullptr}};
+    // dmemory = dK | dV W_kv
+    GemmArgs g = gemm_args(dKV, 2 * h, Wkv, h, dmem, h, Tm, h, 2 * h);
+    if constexpr (BF) SITE(QKV_DGRAD, gemm_bf16(g, false, EPI_STORE, st));
+    else SITE(QKV_DGRAD, gemm_f32(g, true, false, EPI_STORE, 1, st));
+  } else {
+    for (float* z : {gr[STAGE_B_QKV] + h, gr[STAGE_W_QKV] + (int64_t)h * h}) {
+      const int64_t n = z == gr[STAGE_B_QKV] + h ? 2 * h : 2 * (int64_t)h * h;
+      hipLaunchKernelGGL(fill_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, z, n, 0.0f);
+    }
+    HIPCK(hipGetLastError());
+  }
+  // dx = dZ1 + dQ W_q
+  if constexpr (BF) {
+    GradIn gin;
+    if ((r = dgrad_joining(s, SITE_QKV_DGRAD, gemm_args(dQ, h, W, h, nullptr, h, Tn, h, h), dZ1,
+                           (const T*)s->dz1lo, &gin)))
+      return r;
+    tail.gin = gin;
+    tail.gout = dx;
+    tail.gn = (int64_t)Tn * h;
+  } else {
+    GemmArgs g = gemm_args(dQ, h, W, h, dx, h, Tn, h, h);
+    g.aux = dZ1;
+    g.ldaux = h;
+    SITE(QKV_DGRAD, gemm_f32(g, true, false, EPI_RESID, 1, st));
+  }
+  // dW_kv = (dK | dV)^T memory, then dW_o = dZ1^T C and dW_q = dQ^T X with the tail
+  const WgradJob kv = {dKV, 2 * h, c.mem, h, 2 * h, h, gr[STAGE_W_QKV] + (int64_t)h * h};
+  const WgradJob q[2] = {{dZ1, h, v.C, h, h, h, gr[STAGE_W_O]}, {dQ, h, v.X, h, h, h, gr[STAGE_W_QKV]}};
+  if constexpr (BF) {
+    if (Tm > 0 && (r = wgrad_group(s, &kv, 1, TailJobs{}, Tm))) return r;
+    return wgrad_group(s, q, 2, tail, Tn);
+  } else {
+    if (Tm > 0 && (r = wgrad_group_f32(s, &kv, 1, TailJobs{}, true, false, Tm))) return r;
+    return wgrad_group_f32(s, q, 2, tail, true, false, Tn);
+  }
 }
 
 bool valid_dims(int hidden, int heads, int ffn, stage_dtype dtype) {
@@ -1111,6 +1419,20 @@ stage_status build_params(stage_t* s, uint64_t seed) {
   if (e == hipSuccess) e = hipStreamSynchronize(s->stream);
   if (e != hipSuccess)
     return fail(s, STAGE_EHIP, std::string("initialisation kernels: ") + hipGetErrorString(e));
+  return STAGE_OK;
+}
+
+// Zero gradients of everything the stage holds (an empty batch).
+stage_status zero_grads(stage_t* s) {
+  auto zero = [&](float* p, int64_t n) {
+    hipLaunchKernelGGL(fill_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s->stream, p, n,
+                       0.0f);
+  };
+  for (int l = 0; l < s->L; ++l)
+    for (int w = 0; w < STAGE_NPARAM; ++w)
+      if (has_param(s, l, w)) zero(s->grad[l][w], param_numel(s, w));
+  if (s->relpos) zero(s->rp_grad, (int64_t)s->rp.num_buckets * s->H);
+  HIPCK(hipGetLastError());
   return STAGE_OK;
 }
 
@@ -1230,12 +1552,15 @@ stage_status stage_forward(stage_t* s, const void* x, const uint8_t* key_mask, i
   if (st) return st;
   s->B = batch;
   s->S = seq;
+  s->cross = false;
+  s->masked = key_mask != nullptr;
   s->have_ctx = false;
   s->rec_valid = false;
   if (T == 0) {
     s->have_ctx = true;
     return STAGE_OK;
   }
+  if (s->relpos && (st = ensure_attn_ws(s, nullptr))) return st;
   st = s->dtype == STAGE_BF16 ? forward_impl<bf16_t>(s, (const bf16_t*)x, key_mask, (bf16_t*)y)
                               : forward_impl<float>(s, (const float*)x, key_mask, (float*)y);
   if (st) return st;
@@ -1246,21 +1571,12 @@ stage_status stage_forward(stage_t* s, const void* x, const uint8_t* key_mask, i
 stage_status stage_backward(stage_t* s, const void* dy, void* dx) {
   if (!s) return STAGE_EINVAL;
   s->err.clear();
-  if (!s->have_ctx) return fail(s, STAGE_ESTATE, "stage_backward needs a preceding stage_forward");
+  if (!s->have_ctx || s->cross)
+    return fail(s, STAGE_ESTATE, "stage_backward needs a preceding stage_forward");
   const int64_t T = (int64_t)s->B * s->S;
   if (T > 0 && (!dy || !dx)) return fail(s, STAGE_EINVAL, "null dy or dx");
   s->have_ctx = false;
-  if (T == 0) {
-    for (int l = 0; l < s->L; ++l)
-      for (int w = 0; w < STAGE_NPARAM; ++w) {
-        if (!has_param(s, l, w)) continue;
-        int64_t n = param_numel(s, w);
-        hipLaunchKernelGGL(fill_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0,
-                           s->stream, s->grad[l][w], n, 0.0f);
-      }
-    HIPCK(hipGetLastError());
-    return STAGE_OK;
-  }
+  if (T == 0) return zero_grads(s);
   stage_status st = s->dtype == STAGE_BF16 ? backward_bf16(s, (const bf16_t*)dy, (bf16_t*)dx)
                                            : backward_f32(s, (const float*)dy, (float*)dx);
   s->rec_valid = st == STAGE_OK && s->record_grads && (int)s->rec.size() == s->L;
@@ -1270,7 +1586,8 @@ stage_status stage_backward(stage_t* s, const void* dy, void* dx) {
 stage_status stage_backward_noalloc(stage_t* s, const void* dy, void* dx) {
   if (!s) return STAGE_EINVAL;
   s->err.clear();
-  if (!s->have_ctx) return fail(s, STAGE_ESTATE, "stage_backward needs a preceding stage_forward");
+  if (!s->have_ctx || s->cross)
+    return fail(s, STAGE_ESTATE, "stage_backward needs a preceding stage_forward");
   float* base = scratch_of(s->device);
   if (!base) return fail(s, STAGE_ESTATE, "static scratch not resolved for the stage's device");
   // The backward's partial buffers, laid out in the scratch (256-byte
@@ -1325,6 +1642,120 @@ stage_status stage_backward_noalloc(stage_t* s, const void* dy, void* dx) {
   return st;
 }
 
+stage_status stage_set_relpos(stage_t* s, int num_buckets, int max_distance) {
+  if (!s) return STAGE_EINVAL;
+  s->err.clear();
+  attn_relpos rp{};
+  if (num_buckets != 0) {
+    const stage_status st = attn_relpos_init(num_buckets, max_distance, 1, &rp);
+    if (st) return fail(s, st, attn_last_error());
+    if (s->L == 1 && s->ffn_first)
+      return fail(s, STAGE_EINVAL, "the stage holds no attention half");
+  }
+  HIPCK(hipStreamSynchronize(s->stream));
+  // (the earlier table, if any, goes with its bytes)
+  for (float** p : {&s->rp_table, &s->rp_grad}) {
+    if (!*p) continue;
+    s->allocs.erase(std::find(s->allocs.begin(), s->allocs.end(), (void*)*p));
+    s->bytes_param -= (int64_t)s->rp.num_buckets * s->H * 4;
+    (void)hipFree(*p);
+    *p = nullptr;
+  }
+  s->relpos = false;
+  s->have_ctx = false;
+  s->cap_T = -1;  // (fp32 stages past 512 tokens hold no score matrix with a bias)
+  if (num_buckets == 0) return STAGE_OK;
+  s->rp = rp;
+  const int64_t n = (int64_t)num_buckets * s->H;
+  for (float** p : {&s->rp_table, &s->rp_grad}) {
+    const stage_status st = dev_alloc(s, s->allocs, (void**)p, n * 4);
+    if (st) {
+      s->bytes_param -= n * 4;
+      return st;
+    }
+    hipLaunchKernelGGL(fill_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s->stream, *p, n,
+                       0.0f);
+  }
+  HIPCK(hipGetLastError());
+  s->relpos = true;
+  return STAGE_OK;
+}
+
+stage_status stage_relpos(stage_t* s, float** table, float** grad, int64_t* numel) {
+  if (!s) return STAGE_EINVAL;
+  if (!s->relpos) return fail(s, STAGE_ESTATE, "the stage has no relative position bias");
+  if (table) *table = s->rp_table;
+  if (grad) *grad = s->rp_grad;
+  if (numel) *numel = (int64_t)s->rp.num_buckets * s->H;
+  return STAGE_OK;
+}
+
+stage_status stage_forward_cross(stage_t* s, const void* x, const void* memory, const uint8_t* key_mask,
+                                 int batch, int seq, int mem_seq, void* y) {
+  if (!s) return STAGE_EINVAL;
+  s->err.clear();
+  if (s->L != 1 || s->ffn_first || !s->attn_last)
+    return fail(s, STAGE_EINVAL, "cross attention needs a stage of one attention half");
+  if (s->relpos) return fail(s, STAGE_EINVAL, "cross attention takes no relative position bias");
+  if (batch < 0 || seq < 0 || mem_seq < 0) return fail(s, STAGE_EINVAL, "negative batch or length");
+  const int64_t T = (int64_t)batch * seq, Tm = (int64_t)batch * mem_seq;
+  if (T > 0 && (!x || !y)) return fail(s, STAGE_EINVAL, "null x or y");
+  if (Tm > 0 && !memory) return fail(s, STAGE_EINVAL, "null memory");
+  if (T > 0 && (x == y || (Tm > 0 && memory == y)))
+    return fail(s, STAGE_EINVAL, "y may not be an input");
+  const int64_t lim = ((int64_t)1 << 31) / (s->dtype == STAGE_BF16 ? 2 : 1);
+  if (T * std::max(3 * s->h, s->f) >= lim || Tm * std::max(3 * s->h, s->f) >= lim)
+    return fail(s, STAGE_EINVAL, "batch * seq too large");
+  stage_status st = ensure_activations(s, batch, seq);
+  if (st) return st;
+  s->B = batch;
+  s->S = seq;
+  s->M = mem_seq;
+  s->cross = true;
+  s->masked = key_mask != nullptr;
+  s->have_ctx = false;
+  s->rec_valid = false;
+  if (T > 0) {
+    const size_t need = cross_splitk_need(s, T, Tm), cb = cross_layout(s, Tm).elems;
+    if (need > s->splitk_elems && (st = grow_splitk(s, need))) return st;
+    if (cb > s->cross_elems && (st = grow(s, &s->cross_buf, &s->cross_elems, &s->cross_bytes, cb)))
+      return st;
+    if ((st = ensure_attn_ws(s, nullptr))) return st;
+    st = s->dtype == STAGE_BF16
+             ? forward_cross_impl<bf16_t>(s, (const bf16_t*)x, (const bf16_t*)memory, key_mask, (bf16_t*)y)
+             : forward_cross_impl<float>(s, (const float*)x, (const float*)memory, key_mask, (float*)y);
+    if (st) return st;
+  }
+  s->have_ctx = true;
+  return STAGE_OK;
+}
+
+stage_status stage_backward_cross(stage_t* s, const void* dy, void* dx, void* dmemory) {
+  if (!s) return STAGE_EINVAL;
+  s->err.clear();
+  if (!s->have_ctx || !s->cross)
+    return fail(s, STAGE_ESTATE, "stage_backward_cross needs a preceding stage_forward_cross");
+  const int64_t T = (int64_t)s->B * s->S, Tm = (int64_t)s->B * s->M;
+  if (T > 0 && (!dy || !dx)) return fail(s, STAGE_EINVAL, "null dy or dx");
+  if (Tm > 0 && !dmemory) return fail(s, STAGE_EINVAL, "null dmemory");
+  if ((uintptr_t)dmemory % 16) return fail(s, STAGE_EINVAL, "dmemory is not 16-byte aligned");
+  s->have_ctx = false;
+  if (T == 0) {
+    if (Tm > 0) {
+      const int64_t n = Tm * s->h * (int64_t)s->esz / 4;
+      hipLaunchKernelGGL(fill_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s->stream,
+                         (float*)dmemory, n, 0.0f);
+    }
+    return zero_grads(s);
+  }
+  const stage_status st =
+      s->dtype == STAGE_BF16
+          ? backward_cross_impl<bf16_t>(s, (const bf16_t*)dy, (bf16_t*)dx, (bf16_t*)dmemory)
+          : backward_cross_impl<float>(s, (const float*)dy, (float*)dx, (float*)dmemory);
+  s->rec_valid = st == STAGE_OK && s->record_grads && (int)s->rec.size() == s->L;
+  return st;
+}
+
 stage_status stage_param(stage_t* s, int layer, int which, void** dev_ptr, int64_t* numel,
                          stage_dtype* dtype) {
   stage_status st = check_param(s, layer, which);
@@ -1364,7 +1795,8 @@ static void* saved_ptr(stage_t* s, int layer, int which, size_t* bytes) {
   *bytes = 0;
   switch (which) {
     case STAGE_SAVED_X: if (attn) *bytes = T * s->h * e; return attn ? v.X : nullptr;
-    case STAGE_SAVED_QKV: if (attn) *bytes = T * 3 * s->h * e; return attn ? v.QKV : nullptr;
+    // (of a cross-attention pass: Q alone)
+    case STAGE_SAVED_QKV: if (attn) *bytes = T * (s->cross ? 1 : 3) * s->h * e; return attn ? v.QKV : nullptr;
     case STAGE_SAVED_CTX: if (attn) *bytes = T * s->h * e; return attn ? v.C : nullptr;
     case STAGE_SAVED_H1: if (ffn) *bytes = T * s->h * e; return ffn ? v.H1 : nullptr;
     case STAGE_SAVED_GD: if (ffn) *bytes = T * s->f * e; return ffn ? v.Gd : nullptr;
