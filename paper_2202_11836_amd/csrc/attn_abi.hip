@@ -81,6 +81,7 @@ struct Workspace {
   int64_t dsum, tpart, part, total;  // bytes
   XKvPlan kv;
   XFewPlan few;
+  int dq_ks;
 };
 Workspace workspace_of(const attn_shape* s, const attn_relpos* rp, bool backward) {
   Workspace w{};
@@ -95,8 +96,11 @@ Workspace workspace_of(const attn_shape* s, const attn_relpos* rp, bool backward
     return w;
   }
   w.dsum = ((int64_t)s->batch * s->heads * s->seq_q * 4 + 15) / 16 * 16;
+  w.dq_ks = xattn_dq_split(s->batch, s->heads, s->seq_q, s->causal, rp != nullptr, s->dtype);
+  const int64_t qb = 128 / w.dq_ks;  // queries of a work-group
   if (rp)
-    w.tpart = ((int64_t)s->batch * s->heads * row_blocks(s->seq_q) * rp->num_buckets * 4 + 15) / 16 * 16;
+    w.tpart = ((int64_t)s->batch * s->heads * ((s->seq_q + qb - 1) / qb) * rp->num_buckets * 4 + 15) /
+              16 * 16;
   w.kv = xattn_kv_plan(s->batch, s->kv_heads, rep, s->seq_q, s->seq_k, s->causal, s->dtype);
   if (w.kv.splits > 1)
     w.part = (int64_t)w.kv.splits * s->batch * s->kv_heads * s->seq_k * 2 * XHD * 4;
@@ -118,8 +122,9 @@ stage_status check_shape(const attn_shape* s, const attn_relpos* rp) {
     return bad(STAGE_EINVAL, "scale must be finite and positive");
   if (rp && !relpos_ok(rp)) return bad(STAGE_EINVAL, "rp is not one that attn_relpos_init filled");
   // A launch holds fewer than 2^32 threads, 256 to a work-group.
+  // (the dQ kernel may take two for 128 queries)
   const double most = 16777215.0;
-  if ((double)s->batch * s->heads * (double)row_blocks(s->seq_q) > most ||
+  if (2.0 * s->batch * s->heads * (double)row_blocks(s->seq_q) > most ||
       (double)s->batch * s->kv_heads * (double)row_blocks(s->seq_k) +
               (rp ? (double)rp->num_buckets * s->heads : 0.0) > most)
     return bad(STAGE_EINVAL, "batch * heads * length too large");
@@ -342,6 +347,7 @@ stage_status attn_backward(const attn_shape* s, const attn_relpos* rp, const flo
   a.dsum = (float*)workspace;
   a.tpart = (float*)((char*)workspace + w.dsum);
   a.part = (float*)((char*)workspace + w.dsum + w.tpart);
+  a.dq_ks = w.dq_ks;
   a.kv_chunk = w.kv.chunk;
   a.kv_splits = w.kv.splits;
   const hipError_t e = xattn_backward(a, s->dtype, (hipStream_t)hip_stream);

@@ -21,13 +21,14 @@ struct XAttnArgs {
   float* lse;              // [B, H, Sq], natural logarithm (forward: may be null)
   float* dtable;           // [nb, H] or null
   float* dsum;             // workspace [B, H, Sq]: D of the backward
-  float* tpart;            // workspace [B, H, ceil(Sq / 128)][nb]: sums of dS by bucket
+  float* tpart;            // workspace [B, H, ceil(Sq * dq_ks / 128)][nb]: sums of dS by bucket
   float* part;             // workspace: partial results of the splits
   int64_t sq[3], sk[3], sv[3], so[3], sdo[3], sdq[3], sdk[3], sdv[3];
   int B, Sq, Sk, H, G, rep;  // G key heads, rep = H / G query heads to each
   int causal;
   int kv_chunk, kv_splits;   // XKvPlan
   int few_waves, few_splits; // XFewPlan
+  int dq_ks;                 // xattn_dq_split
   float c;      // scale * log2(e)
   float scale;
   // Buckets (attn_relpos): nb in all, nbd to a direction, `one` of them with one
@@ -43,6 +44,9 @@ struct XKvPlan {
   int rows, chunk, splits;
 };
 XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_dtype dt);
+
+// Wavefronts (1 or 2) that share 32 queries in the dQ kernel, along the keys.
+int xattn_dq_split(int B, int H, int Sq, int causal, bool bias, stage_dtype dt);
 
 // The forward kernel that serves few queries (xattn_few.hip): wavefronts of a
 // work-group and splits of the keys, 0 splits where the other kernel is faster.  With

@@ -20,6 +20,7 @@
 //     fixed order.
 
 #include <algorithm>
+#include <cmath>
 
 #include "xattn.h"
 
@@ -35,6 +36,10 @@ __device__ __forceinline__ void x_block(const XAttnArgs& a, int nrow, bool last_
 }
 
 __device__ __forceinline__ int x_dist_n(const XAttnArgs& a) { return 2 * (a.reach + XPAD) + 1; }
+
+// An index into that table, told to be one: only then do the reads' offsets go into
+// the instructions.
+__device__ __forceinline__ int x_idx(int i) { return i & 0x1fff; }
 
 // The bias of head h by distance, -(reach + XPAD) .. reach + XPAD, in units of
 // log2.
@@ -150,7 +155,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(
         uint32_t bits = x_lane_bits(rows, hf);
         if (a.causal) bits &= x_upto(p0 + rr - k0 - 4 * hf);
         if (near) {
-          const float* d = dist + (k0 + 4 * hf - p0 - rr + mid);
+          const float* d = dist + x_idx(k0 + 4 * hf - p0 - rr + mid);
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], mul, d[8 * (r >> 2) + (r & 3)]);
         } else {
@@ -218,26 +223,35 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(
 // so that diagonals which leave query 31 go on in the upper lanes.  96 vector
 // instructions and no LDS: adding the 1024 values to 63 sums in LDS took 190 cycles
 // per atomic of a wavefront (the dQ kernel of 32 x 512 tokens and 12 heads 315 us).
-__device__ __forceinline__ float x_diagonals(const f32x16_t& s) {
-  float d = 0.0f;
-  auto step = [&](uint32_t v) {
+__device__ __forceinline__ float x_diagonals(const f32x16_t& s, int lane) {
+  // Keys 0-15 and 16-31 in a chain each (a lane move has to wait for the addition
+  // before it), joined by moving the first one's sums 16 lanes up.
+  float d[2] = {0.0f, 0.0f};
+  auto step = [](float& d, uint32_t v) {
     const float up = __uint_as_float(
         __builtin_amdgcn_update_dpp(0, __float_as_uint(d), 0x138 /* wave_shr:1 */, 0xf, 0xf, true));
     d = up + __uint_as_float(v);
   };
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t hi[4];
+  for (int i = 0; i < 2; ++i) {
+    uint32_t hi[2][4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[4 * i + e]), 0u, false, false);
-      step(r[0]);
-      hi[e] = r[1];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[8 * c + 4 * i + e]), 0u, false,
+                                                        false);
+        step(d[c], r[0]);
+        hi[c][e] = r[1];
+      }
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) step(hi[e]);
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) step(d[c], hi[c][e]);
   }
-  return d;
+  const float up = __shfl_up(d[0], 16, 64);
+  return lane < 16 ? d[1] : d[1] + up;
 }
 
 // Adds v of lane l, the sum at distance rel0 + l (lanes from n on have none), to
@@ -257,9 +271,11 @@ __device__ __forceinline__ void x_add_buckets(const XAttnArgs& a, float v, int r
   __builtin_amdgcn_wave_barrier();
 }
 
-template <typename T, bool BIAS, bool RED>
-__global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
-  constexpr int TILE = XKT * XT<T>::ROWB;
+// KS = 2: two wavefronts share 32 queries, one with the first 32 keys of each block
+// and one with the others, and add up at the end; a work-group has 64 queries then.
+template <typename T, bool BIAS, bool RED, int KS>
+__global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a) {
+  constexpr int TILE = XKT * XT<T>::ROWB, QB = XQB / KS, QW = 4 / KS;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   // [2][K, V]; with a bias: dist, the wavefronts' sums by distance [4][nd] and by
   // bucket [4][nb]
@@ -277,17 +293,17 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
   }
 
   int qb, bh;
-  const int nq = (a.Sq + XQB - 1) / XQB;
+  const int nq = (a.Sq + QB - 1) / QB;
   x_block(a, nq, a.causal, qb, bh);
   const int b = bh / a.H, h = bh % a.H, g = h / a.rep;
-  const int q0 = qb * XQB + wave * 32, q = q0 + rr;
+  const int q0 = qb * QB + wave % QW * 32, q = q0 + rr, ks = wave / QW;
   const bool qv = q < a.Sq;
   const int qp = x_q_pos(a, b);
   const int p0 = q0 + qp;
   const T* K = (const T*)a.k + b * a.sk[0] + g * a.sk[2];
   const T* V = (const T*)a.v + b * a.sv[0] + g * a.sv[2];
   const int lim =
-      a.causal ? max(0, min(a.Sk, min(qb * XQB + XQB, a.Sq) + qp)) : a.Sk;
+      a.causal ? max(0, min(a.Sk, min(qb * QB + QB, a.Sq) + qp)) : a.Sk;
 
   const typename XT<T>::Frag qf = x_frag(
       (const T*)a.q + b * a.sq[0] + (int64_t)q * a.sq[1] + h * a.sq[2], qv, hf);
@@ -318,6 +334,17 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
     for (int i = lane; i < a.nb; i += 64) bsum[i] = 0.0f;
   }
 
+  // Sum of a value over the wavefronts that share the queries (in the ring's place,
+  // after the pass's last barrier), the same in both.
+  auto join = [&](float v) {
+    if constexpr (KS == 1) return v;
+    float* p = (float*)lds + lane;
+    p[wave * 64] = v;
+    __syncthreads();
+    v = p[wave % QW * 64] + p[(wave % QW + QW) * 64];
+    __syncthreads();
+    return v;
+  };
   f32x16_t dq[2] = {zero16(), zero16()};
   f32x16_t pk[2] = {zero16(), zero16()};  // FIX: P K
   float rsum = 0.0f;                      // FIX: row sum of dS; RED: of P
@@ -342,7 +369,8 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
         __syncthreads();
       }
 #pragma unroll
-      for (int sub = 0; sub < 2; ++sub) {
+      for (int i = 0; i < 2 / KS; ++i) {
+        const int sub = KS == 2 ? ks : i;
         const int k0 = kb * XKT + 32 * sub;
         const uint32_t rows = (uint32_t)(word >> (32 * sub));
         if (rows == 0 || (a.causal && k0 > p0 + 31)) continue;
@@ -354,7 +382,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
         const bool full = rows == 0xffffffffu && (!a.causal || k0 + 31 <= p0);
         const bool near = BIAS && k0 + 31 - p0 > -a.reach && k0 - p0 - 31 < a.reach;
         if (near) {
-          const float* d = dist + (k0 + 4 * hf - p0 - rr + mid);
+          const float* d = dist + x_idx(k0 + 4 * hf - p0 - rr + mid);
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, d[8 * (r >> 2) + (r & 3)]) - lse2);
@@ -382,9 +410,12 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
             s[r] *= RED ? dp[r] - D : dp[r];  // dS
             if constexpr (FIX) rsum += s[r];
           }
+          // (bf16: the product first, whose rounded copy frees the registers that the
+          // diagonals' moves overwrite)
+          if constexpr (sizeof(T) == 2) x_mma_cols<T>(kv, 32 * sub, s, dq, lane);
           if constexpr (BIAS) {
             if (a.dtable && near) {
-              const float v = x_diagonals(s);
+              const float v = x_diagonals(s, lane);
               if (lane < 63) diag[k0 - p0 + 31 - lane + mid] += v;
             } else if (a.dtable) {
               float t = s[0];
@@ -394,7 +425,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
               else gfar_l += t;
             }
           }
-          x_mma_cols<T>(kv, 32 * sub, s, dq, lane);
+          if constexpr (sizeof(T) == 4) x_mma_cols<T>(kv, 32 * sub, s, dq, lane);
         }
       }
       kb = kn;
@@ -407,20 +438,44 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
     // rows of dS then sum to zero to the last bits, as far buckets of long rows
     // need.
     const HalfPair pr = half_pair(D), ps = half_pair(rsum);
-    const float total = ps.x + ps.y;
-    D = total == 0.0f ? 0.0f : (pr.x + pr.y) / total;
+    const float top = join(pr.x + pr.y), total = join(ps.x + ps.y);
+    D = total == 0.0f ? 0.0f : top / total;
   }
   sweep(std::false_type());
+  if constexpr (KS == 2) {
+    // [wavefront][dq, P K][register][lane]
+    float* p = (float*)lds + wave % QW * (FIX ? 64 : 32) * 64 + lane;
+    if (ks == 1) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          p[(16 * t + r) * 64] = dq[t][r];
+          if constexpr (FIX) p[(32 + 16 * t + r) * 64] = pk[t][r];
+        }
+    }
+    __syncthreads();
+    if (ks == 0) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          dq[t][r] += p[(16 * t + r) * 64];
+          if constexpr (FIX) pk[t][r] += p[(32 + 16 * t + r) * 64];
+        }
+    }
+    __syncthreads();
+  }
   if constexpr (FIX) {
     const HalfPair pr = half_pair(rsum);
-    const float off = pr.x + pr.y;
+    const float off = join(pr.x + pr.y);
     D += off;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[t][r] = fmaf(-off, pk[t][r], dq[t][r]);
   }
-  if (hf == 0 && qv) a.dsum[row] = D;
+  if (hf == 0 && qv && ks == 0) a.dsum[row] = D;
   if constexpr (BIAS) {
     if (a.dtable) {
       const float* all = diag - wave * nd;  // (after the pass's last barrier)
@@ -443,8 +498,9 @@ __global__ __launch_bounds__(256, 2) void xattn_dq_kernel(XAttnArgs a) {
             (p[i] + p[a.nb + i]) + (p[2 * a.nb + i] + p[3 * a.nb + i]);
     }
   }
-  x_store<T>(dq, a.scale, (T*)lds + wave * 32 * XT<T>::LD,
-             (T*)a.dq + b * a.sdq[0] + h * a.sdq[2], a.sdq[1], q0, a.Sq);
+  if (ks == 0)
+    x_store<T>(dq, a.scale, (T*)lds + wave * 32 * XT<T>::LD,
+               (T*)a.dq + b * a.sdq[0] + h * a.sdq[2], a.sdq[1], q0, a.Sq);
 }
 
 // ---------------------------------------------------------------------------
@@ -460,7 +516,7 @@ template <typename T> constexpr int kv_lds() {
 }
 
 __device__ __forceinline__ void x_dtable_sum(const XAttnArgs& a, int w, float* red) {
-  const int c = w % a.nb, h = w / a.nb, nq = (a.Sq + XQB - 1) / XQB;
+  const int qb = XQB / a.dq_ks, c = w % a.nb, h = w / a.nb, nq = (a.Sq + qb - 1) / qb;
   float t = 0.0f;
   for (int64_t i = threadIdx.x; i < (int64_t)a.B * nq; i += 256)
     t += a.tpart[((i / nq * a.H + h) * nq + i % nq) * a.nb + c];
@@ -586,9 +642,9 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
       if (a.causal) bits &= ~x_upto(k0 + rr - p0 - 4 * hf - 1);
       if constexpr (!BIAS) {
       } else if (near) {
-        const float* d = dist + (k0 + rr - p0 - 4 * hf + mid);
+        const float* d = dist + x_idx(k0 + rr - p0 - 4 * hf + mid - 27);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, d[-(8 * (r >> 2) + (r & 3))]);
+        for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, d[27 - (8 * (r >> 2) + (r & 3))]);
       } else {
         const float far = k0 > p0 ? far_r : far_l;
 #pragma unroll
@@ -678,20 +734,23 @@ hipError_t forward_t(const XAttnArgs& a, hipStream_t st) {
 template <typename T>
 hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
   hipError_t e = hipSuccess;
-  const int64_t gq = (int64_t)a.B * a.H * ((a.Sq + XQB - 1) / XQB);
+  const int qb = XQB / a.dq_ks;
+  const int64_t gq = (int64_t)a.B * a.H * ((a.Sq + qb - 1) / qb);
   if (gq > 0) {
+    // The bias gradient is a sum of many dS that nearly cancel, in fp32: with D from
+    // a bf16 out it would be off by out's rounding.
+    constexpr bool BF = sizeof(T) == 2;
+    const bool red = BF && a.dtable;
     size_t lds = 4 * XKT * XT<T>::ROWB;
-    if (!a.table) {
-      e = launch(xattn_dq_kernel<T, false, false>, gq, lds, st, a);
-    } else {
-      lds += dist_bytes(a) + 4 * (size_t)(2 * (a.reach + XPAD) + 1 + a.nb) * 4;
-      // The bias gradient is a sum of many dS that nearly cancel, in fp32: with
-      // D from a bf16 out it would be off by out's rounding.
-      if (sizeof(T) == 2 && a.dtable)
-        e = launch(xattn_dq_kernel<T, true, sizeof(T) == 2>, gq, lds, st, a);
-      else
-        e = launch(xattn_dq_kernel<T, true, false>, gq, lds, st, a);
-    }
+    if (a.table) lds += dist_bytes(a) + 4 * (size_t)(2 * (a.reach + XPAD) + 1 + a.nb) * 4;
+    if (a.dq_ks == 1)
+      e = !a.table ? launch(xattn_dq_kernel<T, false, false, 1>, gq, lds, st, a)
+          : red    ? launch(xattn_dq_kernel<T, true, BF, 1>, gq, lds, st, a)
+                   : launch(xattn_dq_kernel<T, true, false, 1>, gq, lds, st, a);
+    else
+      e = !a.table ? launch(xattn_dq_kernel<T, false, false, 2>, gq, lds, st, a)
+          : red    ? launch(xattn_dq_kernel<T, true, BF, 2>, gq, lds, st, a)
+                   : launch(xattn_dq_kernel<T, true, false, 2>, gq, lds, st, a);
     if (e != hipSuccess) return e;
   }
   const int64_t n_kv = (int64_t)a.B * a.G * ((a.Sk + XQB - 1) / XQB) * a.kv_splits;
@@ -708,6 +767,26 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
 }
 
 }  // namespace
+
+// Half as many queries to a work-group fill more CUs and waste fewer rows of the last
+// block, but read the keys twice as often.  us of both for 512 keys by work-groups per
+// CU, fitted to 30 shapes: 2 x 16 heads of 512 queries with bias 34 -> 26, 12 x 16 heads
+// 57 -> 67; under `causal`, where the long rows decide, 13 x 16 heads of 387 58 -> 50;
+// fp32, 8 x 12 heads of 128: 26 -> 19.
+int xattn_dq_split(int B, int H, int Sq, int causal, bool bias, stage_dtype dt) {
+  const double cus = device_cus(), bh = (double)B * H;
+  const double n1 = std::max(1.0, bh * ((Sq + XQB - 1) / XQB) / cus);
+  const double n2 = std::max(1.0, bh * ((Sq + XQB / 2 - 1) / (XQB / 2)) / cus);
+  double t1, t2;
+  if (dt == STAGE_F32) {
+    t1 = 11 + 52 * std::ceil(n1);
+    t2 = 8 + 26.5 * std::ceil(n2);
+  } else {
+    t1 = bias ? 24 + 10.8 * n1 : 8.5 + 8.5 * n1;
+    t2 = bias ? 15.5 + 8.4 * n2 : 8 + 6 * n2;
+  }
+  return t2 * (causal ? 0.8 : 1.0) < t1 ? 2 : 1;
+}
 
 XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_dtype dt) {
   const int rows = dt == STAGE_BF16 ? x_qb<bf16_t>() : x_qb<float>();
