@@ -1,5 +1,6 @@
 // C ABI of the attention operators (include/attn.h): argument checks, the borders
 // of the relative position buckets, the workspace's layout.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstdarg>
@@ -22,19 +23,21 @@ stage_status bad(stage_status st, const char* fmt, ...) {
 // A natural number of up to 4096 bits, for exact powers.
 struct Big {
   uint32_t w[128] = {1};
-  void mul(uint32_t f) {
-    uint64_t c = 0;
-    for (uint32_t& x : w) {
-      c += (uint64_t)x * f;
-      x = (uint32_t)c;
-      c >>= 32;
+  int n = 1;  // words in use
+  void mul(uint32_t f, int times) {
+    while (times-- > 0) {
+      uint64_t c = 0;
+      for (int i = 0; i < n; ++i) {
+        c += (uint64_t)w[i] * f;
+        w[i] = (uint32_t)c;
+        c >>= 32;
+      }
+      if (c) w[n++] = (uint32_t)c;
     }
   }
-  void mul(uint32_t f, int times) {
-    while (times-- > 0) mul(f);
-  }
   bool operator>=(const Big& o) const {
-    for (int i = 127; i >= 0; --i)
+    if (n != o.n) return n > o.n;
+    for (int i = n - 1; i >= 0; --i)
       if (w[i] != o.w[i]) return w[i] > o.w[i];
     return true;
   }
@@ -81,7 +84,7 @@ struct Workspace {
   int64_t dsum, tpart, part, total;  // bytes
   XKvPlan kv;
   XFewPlan few;
-  int dq_ks;
+  XDqPlan dq;
 };
 Workspace workspace_of(const attn_shape* s, const attn_relpos* rp, bool backward) {
   Workspace w{};
@@ -96,14 +99,17 @@ Workspace workspace_of(const attn_shape* s, const attn_relpos* rp, bool backward
     return w;
   }
   w.dsum = ((int64_t)s->batch * s->heads * s->seq_q * 4 + 15) / 16 * 16;
-  w.dq_ks = xattn_dq_split(s->batch, s->heads, s->seq_q, s->causal, rp != nullptr, s->dtype);
-  const int64_t qb = 128 / w.dq_ks;  // queries of a work-group
+  w.dq = xattn_dq_plan(s->batch, s->heads, s->seq_q, s->seq_k, s->causal, rp != nullptr, s->dtype);
+  const int64_t qb = 128 / w.dq.ks;  // queries of a work-group
   if (rp)
     w.tpart = ((int64_t)s->batch * s->heads * ((s->seq_q + qb - 1) / qb) * rp->num_buckets * 4 + 15) /
               16 * 16;
   w.kv = xattn_kv_plan(s->batch, s->kv_heads, rep, s->seq_q, s->seq_k, s->causal, s->dtype);
   if (w.kv.splits > 1)
     w.part = (int64_t)w.kv.splits * s->batch * s->kv_heads * s->seq_k * 2 * XHD * 4;
+  if (w.dq.splits > 1)  // (its partial results are summed before those of dK, dV are made)
+    w.part = std::max(w.part, (int64_t)w.dq.splits * s->batch * s->heads * s->seq_q *
+                                  xattn_dq_row(s->dtype) * 4);
   w.total = w.dsum + w.tpart + w.part;
   return w;
 }
@@ -230,10 +236,11 @@ stage_status attn_relpos_init(int num_buckets, int max_distance, int bidirection
   r.n_borders = k.m - 1;
   r.reach = k.one;
   for (int j = 1; j < k.m; ++j) {
-    // An estimate, moved to the least distance that is in the bucket.
-    int n = (int)std::lround(k.one * std::pow((double)max_distance / k.one, (double)j / k.m));
-    while (n > k.one && reaches(n - 1, k.one, k.m, max_distance, j)) --n;
-    while (!reaches(n, k.one, k.m, max_distance, j)) ++n;
+    // The border as a real number (at most 2048, in 53 bits) tells its least whole
+    // number, except next to one, which is looked at exactly.
+    const double x = k.one * std::pow((double)max_distance / k.one, (double)j / k.m);
+    int n = (int)std::lround(x);
+    if (std::fabs(x - n) > 1e-6 ? n < x : !reaches(n, k.one, k.m, max_distance, j)) ++n;
     r.border[j - 1] = r.reach = n;
   }
   *out = r;
@@ -347,7 +354,8 @@ stage_status attn_backward(const attn_shape* s, const attn_relpos* rp, const flo
   a.dsum = (float*)workspace;
   a.tpart = (float*)((char*)workspace + w.dsum);
   a.part = (float*)((char*)workspace + w.dsum + w.tpart);
-  a.dq_ks = w.dq_ks;
+  a.dq_ks = w.dq.ks;
+  a.dq_splits = w.dq.splits;
   a.kv_chunk = w.kv.chunk;
   a.kv_splits = w.kv.splits;
   const hipError_t e = xattn_backward(a, s->dtype, (hipStream_t)hip_stream);

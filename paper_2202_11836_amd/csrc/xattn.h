@@ -28,7 +28,7 @@ struct XAttnArgs {
   int causal;
   int kv_chunk, kv_splits;   // XKvPlan
   int few_waves, few_splits; // XFewPlan
-  int dq_ks;                 // xattn_dq_split
+  int dq_ks, dq_splits;      // XDqPlan
   float c;      // scale * log2(e)
   float scale;
   // Buckets (attn_relpos): nb in all, nbd to a direction, `one` of them with one
@@ -45,8 +45,15 @@ struct XKvPlan {
 };
 XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_dtype dt);
 
-// Wavefronts (1 or 2) that share 32 queries in the dQ kernel, along the keys.
-int xattn_dq_split(int B, int H, int Sq, int causal, bool bias, stage_dtype dt);
+// How the dQ kernel goes along the keys: ks wavefronts (1 or 2) of a work-group share
+// 32 queries, and `splits` work-groups the keys.  With several splits each leaves, per
+// query, xattn_dq_row floats in the workspace, [split][B, H][Sq]: 64 of dQ, on bf16
+// also 64 of P K and the sum of its dS.
+struct XDqPlan {
+  int ks, splits;
+};
+XDqPlan xattn_dq_plan(int B, int H, int Sq, int Sk, int causal, bool bias, stage_dtype dt);
+inline int xattn_dq_row(stage_dtype dt) { return dt == STAGE_BF16 ? 132 : 64; }
 
 // The forward kernel that serves few queries (xattn_few.hip): wavefronts of a
 // work-group and splits of the keys, 0 splits where the other kernel is faster.  With

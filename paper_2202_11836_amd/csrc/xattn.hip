@@ -61,21 +61,22 @@ __device__ __forceinline__ void x_clear_hidden(char* kv, uint64_t word) {
   }
 }
 
-// The blocks of a pass over the keys, with the first of them on its way into stage
-// 0: block 0 is requested before the mask says whether it holds a key (it nearly
+// The blocks [first, last) of a pass over the keys, with the first of them on its way
+// into stage 0: block `first` is requested before the mask says whether it holds a key (it nearly
 // always does), so that the two latencies overlap.  Returns the first block.
 template <typename T>
 __device__ __forceinline__ int x_start(const XAttnArgs& a, int b, const T* K, const T* V, int lim,
-                                       char* kv, int wave, int lane, KeyBlocks<XKT>& blocks) {
+                                       int first, int last, char* kv, int wave, int lane,
+                                       KeyBlocks<XKT>& blocks) {
   constexpr int TILE = XKT * XT<T>::ROWB;
-  blocks.init(a.mask ? a.mask + (int64_t)b * a.Sk : nullptr, lim, (lim + XKT - 1) / XKT, lane);
-  if (blocks.nblk == 0) return 0;
-  x_dma<T, XKT, 4>(K, a.sk[1], 0, lim, kv, wave, lane);
-  x_dma<T, XKT, 4>(V, a.sv[1], 0, lim, kv + TILE, wave, lane);
-  blocks.load(0);
-  const int kb = blocks.next(0);
-  if (kb > 0) wait_all();  // (each wavefront writes its own rows of the tiles)
-  if (kb > 0 && kb < blocks.nblk) {
+  blocks.init(a.mask ? a.mask + (int64_t)b * a.Sk : nullptr, lim, last, lane);
+  if (first >= last) return last;
+  x_dma<T, XKT, 4>(K, a.sk[1], first * XKT, lim, kv, wave, lane);
+  x_dma<T, XKT, 4>(V, a.sv[1], first * XKT, lim, kv + TILE, wave, lane);
+  blocks.load(first);
+  const int kb = blocks.next(first);
+  if (kb > first) wait_all();  // (each wavefront writes its own rows of the tiles)
+  if (kb > first && kb < last) {
     x_dma<T, XKT, 4>(K, a.sk[1], kb * XKT, lim, kv, wave, lane);
     x_dma<T, XKT, 4>(V, a.sv[1], kb * XKT, lim, kv + TILE, wave, lane);
   }
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(
       x_frag((const T*)a.q + b * a.sq[0] + (int64_t)(q0 + rr) * a.sq[1] + h * a.sq[2],
              q0 + rr < a.Sq, hf);
   KeyBlocks<XKT> blocks;
-  int kb = x_start(a, b, K, V, lim, lds, wave, lane, blocks);
+  int kb = x_start(a, b, K, V, lim, 0, (lim + XKT - 1) / XKT, lds, wave, lane, blocks);
   float far_l = 0.0f, far_r = 0.0f;
   const int mid = a.reach + XPAD;
   if constexpr (BIAS) {
@@ -294,7 +295,10 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
 
   int qb, bh;
   const int nq = (a.Sq + QB - 1) / QB;
-  x_block(a, nq, a.causal, qb, bh);
+  attn_block(blockIdx.x, gridDim.x, nq * a.dq_splits, qb, bh);
+  const int split = qb % a.dq_splits;
+  qb /= a.dq_splits;
+  if (a.causal) qb = nq - 1 - qb;  // (the long ones start first)
   const int b = bh / a.H, h = bh % a.H, g = h / a.rep;
   const int q0 = qb * QB + wave % QW * 32, q = q0 + rr, ks = wave / QW;
   const bool qv = q < a.Sq;
@@ -304,6 +308,9 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
   const T* V = (const T*)a.v + b * a.sv[0] + g * a.sv[2];
   const int lim =
       a.causal ? max(0, min(a.Sk, min(qb * QB + QB, a.Sq) + qp)) : a.Sk;
+
+  const int nblk = (lim + XKT - 1) / XKT, per = (nblk + a.dq_splits - 1) / a.dq_splits;
+  const int first = min(nblk, split * per), last = min(nblk, first + per);
 
   const typename XT<T>::Frag qf = x_frag(
       (const T*)a.q + b * a.sq[0] + (int64_t)q * a.sq[1] + h * a.sq[2], qv, hf);
@@ -348,10 +355,10 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
   f32x16_t dq[2] = {zero16(), zero16()};
   f32x16_t pk[2] = {zero16(), zero16()};  // FIX: P K
   float rsum = 0.0f;                      // FIX: row sum of dS; RED: of P
-  auto sweep = [&](auto first) {
-    constexpr bool SUM_D = decltype(first)::value;
+  auto sweep = [&](auto sum_d) {
+    constexpr bool SUM_D = decltype(sum_d)::value;
     KeyBlocks<XKT> blocks;
-    int kb = x_start(a, b, K, V, lim, lds, wave, lane, blocks);
+    int kb = x_start(a, b, K, V, lim, first, last, lds, wave, lane, blocks);
     for (int st = 0; kb < blocks.nblk; st ^= 1) {
       const uint64_t word = blocks.word(kb);
       const uint64_t hidden = blocks.in_range(kb) & ~word;
@@ -469,13 +476,33 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
   if constexpr (FIX) {
     const HalfPair pr = half_pair(rsum);
     const float off = join(pr.x + pr.y);
-    D += off;
+    if (a.dq_splits > 1) {
+      rsum = off;
+    } else {
+      D += off;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dq[t][r] = fmaf(-off, pk[t][r], dq[t][r]);
+        for (int r = 0; r < 16; ++r) dq[t][r] = fmaf(-off, pk[t][r], dq[t][r]);
+    }
   }
-  if (hf == 0 && qv && ks == 0) a.dsum[row] = D;
+  if (hf == 0 && qv && ks == 0 && split == 0) a.dsum[row] = D;
+  if constexpr (!RED) {
+    if (a.dq_splits > 1) {
+      if (ks == 1) return;
+      constexpr int ROW = sizeof(T) == 2 ? 132 : 64;
+      float* to = a.part + (((int64_t)split * a.B + b) * a.H + h) * a.Sq * ROW;
+      float* stage = (float*)lds + wave * 32 * XT<float>::LD;
+      x_store<float>(dq, 1.0f, stage, to, ROW, q0, a.Sq);
+      if constexpr (FIX) {
+        lds_wait();
+        __builtin_amdgcn_wave_barrier();
+        x_store<float>(pk, 1.0f, stage, to + XHD, ROW, q0, a.Sq);
+        if (hf == 0 && qv) to[(int64_t)q * ROW + 2 * XHD] = rsum;
+      }
+      return;
+    }
+  }
   if constexpr (BIAS) {
     if (a.dtable) {
       const float* all = diag - wave * nd;  // (after the pass's last barrier)
@@ -501,6 +528,37 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
   if (ks == 0)
     x_store<T>(dq, a.scale, (T*)lds + wave * 32 * XT<T>::LD,
                (T*)a.dq + b * a.sdq[0] + h * a.sdq[2], a.sdq[1], q0, a.Sq);
+}
+
+// dQ and D from the splits, in order: 16 threads to a query, 4 columns each.
+template <typename T>
+__global__ __launch_bounds__(256) void xattn_dq_sum_kernel(XAttnArgs a) {
+  constexpr bool FIX = sizeof(T) == 2;
+  constexpr int ROW = FIX ? 132 : 64;
+  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), n = (int64_t)a.B * a.H * a.Sq;
+  if (row >= n) return;
+  const int c = (threadIdx.x & 15) * 4;
+  const float* p = a.part + row * ROW;
+  f32x4_t dq = {0.0f, 0.0f, 0.0f, 0.0f}, pk = dq;
+  float off = 0.0f;
+#pragma unroll 4
+  for (int i = 0; i < a.dq_splits; ++i, p += n * ROW) {
+    dq += *(const f32x4_t*)(p + c);
+    if constexpr (FIX) {
+      pk += *(const f32x4_t*)(p + XHD + c);
+      off += p[2 * XHD];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) dq[e] = (FIX ? fmaf(-off, pk[e], dq[e]) : dq[e]) * a.scale;
+  const int q = (int)(row % a.Sq), bh = (int)(row / a.Sq), b = bh / a.H, h = bh % a.H;
+  T* to = (T*)a.dq + b * a.sdq[0] + (int64_t)q * a.sdq[1] + h * a.sdq[2] + c;
+  if constexpr (FIX) {
+    *(u32x2_t*)to = u32x2_t{pack_bf16x2(dq[0], dq[1]), pack_bf16x2(dq[2], dq[3])};
+    if (c == 0) a.dsum[row] += off;
+  } else {
+    *(f32x4_t*)to = dq;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -735,7 +793,7 @@ template <typename T>
 hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
   hipError_t e = hipSuccess;
   const int qb = XQB / a.dq_ks;
-  const int64_t gq = (int64_t)a.B * a.H * ((a.Sq + qb - 1) / qb);
+  const int64_t gq = (int64_t)a.B * a.H * ((a.Sq + qb - 1) / qb) * a.dq_splits;
   if (gq > 0) {
     // The bias gradient is a sum of many dS that nearly cancel, in fp32: with D from
     // a bf16 out it would be off by out's rounding.
@@ -751,6 +809,8 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
       e = !a.table ? launch(xattn_dq_kernel<T, false, false, 2>, gq, lds, st, a)
           : red    ? launch(xattn_dq_kernel<T, true, BF, 2>, gq, lds, st, a)
                    : launch(xattn_dq_kernel<T, true, false, 2>, gq, lds, st, a);
+    if (e == hipSuccess && a.dq_splits > 1)
+      e = launch(xattn_dq_sum_kernel<T>, ((int64_t)a.B * a.H * a.Sq + 15) / 16, 0, st, a);
     if (e != hipSuccess) return e;
   }
   const int64_t n_kv = (int64_t)a.B * a.G * ((a.Sk + XQB - 1) / XQB) * a.kv_splits;
@@ -773,7 +833,7 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
 // CU, fitted to 30 shapes: 2 x 16 heads of 512 queries with bias 34 -> 26, 12 x 16 heads
 // 57 -> 67; under `causal`, where the long rows decide, 13 x 16 heads of 387 58 -> 50;
 // fp32, 8 x 12 heads of 128: 26 -> 19.
-int xattn_dq_split(int B, int H, int Sq, int causal, bool bias, stage_dtype dt) {
+XDqPlan xattn_dq_plan(int B, int H, int Sq, int Sk, int causal, bool bias, stage_dtype dt) {
   const double cus = device_cus(), bh = (double)B * H;
   const double n1 = std::max(1.0, bh * ((Sq + XQB - 1) / XQB) / cus);
   const double n2 = std::max(1.0, bh * ((Sq + XQB / 2 - 1) / (XQB / 2)) / cus);
@@ -785,7 +845,18 @@ int xattn_dq_split(int B, int H, int Sq, int causal, bool bias, stage_dtype dt) 
     t1 = bias ? 24 + 10.8 * n1 : 8.5 + 8.5 * n1;
     t2 = bias ? 15.5 + 8.4 * n2 : 8 + 6 * n2;
   }
-  return t2 * (causal ? 0.8 : 1.0) < t1 ? 2 : 1;
+  const int ks = t2 * (causal ? 0.8 : 1.0) < t1 ? 2 : 1;
+  // Few queries over many keys: split the keys too, as far as CUs are free (two work-
+  // groups on one take turns).  A block of 64 keys takes 0.75 us, fp32 3.3, the sum of
+  // the splits a launch of 5: 16 x 4 heads of 25 queries over 4045 keys 54 -> 20 + 5 us
+  // in 4 splits, fp32 221 -> 64 + 5; 4 x 16 heads of 64 over 1024 keys 18.6 -> 13.4 +
+  // 4.8.  (A bias gradient needs D before the pass: one split.)
+  const double wgs = bh * ((Sq + XQB / ks - 1) / (XQB / ks)), blocks = (Sk + XKT - 1) / XKT;
+  int splits = 1;
+  if (!bias && wgs > 0)
+    splits = std::max(1, (int)std::min(std::floor(cus / wgs), std::floor(blocks / 2)));
+  if (blocks * (dt == STAGE_F32 ? 3.3 : 0.75) * (1.0 - 1.0 / splits) < 8.0) splits = 1;
+  return {ks, splits};
 }
 
 XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_dtype dt) {
