@@ -28,11 +28,21 @@ namespace {
 
 constexpr int XQB = 128;  // rows (queries or keys) of a work-group
 
-// Work-groups in an order that starts the long ones first under `causal`.
-__device__ __forceinline__ void x_block(const XAttnArgs& a, int nrow, bool last_first, int& rb,
+// Work-group w of n -> (row block, batch * head): as attn_block, or, with `causal`, the
+// first row block of every head, then the second of every head, and so on (those with
+// the most work first).  Work-groups go round the CUs, and with a head's row blocks in
+// a row a CU got the same one of every head: 13 x 16 heads of 512 (with a bias) were as
+// slow as without `causal`, forward 25.5 -> 19.7 us, dQ 58.6 -> 41.2, dK and dV 45.4 ->
+// 31.7 in this order.  (A head stays on one XCD where the heads are a multiple of 8.)
+__device__ __forceinline__ void x_block(const XAttnArgs& a, int w, int n, int nq, int& rb,
                                         int& bh) {
-  attn_block(blockIdx.x, gridDim.x, nrow, rb, bh);
-  if (last_first) rb = nrow - 1 - rb;
+  if (a.causal) {
+    const int heads = n / nq;
+    rb = w / heads;
+    bh = w % heads;
+  } else {
+    attn_block(w, n, nq, rb, bh);
+  }
 }
 
 __device__ __forceinline__ int x_dist_n(const XAttnArgs& a) { return 2 * (a.reach + XPAD) + 1; }
@@ -93,7 +103,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(
   float* dist = (float*)(lds + 4 * TILE);
 
   int qb, bh;
-  x_block(a, (a.Sq + XQB - 1) / XQB, a.causal, qb, bh);
+  const int nq = (a.Sq + XQB - 1) / XQB;
+  x_block(a, blockIdx.x, gridDim.x, nq, qb, bh);
+  if (a.causal) qb = nq - 1 - qb;
   const int b = bh / a.H, h = bh % a.H, g = h / a.rep;
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -140,7 +152,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(
     for (int sub = 0; sub < 2; ++sub) {
       const int k0 = kb * XKT + 32 * sub;
       const uint32_t rows = (uint32_t)(word >> (32 * sub));
-      if (rows == 0 || (a.causal && k0 > p0 + 31)) continue;
+      if (rows == 0 || q0 >= a.Sq || (a.causal && k0 > p0 + 31)) continue;
       f32x16_t s = x_mma_rows(kv, 32 * sub, qf, zero16(), lane);
       const bool full = rows == 0xffffffffu && (!a.causal || k0 + 31 <= p0);
       const bool near = BIAS && k0 + 31 - p0 > -a.reach && k0 - p0 - 31 < a.reach;
@@ -295,10 +307,10 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
 
   int qb, bh;
   const int nq = (a.Sq + QB - 1) / QB;
-  attn_block(blockIdx.x, gridDim.x, nq * a.dq_splits, qb, bh);
+  x_block(a, blockIdx.x, gridDim.x, nq * a.dq_splits, qb, bh);
   const int split = qb % a.dq_splits;
   qb /= a.dq_splits;
-  if (a.causal) qb = nq - 1 - qb;  // (the long ones start first)
+  if (a.causal) qb = nq - 1 - qb;
   const int b = bh / a.H, h = bh % a.H, g = h / a.rep;
   const int q0 = qb * QB + wave % QW * 32, q = q0 + rr, ks = wave / QW;
   const bool qv = q < a.Sq;
@@ -380,7 +392,7 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
         const int sub = KS == 2 ? ks : i;
         const int k0 = kb * XKT + 32 * sub;
         const uint32_t rows = (uint32_t)(word >> (32 * sub));
-        if (rows == 0 || (a.causal && k0 > p0 + 31)) continue;
+        if (rows == 0 || q0 >= a.Sq || (a.causal && k0 > p0 + 31)) continue;
         f32x16_t s = x_mma_rows(kv, 32 * sub, qf, zero16(), lane);
         // (RED: both passes form the same dP, so that the matrix core's rounding,
         // which is one-sided, cancels in dP - D; from an accumulator that starts at
@@ -597,7 +609,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int kblk, bg;
-  attn_block(blockIdx.x, n_kv, (a.Sk + XQB - 1) / XQB * a.kv_splits, kblk, bg);
+  x_block(a, blockIdx.x, n_kv, (a.Sk + XQB - 1) / XQB * a.kv_splits, kblk, bg);
   const int split = kblk % a.kv_splits;
   kblk /= a.kv_splits;
   const int b = bg / a.G, g = bg % a.G;
