@@ -298,6 +298,7 @@ stage_status attn_forward(const attn_shape* s, const attn_relpos* rp, const floa
   a.part = (float*)workspace;
   a.few_waves = w.few.waves;
   a.few_splits = w.few.splits;
+  a.few_stream = w.few.stream;
   const hipError_t e = xattn_forward(a, s->dtype, (hipStream_t)hip_stream);
   if (e != hipSuccess) return bad(STAGE_EHIP, "attn_forward: %s", hipGetErrorString(e));
   return STAGE_OK;

@@ -27,7 +27,7 @@ struct XAttnArgs {
   int B, Sq, Sk, H, G, rep;  // G key heads, rep = H / G query heads to each
   int causal;
   int kv_chunk, kv_splits;   // XKvPlan
-  int few_waves, few_splits; // XFewPlan
+  int few_waves, few_splits, few_stream;  // XFewPlan
   int dq_ks, dq_splits;      // XDqPlan
   float c;      // scale * log2(e)
   float scale;
@@ -56,13 +56,14 @@ XDqPlan xattn_dq_plan(int B, int H, int Sq, int Sk, int causal, bool bias, stage
 inline int xattn_dq_row(stage_dtype dt) { return dt == STAGE_BF16 ? 132 : 64; }
 
 // The forward kernel that serves few queries (xattn_few.hip): wavefronts of a
-// work-group and splits of the keys, 0 splits where the other kernel is faster.  With
+// work-group and splits of the keys, 0 splits where the other kernel is faster; stream:
+// keys and values are marked as read once.  With
 // more than one split it leaves, in the workspace, per split and row (query and query
 // head of a key head, in tiles of 32) XFEW_ROW floats: 64 sums of P v, the exponents'
 // offset and the sum of P.  buckets, reach: of the bias, 0 without one.
 constexpr int XFEW_ROW = 68;
 struct XFewPlan {
-  int waves, splits;
+  int waves, splits, stream;
 };
 XFewPlan xattn_few_plan(int B, int G, int rep, int Sq, int Sk, int buckets, int reach,
                         stage_dtype dt);
@@ -128,8 +129,8 @@ __device__ __forceinline__ int x_off(int r, int c) {
 
 // Rows [row0, row0 + NR) of a [lim][64] operand into a tile with direct-to-LDS
 // loads by NW wavefronts; rows from lim on are zero.  The buffer resource starts at
-// row0, so the operand may be of any length.
-template <typename T, int NR, int NW>
+// row0, so the operand may be of any length.  STREAM: marked as read once.
+template <typename T, int NR, int NW, bool STREAM = false>
 __device__ __forceinline__ void x_dma(const T* base, int64_t ld, int row0, int lim, char* tile,
                                       int wave, int lane) {
   constexpr int RPI = 1024 / XT<T>::ROWB, CPR = XT<T>::CPR;
@@ -143,7 +144,8 @@ __device__ __forceinline__ void x_dma(const T* base, int64_t ld, int row0, int l
     const int r = RPI * q + lane / CPR;
     const int c = (lane % CPR) ^ XT<T>::swz(r);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_t*)(tile + q * 1024), 16,
-                                             r * (int)ld * (int)sizeof(T) + 16 * c, 0, 0, 0);
+                                             r * (int)ld * (int)sizeof(T) + 16 * c, 0, 0,
+                                             STREAM ? 2 /* nt */ : 0);
   }
 }
 
@@ -161,6 +163,20 @@ __device__ __forceinline__ typename XT<T>::Frag x_frag(const T* p, bool valid, i
   }
   return r;
 }
+
+// Waits for values that were loaded, here: with the wait left to their first use inside a
+// loop, the compiler has every iteration wait for every load in flight.
+template <typename F>
+__device__ __forceinline__ void x_arrived(F& r) {
+  constexpr int N = sizeof(r) / 16;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    u32x4_t w = __builtin_bit_cast(u32x4_t, r.f[i]);
+    asm volatile("" : "+v"(w));
+    r.f[i] = __builtin_bit_cast(decltype(r.f[0] + r.f[0]), w);
+  }
+}
+__device__ __forceinline__ void x_arrived(float& v) { asm volatile("" : "+v"(v)); }
 
 __device__ __forceinline__ f32x16_t mfma32_f32(float a, float b, f32x16_t c) {
   return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
@@ -242,12 +258,6 @@ __device__ __forceinline__ void x_store(const f32x16_t acc[2], float mul, T* sta
     if (row0 + row < nrows)
       *(u32x4_t*)(dst + (int64_t)(row0 + row) * ld + col) = *(const u32x4_t*)(stage + row * LD + col);
   }
-}
-
-// "At most N vector memory operations outstanding, no LDS operation" (gfx9 encoding).
-template <int N>
-__device__ __forceinline__ void x_wait_vm() {
-  __builtin_amdgcn_s_waitcnt((N & 15) | 0x70 | (((N >> 4) & 3) << 14));
 }
 
 // The blocks of BK keys that a wavefront goes through: those of [0, nblk) that

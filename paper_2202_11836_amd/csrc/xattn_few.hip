@@ -5,13 +5,14 @@
 // the keys share the work along the keys, and are joined by their exponents' offsets
 // and sums, in LDS and, with several splits, by a second launch.  Each wavefront has
 // a two-stage ring of 32-key blocks in LDS to itself and waits for nobody until the
-// join; with 8 wavefronts on a CU (in one work-group or two) 64 KB are on their way
-// at any time.  The scores and products are those of xattn.hip: a tile costs 0.3 us
-// of a SIMD's time whether one of its rows is in use or all, and its 8 KB take the
-// memory 0.4 us at 256 CUs' share of 5.2 TB/s and 4 SIMDs.  Measured: 16 x 16 heads,
-// one token over 8192 keys, 97 us (5.5 TB/s); where there is less to read, the chain
-// of one wavefront's blocks (0.75 us each) and the join (5 us) are what is left.  A
-// ring of 3 or 4 stages changed nothing.
+// join: it waits for a block, requests the next one and computes.  (Requesting before the
+// wait puts twice as much on its way and is slower for long caches: 16 x 16 heads over
+// 8192 keys 105 us, 98 like this, and a plain read of as many bytes takes 88 to 93.)
+// The scores and products are those of xattn.hip: a tile costs 0.3 us of a SIMD's time
+// whether one of its rows is in use or all, and its 8 KB take the memory 0.4 us at 256
+// CUs' share of 5.5 TB/s and 4 SIMDs.  Measured: 16 x 16 heads, one token over 8192
+// keys, 98 us (5.5 TB/s); where there is less to read, the chain of one wavefront's
+// blocks and the join (5 us) are what is left.
 #include <algorithm>
 #include <cmath>
 
@@ -80,7 +81,7 @@ size_t few_near_bytes(int nb, int reach) { return nb ? 128 * (size_t)nb + 2 * (r
 
 template <typename T, bool BIAS, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void xattn_few_kernel(XAttnArgs a, int n_rt) {
-  constexpr int TILE = FB * XT<T>::ROWB, NDMA = 2 * TILE / 1024;
+  constexpr int TILE = FB * XT<T>::ROWB;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   // [NW][2][K, V]; with a bias: the rows' biases [nb][32] and the buckets by distance
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
@@ -107,12 +108,17 @@ __global__ __launch_bounds__(64 * NW, 2) void xattn_few_kernel(XAttnArgs a, int 
   blocks.init(a.mask ? a.mask + (int64_t)b * a.Sk : nullptr, lim, min(nblk, first + per), lane);
   auto dma = [&](int kb, int stage) {
     char* to = ring + stage * 2 * TILE;
-    x_dma<T, FB, 1>(K, a.sk[1], kb * FB, lim, to, 0, lane);
-    x_dma<T, FB, 1>(V, a.sv[1], kb * FB, lim, to + TILE, 0, lane);
+    if (a.few_stream) {
+      x_dma<T, FB, 1, true>(K, a.sk[1], kb * FB, lim, to, 0, lane);
+      x_dma<T, FB, 1, true>(V, a.sv[1], kb * FB, lim, to + TILE, 0, lane);
+    } else {
+      x_dma<T, FB, 1>(K, a.sk[1], kb * FB, lim, to, 0, lane);
+      x_dma<T, FB, 1>(V, a.sv[1], kb * FB, lim, to + TILE, 0, lane);
+    }
   };
   // The first block is requested before the mask says whether it holds a key.
   if (first < blocks.nblk) dma(first, 0);
-  const typename XT<T>::Frag qf =
+  typename XT<T>::Frag qf =
       x_frag((const T*)a.q + b * a.sq[0] + (int64_t)i * a.sq[1] + h * a.sq[2], rv, hf);
   float far_l = 0.0f, far_r = 0.0f;
   const int mid = a.reach + XPAD;
@@ -143,16 +149,17 @@ __global__ __launch_bounds__(64 * NW, 2) void xattn_few_kernel(XAttnArgs a, int 
   float m = -INFINITY, lsum = 0.0f;
   f32x16_t acc[2] = {zero16(), zero16()};
   const TrAddr tr = tr_addr(lane);
+  x_arrived(qf);
+  if constexpr (BIAS) {
+    x_arrived(far_l);
+    x_arrived(far_r);
+  }
   for (int st = 0; kb < blocks.nblk; st ^= 1) {
     const int k0 = kb * FB;
     const uint32_t bw = blocks.word(kb), hidden = blocks.in_range(kb) & ~bw;
     kb = blocks.next(kb + 1);
-    if (kb < blocks.nblk) {
-      dma(kb, st ^ 1);
-      x_wait_vm<NDMA>();
-    } else {
-      x_wait_vm<0>();
-    }
+    wait_all();
+    if (kb < blocks.nblk) dma(kb, st ^ 1);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
     char* kv = ring + st * 2 * TILE;
@@ -351,7 +358,7 @@ XFewPlan xattn_few_plan(int B, int G, int rep, int Sq, int Sk, int buckets, int 
   const double tiles = (double)B * G * (double)xattn_few_tiles(rep, Sq), cus = device_cus();
   // (the model is one of few work-groups: 16 heads of 2500 queries are 1250 tiles and
   // take 60 us with the other kernel, 75 with this one)
-  if (tiles == 0.0 || tiles > (bf16 ? 4 : 1) * cus) return {0, 0};
+  if (tiles == 0.0 || tiles > (bf16 ? 4 : 1) * cus) return {0, 0, 0};
   const double other = (double)B * G * rep * ((Sq + 127) / 128);
   const double cap = bf16 ? 4 : 2, at_once = std::min(cap, std::ceil(other / cus));
   double best = std::ceil(other / (cap * cus)) *
@@ -359,7 +366,7 @@ XFewPlan xattn_few_plan(int B, int G, int rep, int Sq, int Sk, int buckets, int 
   // No faster than the memory: of several that are bound by it, the fewest
   // wavefronts (16 x 16 heads over 8192 keys: 97 us with 4, 112 with 8).
   const double floor = 2.0 + 2.0 * B * G * (double)Sk * (bf16 ? 128 : 256) / 5.2e6;
-  XFewPlan plan = {0, 0};
+  XFewPlan plan = {0, 0, 0};
   const int blocks = (Sk + FB - 1) / FB;
   for (int waves = 4; waves <= (bf16 ? 8 : 4); waves += 4) {
     const size_t lds = waves * 4 * FB * (bf16 ? 128 : 256) + few_near_bytes(buckets, reach);
@@ -376,10 +383,16 @@ XFewPlan xattn_few_plan(int B, int G, int rep, int Sq, int Sk, int buckets, int 
       t = std::max(t, floor);
       if (t < best) {
         best = t;
-        plan = {waves, splits};
+        plan = {waves, splits, 0};
       }
     }
   }
+  // One tile of rows over keys and values beyond the caches: loads that leave nothing
+  // there let more through (24 x 8 heads over 8192 keys, 403 MB: 90 -> 81 us; 32 x 16
+  // over 1024, 134 MB: 31.5 -> 28.1), but 32 x 16 over 512 (67 MB), whose keys the
+  // caches can hold, take 14.9 -> 15.9.
+  plan.stream = xattn_few_tiles(rep, Sq) == 1 &&
+                2.0 * B * G * (double)Sk * (bf16 ? 128 : 256) > 96.0 * (1 << 20);
   return plan;
 }
 
