@@ -332,9 +332,13 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
   float lse2 = qv ? a.lse[row] * XLOG2E : 0.0f;
   if (lse2 == -INFINITY) lse2 = INFINITY;  // no key: P = exp2(s - inf) = 0
   float D = 0.0f;
+  typename XT<T>::Frag of;
+  if constexpr (!RED)
+    of = x_frag((const T*)a.o + b * a.so[0] + (int64_t)q * a.so[1] + h * a.so[2], qv, hf);
+  // (the first keys are on their way while D and the tables are formed)
+  KeyBlocks<XKT> blocks;
+  int kb = x_start(a, b, K, V, lim, first, last, lds, wave, lane, blocks);
   if constexpr (!RED) {
-    const typename XT<T>::Frag of = x_frag(
-        (const T*)a.o + b * a.so[0] + (int64_t)q * a.so[1] + h * a.so[2], qv, hf);
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(of) / 16); ++i)
 #pragma unroll
@@ -369,8 +373,6 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
   float rsum = 0.0f;                      // FIX: row sum of dS; RED: of P
   auto sweep = [&](auto sum_d) {
     constexpr bool SUM_D = decltype(sum_d)::value;
-    KeyBlocks<XKT> blocks;
-    int kb = x_start(a, b, K, V, lim, first, last, lds, wave, lane, blocks);
     for (int st = 0; kb < blocks.nblk; st ^= 1) {
       const uint64_t word = blocks.word(kb);
       const uint64_t hidden = blocks.in_range(kb) & ~word;
@@ -459,6 +461,7 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
     const HalfPair pr = half_pair(D), ps = half_pair(rsum);
     const float top = join(pr.x + pr.y), total = join(ps.x + ps.y);
     D = total == 0.0f ? 0.0f : top / total;
+    kb = x_start(a, b, K, V, lim, first, last, lds, wave, lane, blocks);
   }
   sweep(std::false_type());
   if constexpr (KS == 2) {
