@@ -628,7 +628,7 @@ def _attn_call(fn, shape, args, backward, dev):
     import torch
     lib = load_library()
     n = ctypes.c_size_t()
-    if torch.cuda.current_device() != dev:
+    if torch._C._cuda_getDevice() != dev:
         with torch.cuda.device(dev):
             return _attn_call(fn, shape, args, backward, dev)
     _attn_check(lib.attn_workspace(shape, args[0], backward, ctypes.byref(n)))
