@@ -299,6 +299,7 @@ stage_status attn_forward(const attn_shape* s, const attn_relpos* rp, const floa
   a.few_waves = w.few.waves;
   a.few_splits = w.few.splits;
   a.few_stream = w.few.stream;
+  xattn_fwd_time(s->batch, s->heads, s->seq_q, s->seq_k, s->causal, s->dtype, &a.fwd_ks);
   const hipError_t e = xattn_forward(a, s->dtype, (hipStream_t)hip_stream);
   if (e != hipSuccess) return bad(STAGE_EHIP, "attn_forward: %s", hipGetErrorString(e));
   return STAGE_OK;
@@ -358,6 +359,7 @@ stage_status attn_backward(const attn_shape* s, const attn_relpos* rp, const flo
   a.dq_ks = w.dq.ks;
   a.dq_splits = w.dq.splits;
   a.kv_chunk = w.kv.chunk;
+  a.kv_qs = w.kv.qs;
   a.kv_splits = w.kv.splits;
   const hipError_t e = xattn_backward(a, s->dtype, (hipStream_t)hip_stream);
   if (e != hipSuccess) return bad(STAGE_EHIP, "attn_backward: %s", hipGetErrorString(e));

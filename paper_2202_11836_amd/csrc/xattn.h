@@ -26,9 +26,10 @@ struct XAttnArgs {
   int64_t sq[3], sk[3], sv[3], so[3], sdo[3], sdq[3], sdk[3], sdv[3];
   int B, Sq, Sk, H, G, rep;  // G key heads, rep = H / G query heads to each
   int causal;
-  int kv_chunk, kv_splits;   // XKvPlan
+  int kv_chunk, kv_splits, kv_qs;         // XKvPlan
   int few_waves, few_splits, few_stream;  // XFewPlan
-  int dq_ks, dq_splits;      // XDqPlan
+  int dq_ks, dq_splits;                   // XDqPlan
+  int fwd_ks;                             // xattn_fwd_time
   float c;      // scale * log2(e)
   float scale;
   // Buckets (attn_relpos): nb in all, nbd to a direction, `one` of them with one
@@ -38,12 +39,17 @@ struct XAttnArgs {
 };
 
 // How the dK / dV kernel goes through the query blocks (of XKvPlan::rows queries of
-// one head) that a block of 128 keys meets: `chunk` of them to a work-group, and with
-// splits > 1 each chunk's fp32 sums go to the workspace, [split][B, G][Sk][dK | dV].
+// one head) that a block of 128 / qs keys meets: `chunk` of them to a work-group, whose
+// wavefronts share 32 keys by qs (1 or 2), and with splits > 1 each chunk's fp32 sums go
+// to the workspace, [split][B, G][Sk][dK | dV].
 struct XKvPlan {
-  int rows, chunk, splits;
+  int rows, chunk, splits, qs;
 };
 XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_dtype dt);
+
+// About how long the forward kernel for many queries takes, in us, and by how many (1 or
+// 2) of its wavefronts 32 queries are shared.
+double xattn_fwd_time(int B, int H, int Sq, int Sk, int causal, stage_dtype dt, int* ks);
 
 // How the dQ kernel goes along the keys: ks wavefronts (1 or 2) of a work-group share
 // 32 queries, and `splits` work-groups the keys.  With several splits each leaves, per

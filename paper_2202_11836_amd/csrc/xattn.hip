@@ -96,26 +96,28 @@ __device__ __forceinline__ int x_start(const XAttnArgs& a, int b, const T* K, co
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
-template <typename T, bool BIAS>
+// KS = 2: two wavefronts share 32 queries, one with the first 32 keys of each block and
+// one with the others, and are joined at the end; a work-group has 64 queries then.
+template <typename T, bool BIAS, int KS>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(XAttnArgs a) {
-  constexpr int TILE = XKT * XT<T>::ROWB;
+  constexpr int TILE = XKT * XT<T>::ROWB, QB = XQB / KS, QW = 4 / KS;
   extern __shared__ __attribute__((aligned(1024))) char lds[];  // [2][K, V], dist
   float* dist = (float*)(lds + 4 * TILE);
 
   int qb, bh;
-  const int nq = (a.Sq + XQB - 1) / XQB;
+  const int nq = (a.Sq + QB - 1) / QB;
   x_block(a, blockIdx.x, gridDim.x, nq, qb, bh);
   if (a.causal) qb = nq - 1 - qb;
   const int b = bh / a.H, h = bh % a.H, g = h / a.rep;
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int q0 = qb * XQB + wave * 32;
+  const int q0 = qb * QB + wave % QW * 32, ks = wave / QW;
   const int qp = x_q_pos(a, b);
   const int p0 = q0 + qp;  // position of the wavefront's first query
   const T* K = (const T*)a.k + b * a.sk[0] + g * a.sk[2];
   const T* V = (const T*)a.v + b * a.sv[0] + g * a.sv[2];
   const int lim =
-      a.causal ? max(0, min(a.Sk, min(qb * XQB + XQB, a.Sq) + qp)) : a.Sk;
+      a.causal ? max(0, min(a.Sk, min(qb * QB + QB, a.Sq) + qp)) : a.Sk;
 
   const typename XT<T>::Frag qf =
       x_frag((const T*)a.q + b * a.sq[0] + (int64_t)(q0 + rr) * a.sq[1] + h * a.sq[2],
@@ -149,7 +151,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(
       __syncthreads();
     }
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
+    for (int i = 0; i < 2 / KS; ++i) {
+      const int sub = KS == 2 ? ks : i;
       const int k0 = kb * XKT + 32 * sub;
       const uint32_t rows = (uint32_t)(word >> (32 * sub));
       if (rows == 0 || q0 >= a.Sq || (a.causal && k0 > p0 + 31)) continue;
@@ -212,12 +215,32 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void xattn_fwd_kernel(
     kb = kn;
   }
   const HalfPair lp = half_pair(lsum);
-  const float ltot = lp.x + lp.y;
+  float ltot = lp.x + lp.y;
+  if constexpr (KS == 2) {
+    // [wavefront][output, offset, sum][lane], in the place of the ring
+    float* p = (float*)lds + wave % QW * 34 * 64 + lane;
+    __syncthreads();
+    if (ks == 1) {
+#pragma unroll
+      for (int r = 0; r < 32; ++r) p[r * 64] = acc[r >> 4][r & 15];
+      p[32 * 64] = m;
+      p[33 * 64] = ltot;
+    }
+    __syncthreads();
+    if (ks == 1) return;
+    const float m1 = p[32 * 64], top = fmaxf(m, m1), off = top == -INFINITY ? 0.0f : top;
+    const float f0 = __builtin_amdgcn_exp2f(m - off), f1 = __builtin_amdgcn_exp2f(m1 - off);
+#pragma unroll
+    for (int r = 0; r < 32; ++r)
+      acc[r >> 4][r & 15] = fmaf(p[r * 64], f1, acc[r >> 4][r & 15] * f0);
+    ltot = fmaf(p[33 * 64], f1, ltot * f0);
+    m = top;
+  }
   if (a.lse && hf == 0 && q0 + rr < a.Sq)
     a.lse[((int64_t)b * a.H + h) * a.Sq + q0 + rr] =
         ltot == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(ltot)) * XLN2;
-  __syncthreads();  // the ring becomes the output staging area
-  x_store<T>(acc, ltot == 0.0f ? 0.0f : 1.0f / ltot, (T*)lds + wave * 32 * XT<T>::LD,
+  if constexpr (KS == 1) __syncthreads();  // the ring becomes the output staging area
+  x_store<T>(acc, ltot == 0.0f ? 0.0f : 1.0f / ltot, (T*)(lds + (KS == 2 ? 2 * 34 * 256 : 0)) + wave * 32 * XT<T>::LD,
              (T*)a.out + b * a.so[0] + h * a.so[2], a.so[1], q0, a.Sq);
 }
 
@@ -599,9 +622,11 @@ __device__ __forceinline__ void x_dtable_sum(const XAttnArgs& a, int w, float* r
   if (threadIdx.x == 0) a.dtable[(int64_t)c * a.H + h] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-template <typename T, bool BIAS>
+// QS = 2: two wavefronts share 32 keys, each with every other tile of queries, and add
+// up at the end; a work-group has 64 keys then.
+template <typename T, bool BIAS, int QS>
 __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_kv) {
-  constexpr int QB = x_qb<T>(), TILE = QB * XT<T>::ROWB;
+  constexpr int QB = x_qb<T>(), TILE = QB * XT<T>::ROWB, KB = XQB / QS, KW = 4 / QS;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   float* rowv = (float*)(lds + 4 * TILE);
   float* dist = (float*)(lds + kv_lds<T>());
@@ -612,14 +637,14 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int kblk, bg;
-  x_block(a, blockIdx.x, n_kv, (a.Sk + XQB - 1) / XQB * a.kv_splits, kblk, bg);
+  x_block(a, blockIdx.x, n_kv, (a.Sk + KB - 1) / KB * a.kv_splits, kblk, bg);
   const int split = kblk % a.kv_splits;
   kblk /= a.kv_splits;
   const int b = bg / a.G, g = bg % a.G;
-  const int k0 = kblk * XQB + wave * 32, key = k0 + rr;
+  const int k0 = kblk * KB + wave % KW * 32, key = k0 + rr, qs = wave / KW;
   const int qp = x_q_pos(a, b);
   // Queries from q_first on see a key of this work-group, those before it none.
-  const int q_first = a.causal ? max(0, kblk * XQB - qp) : 0;
+  const int q_first = a.causal ? max(0, kblk * KB - qp) : 0;
   const int qb0 = q_first / QB, nqb = max(0, (a.Sq + QB - 1) / QB - qb0);
   const int it0 = split * a.kv_chunk;
   int n_it = min(nqb * a.rep, it0 + a.kv_chunk);
@@ -695,16 +720,17 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
     const char* dOs = Qs + TILE;
     const float* lv = rowv + st * 2 * QB;
 #pragma unroll
-    for (int sub = 0; sub < QB / 32; ++sub) {
+    for (int i = 0; i < QB / 32 / QS; ++i) {
+      const int sub = QS == 2 ? 2 * i + qs : i;
       const int r0 = qr + 32 * sub;   // first query
       const int p0 = r0 + qp;         // its position
       if (!any_valid || r0 >= a.Sq || (a.causal && k0 > p0 + 31)) continue;
       f32x16_t dp;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4_t d4 = *(const f32x4_t*)(lv + QB + 32 * sub + 8 * i + 4 * hf);
+      for (int j = 0; j < 4; ++j) {
+        const f32x4_t d4 = *(const f32x4_t*)(lv + QB + 32 * sub + 8 * j + 4 * hf);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) dp[4 * i + e] = d4[e];
+        for (int e = 0; e < 4; ++e) dp[4 * j + e] = d4[e];
       }
       f32x16_t s = x_mma_rows(Qs, 32 * sub, kf, zero16(), lane);
       dp = x_mma_rows(dOs, 32 * sub, vf, dp, lane);
@@ -724,12 +750,12 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
         for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, far);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4_t l4 = *(const f32x4_t*)(lv + 32 * sub + 8 * i + 4 * hf);
+      for (int j = 0; j < 4; ++j) {
+        const f32x4_t l4 = *(const f32x4_t*)(lv + 32 * sub + 8 * j + 4 * hf);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float x = s[4 * i + e];
-          s[4 * i + e] = __builtin_amdgcn_exp2f(BIAS ? x - l4[e] : fmaf(x, a.c, -l4[e]));
+          const float x = s[4 * j + e];
+          s[4 * j + e] = __builtin_amdgcn_exp2f(BIAS ? x - l4[e] : fmaf(x, a.c, -l4[e]));
         }
       }
       if (!full) {
@@ -745,6 +771,27 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
     raw = raw2;
   }
   __syncthreads();  // the ring becomes the output staging area
+  if constexpr (QS == 2) {
+    // [wavefront][dK, dV][register][lane]
+    float* p = (float*)lds + wave % KW * 64 * 64 + lane;
+    if (qs == 1) {
+#pragma unroll
+      for (int r = 0; r < 32; ++r) {
+        p[r * 64] = dk[r >> 4][r & 15];
+        p[(32 + r) * 64] = dv[r >> 4][r & 15];
+      }
+    }
+    __syncthreads();
+    if (qs == 0) {
+#pragma unroll
+      for (int r = 0; r < 32; ++r) {
+        dk[r >> 4][r & 15] += p[r * 64];
+        dv[r >> 4][r & 15] += p[(32 + r) * 64];
+      }
+    }
+    __syncthreads();
+    if (qs == 1) return;
+  }
   if (a.kv_splits > 1) {
     float* to = a.part + ((int64_t)split * a.B * a.G + bg) * a.Sk * 2 * XHD;
     float* stage = (float*)lds + wave * 32 * XT<float>::LD;
@@ -770,7 +817,8 @@ __global__ __launch_bounds__(256) void xattn_kv_sum_kernel(XAttnArgs a) {
   const int key = (int)(row % a.Sk), bg = (int)(row / a.Sk), b = bg / a.G, g = bg % a.G;
   const int c = (threadIdx.x & 31) * 4;
   const int qp = x_q_pos(a, b);
-  const int q_first = a.causal ? max(0, key / XQB * XQB - qp) : 0;
+  const int kb = XQB / a.kv_qs;
+  const int q_first = a.causal ? max(0, key / kb * kb - qp) : 0;
   const int n_it = max(0, (a.Sq + QB - 1) / QB - q_first / QB) * a.rep;
   const int splits = max(1, (n_it + a.kv_chunk - 1) / a.kv_chunk);
   f32x4_t t = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -797,11 +845,16 @@ size_t dist_bytes(const XAttnArgs& a) {
 template <typename T>
 hipError_t forward_t(const XAttnArgs& a, hipStream_t st) {
   if (a.few_splits > 0) return xattn_few(a, sizeof(T) == 2 ? STAGE_BF16 : STAGE_F32, st);
-  const int64_t grid = (int64_t)a.B * a.H * ((a.Sq + XQB - 1) / XQB);
+  constexpr int KS2 = sizeof(T) == 4 ? 2 : 1;
+  const int qb = XQB / a.fwd_ks;
+  const int64_t grid = (int64_t)a.B * a.H * ((a.Sq + qb - 1) / qb);
   const size_t lds = 4 * XKT * XT<T>::ROWB + dist_bytes(a);
   if (grid == 0) return hipSuccess;
-  return a.table ? launch(xattn_fwd_kernel<T, true>, grid, lds, st, a)
-                 : launch(xattn_fwd_kernel<T, false>, grid, lds, st, a);
+  if (a.fwd_ks == 1)
+    return a.table ? launch(xattn_fwd_kernel<T, true, 1>, grid, lds, st, a)
+                   : launch(xattn_fwd_kernel<T, false, 1>, grid, lds, st, a);
+  return a.table ? launch(xattn_fwd_kernel<T, true, KS2>, grid, lds, st, a)
+                 : launch(xattn_fwd_kernel<T, false, KS2>, grid, lds, st, a);
 }
 
 template <typename T>
@@ -828,15 +881,24 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
       e = launch(xattn_dq_sum_kernel<T>, ((int64_t)a.B * a.H * a.Sq + 15) / 16, 0, st, a);
     if (e != hipSuccess) return e;
   }
-  const int64_t n_kv = (int64_t)a.B * a.G * ((a.Sk + XQB - 1) / XQB) * a.kv_splits;
+  const int kb = XQB / a.kv_qs;
+  const int64_t n_kv = (int64_t)a.B * a.G * ((a.Sk + kb - 1) / kb) * a.kv_splits;
   const int64_t n_red = a.dtable ? (int64_t)a.nb * a.H : 0;
   if (n_kv + n_red == 0) return e;
   const size_t lds = kv_lds<T>() + dist_bytes(a);
   const dim3 grid((unsigned)(n_kv + n_red));
-  if (a.table)
-    hipLaunchKernelGGL((xattn_dkdv_kernel<T, true>), grid, dim3(256), lds, st, a, (int)n_kv);
-  else
-    hipLaunchKernelGGL((xattn_dkdv_kernel<T, false>), grid, dim3(256), lds, st, a, (int)n_kv);
+  constexpr int QS2 = sizeof(T) == 4 ? 2 : 1;
+  if (a.kv_qs == 1) {
+    if (a.table)
+      hipLaunchKernelGGL((xattn_dkdv_kernel<T, true, 1>), grid, dim3(256), lds, st, a, (int)n_kv);
+    else
+      hipLaunchKernelGGL((xattn_dkdv_kernel<T, false, 1>), grid, dim3(256), lds, st, a, (int)n_kv);
+  } else {
+    if (a.table)
+      hipLaunchKernelGGL((xattn_dkdv_kernel<T, true, QS2>), grid, dim3(256), lds, st, a, (int)n_kv);
+    else
+      hipLaunchKernelGGL((xattn_dkdv_kernel<T, false, QS2>), grid, dim3(256), lds, st, a, (int)n_kv);
+  }
   if ((e = hipGetLastError()) != hipSuccess || a.kv_splits == 1) return e;
   return launch(xattn_kv_sum_kernel<T>, ((int64_t)a.B * a.G * a.Sk + 7) / 8, 0, st, a);
 }
@@ -874,19 +936,54 @@ XDqPlan xattn_dq_plan(int B, int H, int Sq, int Sk, int causal, bool bias, stage
   return {ks, splits};
 }
 
+// bf16: see xattn_few_plan.  fp32, fitted to 60 launches of 1 to 32 x 8 to 16 heads with 32
+// to 512 queries and keys: 4 x 8 heads of 512 44 us with a wavefront to 32 queries, 28
+// with two, 8 x 12 of 300 50 and 31, 8 x 12 of 128 13.4 and 10.4; 16 x 12 of 512, where
+// every CU has several work-groups, 115 and 124.  (Under `causal` the shares of a
+// work-group's rows differ, which the smaller ones even out.)
+double xattn_fwd_time(int B, int H, int Sq, int Sk, int causal, stage_dtype dt, int* ks) {
+  const double cus = device_cus(), blocks = (Sk + XKT - 1) / XKT;
+  const double n1 = (double)B * H * ((Sq + XQB - 1) / XQB);
+  *ks = 1;
+  if (dt == STAGE_BF16) {
+    const double at_once = std::min(4.0, std::ceil(n1 / cus));
+    return std::ceil(n1 / (4 * cus)) * (2.1 + blocks * (1.15 + 0.63 * (at_once - 1)));
+  }
+  const double n2 = (double)B * H * ((Sq + XQB / 2 - 1) / (XQB / 2));
+  const double t1 = (3.5 + 5.05 * blocks) * (0.18 + 0.82 * std::ceil(n1 / cus));
+  const double t2 = (3.7 + 3.05 * blocks) * (0.3 + 0.7 * std::ceil(n2 / cus));
+  if (t2 * (causal ? 0.78 : 1.0) < 0.93 * t1) *ks = 2;
+  return std::min(t1, t2);
+}
+
 XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_dtype dt) {
   const int rows = dt == STAGE_BF16 ? x_qb<bf16_t>() : x_qb<float>();
   const int64_t its = (int64_t)((Sq + rows - 1) / rows) * rep;
   const int64_t wgs = (int64_t)B * G * ((Sk + XQB - 1) / XQB);
-  const int64_t slots = 2 * device_cus();
+  const int64_t cus = device_cus(), slots = 2 * cus;
+  XKvPlan plan = {rows, (int)std::max<int64_t>(its, 1), 1, 1};
   // The sum of the splits is a launch and a pass over them (5 us and more), a block of
   // queries 3 us: 1 x 4 key heads of 4 x 2500 queries and 2500 keys 369 us in one piece
   // (80 work-groups), 96 + 8 in chunks; 8 x 12 heads of 128 (two blocks, fp32) 29 and
   // 22 + 5.
-  if (wgs * 2 > slots || wgs == 0 || its < 4) return {rows, (int)std::max<int64_t>(its, 1), 1};
-  const int64_t all = wgs * its / (causal ? 2 : 1);
-  const int64_t chunk = std::max<int64_t>((all + slots - 1) / slots, 1);
-  return {rows, (int)chunk, (int)((its + chunk - 1) / chunk)};
+  if (wgs * 2 <= slots && wgs > 0 && its >= 4) {
+    const int64_t all = wgs * its / (causal ? 2 : 1);
+    const int64_t chunk = std::max<int64_t>((all + slots - 1) / slots, 1);
+    plan = {rows, (int)chunk, (int)((its + chunk - 1) / chunk), 1};
+  }
+  // fp32: half as many keys to a work-group, two wavefronts to 32 of them, where that
+  // leaves at most two to a CU.  us by work-groups per CU and blocks of queries, fitted
+  // to 60 launches: 8 x 12 heads of 128 24 -> 18.7, of 300 90 -> 61, 8 x 8 of 300 (else in
+  // 3 chunks) 61 -> 58; 16 x 12 of 128 25 -> 33, 16 x 12 of 512 209 -> 249.  (bf16: no
+  // gain for few work-groups, 84 -> 106 at 32 x 12 of 512.)
+  const int64_t halves = (int64_t)B * G * ((Sk + XQB / 2 - 1) / (XQB / 2));
+  if (dt == STAGE_F32 && wgs > 0 && Sq > 32 && halves <= slots) {
+    const int64_t n = wgs * plan.splits;
+    const double t1 = (5.0 + 8.1 * plan.chunk) * ((n + cus - 1) / cus) + (plan.splits > 1 ? 6.0 : 0.0);
+    const double t2 = halves <= cus ? 5.0 + 6.5 * its : 2.0 * (6.0 + 4.6 * its);
+    if (t2 < t1) plan = {rows, (int)std::max<int64_t>(its, 1), 1, 2};
+  }
+  return plan;
 }
 
 hipError_t xattn_forward(const XAttnArgs& a, stage_dtype dt, hipStream_t st) {

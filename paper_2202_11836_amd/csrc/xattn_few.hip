@@ -359,10 +359,8 @@ XFewPlan xattn_few_plan(int B, int G, int rep, int Sq, int Sk, int buckets, int 
   // (the model is one of few work-groups: 16 heads of 2500 queries are 1250 tiles and
   // take 60 us with the other kernel, 75 with this one)
   if (tiles == 0.0 || tiles > (bf16 ? 4 : 1) * cus) return {0, 0, 0};
-  const double other = (double)B * G * rep * ((Sq + 127) / 128);
-  const double cap = bf16 ? 4 : 2, at_once = std::min(cap, std::ceil(other / cus));
-  double best = std::ceil(other / (cap * cus)) *
-                (2.1 + (Sk + 63) / 64 * (bf16 ? 1.15 + 0.63 * (at_once - 1) : 4.9 + 4.5 * (at_once - 1)));
+  int ks;
+  double best = xattn_fwd_time(B, G * rep, Sq, Sk, 0, dt, &ks);
   // No faster than the memory: of several that are bound by it, the fewest
   // wavefronts (16 x 16 heads over 8192 keys: 97 us with 4, 112 with 8).
   const double floor = 2.0 + 2.0 * B * G * (double)Sk * (bf16 ? 128 : 256) / 5.2e6;

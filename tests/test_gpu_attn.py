@@ -163,6 +163,18 @@ def test_tokens(dtype, sq, sk, heads, kv, relpos):
     run(dtype, 2, heads, kv, sq, sk, mask="empty", relpos=relpos, backward=False)
 
 
+# (more tiles than the kernel for few queries takes, fewer work-groups than CUs: fp32
+# wavefronts share their queries, and their keys)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(2, 16, 8, 300, 130), (3, 12, 12, 257, 64), (9, 8, 8, 130, 33)])
+@pytest.mark.parametrize("mask,garbage", [("none", False), ("empty", True), ("blocks", True),
+                                          ("last", False), ("holes", True)])
+@pytest.mark.parametrize("causal,relpos", [(False, None), (True, (32, 128, False)),
+                                           (False, (16, 40, True))])
+def test_shared_work(dtype, shape, mask, garbage, causal, relpos):
+    run(dtype, *shape, mask=mask, garbage=garbage, causal=causal, relpos=relpos)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_no_queries_no_keys_no_batch(dtype):
     rp, dt = P.RelPos(8, 20), DT[dtype]
