@@ -67,6 +67,7 @@ class _RelPos(ctypes.Structure):  # attn_relpos
 # attn_shape: dtype, batch, seq_q, seq_k, heads, kv_heads, causal, scale and the
 # strides of q, k, v, out, dout, dq, dk, dv
 _ATTN_SHAPE = struct.Struct("@7if24q")
+_ATTN_FORWARD_SHAPE = struct.Struct("@7if12q96x")  # (no gradients)
 
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -575,16 +576,16 @@ class RelPos:
 
 def _attn_strides(name, t, shape, dtype, dev):
     """Batch, position and head stride of an operand of this shape, type and device."""
-    if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
+    s = t.stride()
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
         _refuse(f"{name} must be {dtype} {tuple(shape)} on cuda:{dev}")
-    b, p, h, one = t.stride()
-    if one != 1:
+    if s[3] != 1:
         _refuse(f"the 64 values of a head of {name} must lie side by side")
-    return b, p, h
+    return s[:3]
 
 
 def _attn_plain(name, t, shape, dtype, dev):
-    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
         _refuse(f"{name} must be contiguous {dtype} {tuple(shape)} on cuda:{dev}")
     return t.data_ptr()
 
@@ -594,16 +595,19 @@ def _attn_inputs(q, k, v, key_mask, scale, causal, q_pos, relpos, table):
     the head of the packed attn_shape (up to the strides of v) and the arguments from
     rp to q_pos."""
     import torch
-    dtype = q.dtype
-    code = STAGE_BF16 if dtype == torch.bfloat16 else STAGE_F32
-    dev = q.get_device()
-    if code == STAGE_F32 and dtype != torch.float32:
+    dtype, dev, q_shape, kv_shape = q.dtype, q.get_device(), q.shape, k.shape
+    if dtype is torch.bfloat16:
+        code = STAGE_BF16
+    elif dtype is torch.float32:
+        code = STAGE_F32
+    else:
         _refuse("q must be bfloat16 or float32")
-    if q.dim() != 4 or k.dim() != 4 or q.shape[3] != 64 or dev < 0:
+    if len(q_shape) != 4 or len(kv_shape) != 4 or q_shape[3] != 64 or dev < 0:
         _refuse("q, k, v must be [batch, length, heads, 64] on a GPU")
-    B, Sq, H, _ = q_shape = q.shape
-    Sk, G = k.shape[1], k.shape[2]
-    kv_shape = (B, Sk, G, 64)
+    B, Sq, H, D = q_shape
+    _, Sk, G, _ = kv_shape
+    if kv_shape[0] != B or kv_shape[3] != D:
+        _refuse(f"k must be [{B}, {Sk}, {G}, {D}]")
     if (relpos is None) != (table is None):
         _refuse("relpos and table go together")
     rp = tab = mask = pos = None
@@ -626,15 +630,18 @@ def _attn_call(fn, shape, args, backward, dev):
     stream.  The workspace comes from torch's allocator, which gives no memory of a
     stream (or of a captured graph) away while work on it may still use it."""
     import torch
-    lib = load_library()
-    n = ctypes.c_size_t()
     if torch._C._cuda_getDevice() != dev:
         with torch.cuda.device(dev):
             return _attn_call(fn, shape, args, backward, dev)
-    _attn_check(lib.attn_workspace(shape, args[0], backward, ctypes.byref(n)))
-    ws = torch.empty(n.value, dtype=torch.uint8, device=dev) if n.value else None
-    stream = torch._C._cuda_getCurrentRawStream(dev)
-    _attn_check(fn(shape, *args, None if ws is None else ws.data_ptr(), n.value, stream))
+    n = ctypes.c_size_t()
+    _attn_check(_lib.attn_workspace(shape, args[0], backward, ctypes.byref(n)))
+    n, ws, ptr = n.value, None, None
+    if n:
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        ptr = ws.data_ptr()
+    status = fn(shape, *args, ptr, n, torch._C._cuda_getCurrentRawStream(dev))
+    if status:
+        _attn_check(status)
 
 
 def attn_forward(q, k, v, key_mask=None, scale=None, causal=False, q_pos=None, relpos=None,
@@ -654,16 +661,16 @@ def attn_forward(q, k, v, key_mask=None, scale=None, causal=False, q_pos=None, r
     A query without a key gets zeros and lse = -inf.  Runs on the current stream
     of q's device."""
     import torch
+    fn = load_library().attn_forward
     shape, _, dev, head, args = _attn_inputs(q, k, v, key_mask, scale, causal, q_pos, relpos, table)
-    B, Sq, H, _ = shape
+    rows = (shape[0], shape[2], shape[1])
     if out is None:
-        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(shape)
     if lse is None:
-        lse = torch.empty((B, H, Sq), dtype=torch.float32, device=q.device)
-    packed = _ATTN_SHAPE.pack(*head, *_attn_strides("out", out, shape, q.dtype, dev), *(0,) * 12)
-    _attn_call(load_library().attn_forward, packed,
-               (*args, out.data_ptr(), _attn_plain("lse", lse, (B, H, Sq), torch.float32, dev)), 0,
-               dev)
+        lse = q.new_empty(rows, dtype=torch.float32)
+    packed = _ATTN_FORWARD_SHAPE.pack(*head, *_attn_strides("out", out, shape, q.dtype, dev))
+    _attn_call(fn, packed,
+               (*args, out.data_ptr(), _attn_plain("lse", lse, rows, torch.float32, dev)), 0, dev)
     return out, lse
 
 
@@ -672,16 +679,17 @@ def attn_backward(q, k, v, out, lse, dout, key_mask=None, scale=None, causal=Fal
     """Gradients of <out, dout> for attn_forward's arguments, out and lse: returns
     dq, dk, dv and dtable (None without a table), written where given."""
     import torch
+    fn = load_library().attn_backward
     q_shape, kv_shape, dev, head, args = _attn_inputs(q, k, v, key_mask, scale, causal, q_pos,
                                                       relpos, table)
     B, Sq, H, _ = q_shape
     dtype = q.dtype
     if dq is None:
-        dq = torch.empty(q_shape, dtype=dtype, device=q.device)
+        dq = q.new_empty(q_shape)
     if dk is None:
-        dk = torch.empty(kv_shape, dtype=dtype, device=q.device)
+        dk = q.new_empty(kv_shape)
     if dv is None:
-        dv = torch.empty(kv_shape, dtype=dtype, device=q.device)
+        dv = q.new_empty(kv_shape)
     if table is None and dtable is not None:
         _refuse("dtable without a table")
     if table is not None and dtable is None:
@@ -692,7 +700,7 @@ def attn_backward(q, k, v, out, lse, dout, key_mask=None, scale=None, causal=Fal
                               *_attn_strides("dk", dk, kv_shape, dtype, dev),
                               *_attn_strides("dv", dv, kv_shape, dtype, dev))
     to = None if dtable is None else _attn_plain("dtable", dtable, table.shape, torch.float32, dev)
-    _attn_call(load_library().attn_backward, packed,
+    _attn_call(fn, packed,
                (*args, out.data_ptr(), _attn_plain("lse", lse, (B, H, Sq), torch.float32, dev),
                 dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), to), 1, dev)
     return dq, dk, dv, dtable
