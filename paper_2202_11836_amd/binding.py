@@ -608,6 +608,10 @@ def _attn_inputs(q, k, v, key_mask, scale, causal, q_pos, relpos, table):
     _, Sk, G, _ = kv_shape
     if kv_shape[0] != B or kv_shape[3] != D:
         _refuse(f"k must be [{B}, {Sk}, {G}, {D}]")
+    if scale is None:
+        scale = 0.125
+    elif not 0.0 < scale < 3e38:
+        _refuse("scale must be finite and positive")
     if (relpos is None) != (table is None):
         _refuse("relpos and table go together")
     rp = tab = mask = pos = None
@@ -617,7 +621,7 @@ def _attn_inputs(q, k, v, key_mask, scale, causal, q_pos, relpos, table):
         mask = _attn_plain("key_mask", key_mask, (B, Sk), torch.uint8, dev)
     if q_pos is not None:
         pos = _attn_plain("q_pos", q_pos, (B,), torch.int32, dev)
-    head = (code, B, Sq, Sk, H, G, 1 if causal else 0, 0.125 if scale is None else scale,
+    head = (code, B, Sq, Sk, H, G, 1 if causal else 0, scale,
             *_attn_strides("q", q, q_shape, dtype, dev),
             *_attn_strides("k", k, kv_shape, dtype, dev),
             *_attn_strides("v", v, kv_shape, dtype, dev))

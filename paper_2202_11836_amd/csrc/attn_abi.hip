@@ -151,6 +151,8 @@ stage_status check_operand(const char* name, const void* p, const int64_t* given
     if (st[i] < 0) return bad(STAGE_EINVAL, "%s has a negative stride", name);
     if (st[i] > (int64_t)1 << 53 || st[i] * esz % 16)
       return bad(STAGE_EINVAL, "a stride of %s is not a multiple of 16 bytes", name);
+    if (size[i] > 1 && st[i] > ((int64_t)1 << 53) / (size[i] - 1))
+      return bad(STAGE_EINVAL, "%s spans more than 2^53 elements", name);
   }
   if (st[1] * esz >= 1 << 24) return bad(STAGE_EINVAL, "positions of %s lie 16 MiB or more apart", name);
   if (output) {

@@ -1642,7 +1642,7 @@ stage_status stage_backward_noalloc(stage_t* s, const void* dy, void* dx) {
   return st;
 }
 
-stage_status stage_set_relpos(stage_t* s, int num_buckets, int max_distance) {
+stage_status stage_set_relpos(stage_t* s, int num_buckets, int max_distance) try {
   if (!s) return STAGE_EINVAL;
   s->err.clear();
   attn_relpos rp{};
@@ -1679,6 +1679,8 @@ stage_status stage_set_relpos(stage_t* s, int num_buckets, int max_distance) {
   HIPCK(hipGetLastError());
   s->relpos = true;
   return STAGE_OK;
+} catch (const std::bad_alloc&) {
+  return STAGE_ENOMEM;  // (of host memory)
 }
 
 stage_status stage_relpos(stage_t* s, float** table, float** grad, int64_t* numel) {
@@ -1691,7 +1693,7 @@ stage_status stage_relpos(stage_t* s, float** table, float** grad, int64_t* nume
 }
 
 stage_status stage_forward_cross(stage_t* s, const void* x, const void* memory, const uint8_t* key_mask,
-                                 int batch, int seq, int mem_seq, void* y) {
+                                 int batch, int seq, int mem_seq, void* y) try {
   if (!s) return STAGE_EINVAL;
   s->err.clear();
   if (s->L != 1 || s->ffn_first || !s->attn_last)
@@ -1728,9 +1730,11 @@ stage_status stage_forward_cross(stage_t* s, const void* x, const void* memory, 
   }
   s->have_ctx = true;
   return STAGE_OK;
+} catch (const std::bad_alloc&) {
+  return STAGE_ENOMEM;  // (of host memory)
 }
 
-stage_status stage_backward_cross(stage_t* s, const void* dy, void* dx, void* dmemory) {
+stage_status stage_backward_cross(stage_t* s, const void* dy, void* dx, void* dmemory) try {
   if (!s) return STAGE_EINVAL;
   s->err.clear();
   if (!s->have_ctx || !s->cross)
@@ -1754,6 +1758,8 @@ stage_status stage_backward_cross(stage_t* s, const void* dy, void* dx, void* dm
           : backward_cross_impl<float>(s, (const float*)dy, (float*)dx, (float*)dmemory);
   s->rec_valid = st == STAGE_OK && s->record_grads && (int)s->rec.size() == s->L;
   return st;
+} catch (const std::bad_alloc&) {
+  return STAGE_ENOMEM;  // (of host memory)
 }
 
 stage_status stage_param(stage_t* s, int layer, int which, void** dev_ptr, int64_t* numel,

@@ -175,3 +175,13 @@ def test_binding_refuses_cpu_tensors_and_wrong_types():
     for a in ((q, q, q), (q.half(), q, q), (q[..., :32], q, q), (q[0], q, q)):
         with pytest.raises(P.StageError):
             P.attn_forward(*a)
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "out"])
+def test_spans_beyond_any_memory_refused(name):
+    """Strides that pass one by one, over so many sequences that their product would not."""
+    inner = (256, 64) if name in ("q", "out") else (128, 64)
+    st, msg = call(0, shape(batch=5000, **{name: (1 << 51, *inner)}))
+    assert st == 1 and "spans" in msg
+    st, msg = call(1, shape(batch=5000, **{"dq" if name == "out" else name: (1 << 52, *inner)}))
+    assert st == 1 and "spans" in msg

@@ -352,3 +352,11 @@ def test_binding_refusals():
         P.attn_backward(q, k, v, out, lse, q, dk=torch.empty((1, 7, 2, 64), device="cuda").expand(2, 7, 2, 64))
     with pytest.raises(StageError):
         P.attn_backward(q, k, v, out, lse, q, dq=out)
+
+
+def test_scales_beyond_fp32_refused():
+    q = rand((1, 2, 1, 64), 1)
+    for scale in (1e39, float("inf"), -0.5):
+        with pytest.raises(StageError) as e:
+            P.attn_forward(q, q, q, scale=scale)
+        assert e.value.status == 1
