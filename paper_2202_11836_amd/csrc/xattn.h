@@ -30,6 +30,7 @@ struct XAttnArgs {
   int few_waves, few_splits, few_stream;  // XFewPlan
   int dq_ks, dq_splits;                   // XDqPlan
   int fwd_ks;                             // xattn_fwd_time
+  int one_launch;                         // xattn_one_launch
   float c;      // scale * log2(e)
   float scale;
   // Buckets (attn_relpos): nb in all, nbd to a direction, `one` of them with one
@@ -59,6 +60,9 @@ struct XDqPlan {
   int ks, splits;
 };
 XDqPlan xattn_dq_plan(int B, int H, int Sq, int Sk, int causal, bool bias, stage_dtype dt);
+// Whether one kernel makes all of a backward's results.
+int xattn_one_launch(int B, int H, int G, int Sq, int Sk, bool bias, const XDqPlan& dq,
+                     const XKvPlan& kv, stage_dtype dt);
 inline int xattn_dq_row(stage_dtype dt) { return dt == STAGE_BF16 ? 132 : 64; }
 
 // The forward kernel that serves few queries (xattn_few.hip): wavefronts of a

@@ -310,9 +310,8 @@ __device__ __forceinline__ void x_add_buckets(const XAttnArgs& a, float v, int r
 // KS = 2: two wavefronts share 32 queries, one with the first 32 keys of each block
 // and one with the others, and add up at the end; a work-group has 64 queries then.
 template <typename T, bool BIAS, bool RED, int KS>
-__global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a) {
+__device__ __forceinline__ void x_dq(const XAttnArgs& a, int w, int n, char* lds) {
   constexpr int TILE = XKT * XT<T>::ROWB, QB = XQB / KS, QW = 4 / KS;
-  extern __shared__ __attribute__((aligned(1024))) char lds[];
   // [2][K, V]; with a bias: dist, the wavefronts' sums by distance [4][nd] and by
   // bucket [4][nb]
   constexpr bool FIX = sizeof(T) == 2 && !RED;
@@ -330,7 +329,7 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
 
   int qb, bh;
   const int nq = (a.Sq + QB - 1) / QB;
-  x_block(a, blockIdx.x, gridDim.x, nq * a.dq_splits, qb, bh);
+  x_block(a, w, n, nq * a.dq_splits, qb, bh);
   const int split = qb % a.dq_splits;
   qb /= a.dq_splits;
   if (a.causal) qb = nq - 1 - qb;
@@ -567,6 +566,11 @@ __global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a)
     x_store<T>(dq, a.scale, (T*)lds + wave * 32 * XT<T>::LD,
                (T*)a.dq + b * a.sdq[0] + h * a.sdq[2], a.sdq[1], q0, a.Sq);
 }
+template <typename T, bool BIAS, bool RED, int KS>
+__global__ __launch_bounds__(256, RED ? 3 : 2) void xattn_dq_kernel(XAttnArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  x_dq<T, BIAS, RED, KS>(a, blockIdx.x, gridDim.x, lds);
+}
 
 // dQ and D from the splits, in order: 16 threads to a query, 4 columns each.
 template <typename T>
@@ -605,6 +609,7 @@ __global__ __launch_bounds__(256) void xattn_dq_sum_kernel(XAttnArgs a) {
 // gradient: one per bucket and head.
 // ---------------------------------------------------------------------------
 template <typename T> constexpr int x_qb() { return sizeof(T) == 2 ? 128 : 64; }
+constexpr int XOWN = 256;  // most queries (of all heads of a key head) whose D a work-group forms
 // LDS: [2][Q, dO], per stage lse and -D of QB rows, a word per wavefront; with a bias
 // its table by distance follows.
 template <typename T> constexpr int kv_lds() {
@@ -622,22 +627,94 @@ __device__ __forceinline__ void x_dtable_sum(const XAttnArgs& a, int w, float* r
   if (threadIdx.x == 0) a.dtable[(int64_t)c * a.H + h] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
+// D of the x_qb<T>() queries of head h from q0 on, into own (0 behind the last): fp32
+// rowsum(dO * out); bf16 sum(P dP) / sum(P) over all keys, since out's rounding would go
+// into dK (9 queries over 17 keys: its error 1.6 times that of fp32 sums rounded once).
+template <typename T>
+__device__ __forceinline__ void x_own_d(const XAttnArgs& a, int b, int g, int h, int q0, int qp,
+                                        char* ring, float* own, int wave, int lane) {
+  constexpr int QB = x_qb<T>(), TILE = XKT * XT<T>::ROWB;
+  const int hf = lane >> 5, rr = lane & 31, w0 = q0 + 32 * wave, q = w0 + rr;
+  const bool qv = q < a.Sq && 32 * wave < QB;
+  const typename XT<T>::Frag dof = x_frag(
+      (const T*)a.dout + b * a.sdo[0] + (int64_t)q * a.sdo[1] + h * a.sdo[2], qv, hf);
+  float D = 0.0f;
+  if constexpr (sizeof(T) == 4) {
+    const typename XT<T>::Frag of = x_frag(
+        (const T*)a.o + b * a.so[0] + (int64_t)q * a.so[1] + h * a.so[2], qv, hf);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) D += dof.f[i][e] * of.f[i][e];
+    const HalfPair pr = half_pair(D);
+    D = pr.x + pr.y;
+  } else {
+    const T* K = (const T*)a.k + b * a.sk[0] + g * a.sk[2];
+    const T* V = (const T*)a.v + b * a.sv[0] + g * a.sv[2];
+    const int p0 = w0 + qp;
+    const int lim = a.causal ? max(0, min(a.Sk, min(q0 + QB, a.Sq) + qp)) : a.Sk;
+    const typename XT<T>::Frag qf = x_frag(
+        (const T*)a.q + b * a.sq[0] + (int64_t)q * a.sq[1] + h * a.sq[2], qv, hf);
+    float lse2 = qv ? a.lse[((int64_t)b * a.H + h) * a.Sq + q] * XLOG2E : 0.0f;
+    if (lse2 == -INFINITY) lse2 = INFINITY;
+    KeyBlocks<XKT> blocks;
+    int kb = x_start(a, b, K, V, lim, 0, (lim + XKT - 1) / XKT, ring, wave, lane, blocks);
+    float rsum = 0.0f;
+    for (int st = 0; kb < blocks.nblk; st ^= 1) {
+      const uint64_t word = blocks.word(kb);
+      const uint64_t hidden = blocks.in_range(kb) & ~word;
+      const int kn = blocks.next(kb + 1);
+      wait_all();
+      __syncthreads();
+      char* kv = ring + st * 2 * TILE;
+      if (kn < blocks.nblk) {
+        char* nkv = ring + (st ^ 1) * 2 * TILE;
+        x_dma<T, XKT, 4>(K, a.sk[1], kn * XKT, lim, nkv, wave, lane);
+        x_dma<T, XKT, 4>(V, a.sv[1], kn * XKT, lim, nkv + TILE, wave, lane);
+      }
+      if (hidden) {
+        x_clear_hidden<T>(kv, word);
+        __syncthreads();
+      }
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const int k0 = kb * XKT + 32 * sub;
+        const uint32_t rows = (uint32_t)(word >> (32 * sub));
+        if (rows == 0 || w0 >= a.Sq || (a.causal && k0 > p0 + 31)) continue;
+        f32x16_t s = x_mma_rows(kv, 32 * sub, qf, zero16(), lane);
+        const f32x16_t dp = x_mma_rows(kv + TILE, 32 * sub, dof, zero16(), lane);
+        uint32_t bits = x_lane_bits(rows, hf);
+        if (a.causal) bits &= x_upto(p0 + rr - k0 - 4 * hf);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = x_or_zero(__builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse2)), bits, r);
+          D = fmaf(s[r], dp[r], D);
+          rsum += s[r];
+        }
+      }
+      kb = kn;
+    }
+    __syncthreads();  // (the next queries' blocks, or the queries themselves, take the ring)
+    const HalfPair pr = half_pair(D), ps = half_pair(rsum);
+    const float top = pr.x + pr.y, total = ps.x + ps.y;
+    D = total == 0.0f ? 0.0f : top / total;
+  }
+  if (hf == 0 && 32 * wave < QB) own[32 * wave + rr] = qv ? D : 0.0f;
+}
+
 // QS = 2: two wavefronts share 32 keys, each with every other tile of queries, and add
 // up at the end; a work-group has 64 keys then.
-template <typename T, bool BIAS, int QS>
-__global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_kv) {
+// OWN_D: D is formed here, for all queries of the key head, and not read.
+template <typename T, bool BIAS, int QS, bool OWN_D>
+__device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char* lds) {
   constexpr int QB = x_qb<T>(), TILE = QB * XT<T>::ROWB, KB = XQB / QS, KW = 4 / QS;
-  extern __shared__ __attribute__((aligned(1024))) char lds[];
   float* rowv = (float*)(lds + 4 * TILE);
   float* dist = (float*)(lds + kv_lds<T>());
-  if ((int)blockIdx.x >= n_kv) {
-    x_dtable_sum(a, blockIdx.x - n_kv, rowv);
-    return;
-  }
+  float* own = dist;  // OWN_D: [iteration][QB]
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int kblk, bg;
-  x_block(a, blockIdx.x, n_kv, (a.Sk + KB - 1) / KB * a.kv_splits, kblk, bg);
+  x_block(a, w, n_kv, (a.Sk + KB - 1) / KB * a.kv_splits, kblk, bg);
   const int split = kblk % a.kv_splits;
   kblk /= a.kv_splits;
   const int b = bg / a.G, g = bg % a.G;
@@ -679,6 +756,7 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
   auto row_raw = [&](int it) {
     const int r = qrow(it) + (tid & (QB - 1));
     if (!row_thread || r >= a.Sq) return tid < QB ? INFINITY : 0.0f;
+    if (OWN_D && tid >= QB) return own[it * QB + (tid & (QB - 1))];
     return (tid < QB ? a.lse : a.dsum)[((int64_t)b * a.H + head(it)) * a.Sq + r];
   };
   auto row_store = [&](float raw, int st) {
@@ -690,8 +768,13 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
       (const T*)a.k + b * a.sk[0] + (int64_t)key * a.sk[1] + g * a.sk[2], kvalid && it0 < n_it, hf);
   const typename XT<T>::Frag vf = x_frag(
       (const T*)a.v + b * a.sv[0] + (int64_t)key * a.sv[1] + g * a.sv[2], kvalid && it0 < n_it, hf);
+  if (it0 < n_it) dma(it0, lds);
+  if constexpr (OWN_D) {
+    for (int it = 0; it < n_it; ++it)
+      x_own_d<T>(a, b, g, head(it), qrow(it), qp, lds + 2 * TILE, own + it * QB, wave, lane);
+    __syncthreads();
+  }
   if (it0 < n_it) {
-    dma(it0, lds);
     row_store(row_raw(it0), 0);
     if (it0 + 1 < n_it) raw = row_raw(it0 + 1);
   }
@@ -807,6 +890,20 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
   __builtin_amdgcn_wave_barrier();
   x_store<T>(dv, 1.0f, stage, (T*)a.dv + b * a.sdv[0] + g * a.sdv[2], a.sdv[1], k0, a.Sk);
 }
+template <typename T, bool BIAS, int QS>
+__global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_kv) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  if ((int)blockIdx.x < n_kv) x_dkdv<T, BIAS, QS, false>(a, blockIdx.x, n_kv, lds);
+  else x_dtable_sum(a, blockIdx.x - n_kv, (float*)lds);
+}
+
+// The whole backward pass in one launch: work-groups from n_kv on make dQ.
+template <typename T, int QS>
+__global__ __launch_bounds__(256, 2) void xattn_bwd_kernel(XAttnArgs a, int n_kv) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  if ((int)blockIdx.x < n_kv) x_dkdv<T, false, QS, true>(a, blockIdx.x, n_kv, lds);
+  else x_dq<T, false, false, 2>(a, blockIdx.x - n_kv, gridDim.x - n_kv, lds);
+}
 
 // dK and dV from their splits, in order: 32 threads to a key, 4 values each.
 template <typename T>
@@ -861,7 +958,19 @@ template <typename T>
 hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
   hipError_t e = hipSuccess;
   const int qb = XQB / a.dq_ks;
+  const int kb = XQB / a.kv_qs;
+  const int64_t n_kv = (int64_t)a.B * a.G * ((a.Sk + kb - 1) / kb) * a.kv_splits;
   const int64_t gq = (int64_t)a.B * a.H * ((a.Sq + qb - 1) / qb) * a.dq_splits;
+  constexpr int QS2 = sizeof(T) == 4 ? 2 : 1;
+  if (a.one_launch) {
+    const dim3 grid((unsigned)(n_kv + gq));
+    const size_t lds = kv_lds<T>() + XOWN * 4;
+    if (a.kv_qs == 1)
+      hipLaunchKernelGGL((xattn_bwd_kernel<T, 1>), grid, dim3(256), lds, st, a, (int)n_kv);
+    else
+      hipLaunchKernelGGL((xattn_bwd_kernel<T, QS2>), grid, dim3(256), lds, st, a, (int)n_kv);
+    return hipGetLastError();
+  }
   if (gq > 0) {
     // The bias gradient is a sum of many dS that nearly cancel, in fp32: with D from
     // a bf16 out it would be off by out's rounding.
@@ -881,13 +990,10 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
       e = launch(xattn_dq_sum_kernel<T>, ((int64_t)a.B * a.H * a.Sq + 15) / 16, 0, st, a);
     if (e != hipSuccess) return e;
   }
-  const int kb = XQB / a.kv_qs;
-  const int64_t n_kv = (int64_t)a.B * a.G * ((a.Sk + kb - 1) / kb) * a.kv_splits;
   const int64_t n_red = a.dtable ? (int64_t)a.nb * a.H : 0;
   if (n_kv + n_red == 0) return e;
   const size_t lds = kv_lds<T>() + dist_bytes(a);
   const dim3 grid((unsigned)(n_kv + n_red));
-  constexpr int QS2 = sizeof(T) == 4 ? 2 : 1;
   if (a.kv_qs == 1) {
     if (a.table)
       hipLaunchKernelGGL((xattn_dkdv_kernel<T, true, 1>), grid, dim3(256), lds, st, a, (int)n_kv);
@@ -966,7 +1072,10 @@ XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_d
   // queries 3 us: 1 x 4 key heads of 4 x 2500 queries and 2500 keys 369 us in one piece
   // (80 work-groups), 96 + 8 in chunks; 8 x 12 heads of 128 (two blocks, fp32) 29 and
   // 22 + 5.
-  if (wgs * 2 <= slots && wgs > 0 && its >= 4) {
+  // (A block of few queries costs less, so at least four full ones: 8 x 16 heads over 4, 32
+  // queries over 300 keys, 30 us in four chunks, 19 in one; 2 x 8 over 1 21 and 23.)
+  const int64_t full = (int64_t)((std::min(Sq, rows) + 31) / 32) * 32 * its;
+  if (wgs * 2 <= slots && wgs > 0 && its >= 4 && full >= 4 * rows) {
     const int64_t all = wgs * its / (causal ? 2 : 1);
     const int64_t chunk = std::max<int64_t>((all + slots - 1) / slots, 1);
     plan = {rows, (int)chunk, (int)((its + chunk - 1) / chunk), 1};
@@ -984,6 +1093,23 @@ XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_d
     if (t2 < t1) plan = {rows, (int)std::max<int64_t>(its, 1), 1, 2};
   }
   return plan;
+}
+
+// Few work-groups and no bias: both parts of the backward in one launch, which saves the
+// second one and the wait for the first.  us in one and in two: 2 x 8 heads of 64 queries
+// and keys 9.4 and 12.1, fp32 13.9 and 22.6; 3 x 12 of 77 over 201 14 and 16.5; fp32, 10 x
+// 16 of 128 35.9 and 47.9.  bf16 work-groups go through all keys for D: 4 x 16 of 32 over
+// 300 14.5 and 15.6, of 100 over 700 33.6 and 26; two blocks of queries (4 x 16 of 256) 26.5
+// and 20.6.
+int xattn_one_launch(int B, int H, int G, int Sq, int Sk, bool bias, const XDqPlan& dq,
+                     const XKvPlan& kv, stage_dtype dt) {
+  if (bias || dq.splits != 1 || dq.ks != 2 || kv.splits != 1 || Sq == 0 || Sk == 0) return 0;
+  if (kv.chunk * kv.rows > XOWN) return 0;
+  if (dt == STAGE_BF16 && (kv.chunk > 1 || Sk > 6 * XKT)) return 0;
+  const int kb = XQB / kv.qs;
+  const int64_t n = (int64_t)B * G * ((Sk + kb - 1) / kb) +
+                    (int64_t)B * H * ((Sq + XQB / 2 - 1) / (XQB / 2));
+  return n <= 2 * device_cus();
 }
 
 hipError_t xattn_forward(const XAttnArgs& a, stage_dtype dt, hipStream_t st) {
