@@ -46,7 +46,8 @@ struct XAttnArgs {
 struct XKvPlan {
   int rows, chunk, splits, qs;
 };
-XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_dtype dt);
+XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, bool bias,
+                      stage_dtype dt);
 
 // About how long the forward kernel for many queries takes, in us, and by how many (1 or
 // 2) of its wavefronts 32 queries are shared.

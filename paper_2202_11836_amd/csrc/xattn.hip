@@ -1062,7 +1062,8 @@ double xattn_fwd_time(int B, int H, int Sq, int Sk, int causal, stage_dtype dt, 
   return std::min(t1, t2);
 }
 
-XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_dtype dt) {
+XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, bool bias,
+                      stage_dtype dt) {
   const int rows = dt == STAGE_BF16 ? x_qb<bf16_t>() : x_qb<float>();
   const int64_t its = (int64_t)((Sq + rows - 1) / rows) * rep;
   const int64_t wgs = (int64_t)B * G * ((Sk + XQB - 1) / XQB);
@@ -1073,9 +1074,11 @@ XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, stage_d
   // (80 work-groups), 96 + 8 in chunks; 8 x 12 heads of 128 (two blocks, fp32) 29 and
   // 22 + 5.
   // (A block of few queries costs less, so at least four full ones: 8 x 16 heads over 4, 32
-  // queries over 300 keys, 30 us in four chunks, 19 in one; 2 x 8 over 1 21 and 23.)
+  // queries over 300 keys, 30 us in four chunks, 19 in one; 2 x 8 over 1 21 and 23.  With a
+  // bias each head's table is made: 3 x 8 over 2, 56 queries and keys, 20 in one piece,
+  // 9.6 + 3.9 in four.)
   const int64_t full = (int64_t)((std::min(Sq, rows) + 31) / 32) * 32 * its;
-  if (wgs * 2 <= slots && wgs > 0 && its >= 4 && full >= 4 * rows) {
+  if (wgs * 2 <= slots && wgs > 0 && its >= 4 && (bias || full >= 4 * rows)) {
     const int64_t all = wgs * its / (causal ? 2 : 1);
     const int64_t chunk = std::max<int64_t>((all + slots - 1) / slots, 1);
     plan = {rows, (int)chunk, (int)((its + chunk - 1) / chunk), 1};
