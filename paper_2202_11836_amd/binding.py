@@ -67,7 +67,6 @@ class _RelPos(ctypes.Structure):  # attn_relpos
 # attn_shape: dtype, batch, seq_q, seq_k, heads, kv_heads, causal, scale and the
 # strides of q, k, v, out, dout, dq, dk, dv
 _ATTN_SHAPE = struct.Struct("@7if24q")
-_ATTN_FORWARD_SHAPE = struct.Struct("@7if12q96x")  # (no gradients)
 
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -552,10 +551,6 @@ def _attn_check(status: int) -> None:
         raise StageError(status, (load_library().attn_last_error() or b"").decode())
 
 
-def _refuse(msg: str):
-    raise StageError(STAGE_EINVAL, msg)
-
-
 class RelPos:
     """Buckets of a relative position bias (attn_relpos): num_buckets over both
     directions (bidirectional), or for the keys at or before a query only;
@@ -567,85 +562,40 @@ class RelPos:
         self.c = _RelPos()
         _attn_check(load_library().attn_relpos_init(self.num_buckets, self.max_distance,
                                                     int(self.bidirectional), ctypes.byref(self.c)))
-        self.ref = ctypes.byref(self.c)
+        self.ref, self.addr = ctypes.byref(self.c), ctypes.addressof(self.c)
 
     def bucket(self, distance: int) -> int:
         """Bucket of key position - query position."""
         return load_library().attn_relpos_bucket(ctypes.byref(self.c), int(distance))
 
 
-def _attn_strides(name, t, shape, dtype, dev):
-    """Batch, position and head stride of an operand of this shape, type and device."""
-    s = t.stride()
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
-        _refuse(f"{name} must be {dtype} {tuple(shape)} on cuda:{dev}")
-    if s[3] != 1:
-        _refuse(f"the 64 values of a head of {name} must lie side by side")
-    return s[:3]
+_attn_module = None
 
 
-def _attn_plain(name, t, shape, dtype, dev):
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
-        _refuse(f"{name} must be contiguous {dtype} {tuple(shape)} on cuda:{dev}")
-    return t.data_ptr()
-
-
-def _attn_inputs(q, k, v, key_mask, scale, causal, q_pos, relpos, table):
-    """Checks of what both calls take.  Returns the shapes of q and of k, the device,
-    the head of the packed attn_shape (up to the strides of v) and the arguments from
-    rp to q_pos."""
+def _attn_setup():
+    """csrc/py/attn_call.cpp, which checks and marshals the tensors of a call."""
+    global _attn_module
     import torch
-    dtype, dev, q_shape, kv_shape = q.dtype, q.get_device(), q.shape, k.shape
-    if dtype is torch.bfloat16:
-        code = STAGE_BF16
-    elif dtype is torch.float32:
-        code = STAGE_F32
-    else:
-        _refuse("q must be bfloat16 or float32")
-    if len(q_shape) != 4 or len(kv_shape) != 4 or q_shape[3] != 64 or dev < 0:
-        _refuse("q, k, v must be [batch, length, heads, 64] on a GPU")
-    B, Sq, H, D = q_shape
-    _, Sk, G, _ = kv_shape
-    if kv_shape[0] != B or kv_shape[3] != D:
-        _refuse(f"k must be [{B}, {Sk}, {G}, {D}]")
-    if scale is None:
-        scale = 0.125
-    elif not 0.0 < scale < 3e38:
-        _refuse("scale must be finite and positive")
-    if (relpos is None) != (table is None):
-        _refuse("relpos and table go together")
-    rp = tab = mask = pos = None
-    if relpos is not None:
-        rp, tab = relpos.ref, _attn_plain("table", table, (relpos.num_buckets, H), torch.float32, dev)
-    if key_mask is not None:
-        mask = _attn_plain("key_mask", key_mask, (B, Sk), torch.uint8, dev)
-    if q_pos is not None:
-        pos = _attn_plain("q_pos", q_pos, (B,), torch.int32, dev)
-    head = (code, B, Sq, Sk, H, G, 1 if causal else 0, scale,
-            *_attn_strides("q", q, q_shape, dtype, dev),
-            *_attn_strides("k", k, kv_shape, dtype, dev),
-            *_attn_strides("v", v, kv_shape, dtype, dev))
-    return q_shape, kv_shape, dev, head, (rp, tab, q.data_ptr(), k.data_ptr(), v.data_ptr(), mask,
-                                          pos)
+    lib = load_library()
+    try:
+        from . import _attn_call
+    except ImportError as e:
+        raise RuntimeError("_attn_call is not built; run __graft_entry__.build() first") from e
+    _attn_call.setup(*(ctypes.cast(f, ctypes.c_void_p).value
+                       for f in (lib.attn_workspace, lib.attn_forward, lib.attn_backward,
+                                 lib.attn_last_error)),
+                     StageError, torch.bfloat16, torch.float32, torch.uint8, torch.int32,
+                     torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
+                     lambda n, dev: torch.empty(n, dtype=torch.uint8, device=dev))
+    _attn_module = _attn_call
+    return _attn_module
 
 
-def _attn_call(fn, shape, args, backward, dev):
-    """fn(shape, args..., workspace, its bytes, stream) on device dev and its current
-    stream.  The workspace comes from torch's allocator, which gives no memory of a
-    stream (or of a captured graph) away while work on it may still use it."""
+def _attn_on(dev, fn, *args):
+    """The call again, on the device that it gave as the tensors' own."""
     import torch
-    if torch._C._cuda_getDevice() != dev:
-        with torch.cuda.device(dev):
-            return _attn_call(fn, shape, args, backward, dev)
-    n = ctypes.c_size_t()
-    _attn_check(_lib.attn_workspace(shape, args[0], backward, ctypes.byref(n)))
-    n, ws, ptr = n.value, None, None
-    if n:
-        ws = torch.empty(n, dtype=torch.uint8, device=dev)
-        ptr = ws.data_ptr()
-    status = fn(shape, *args, ptr, n, torch._C._cuda_getCurrentRawStream(dev))
-    if status:
-        _attn_check(status)
+    with torch.cuda.device(dev):
+        return fn(*args)
 
 
 def attn_forward(q, k, v, key_mask=None, scale=None, causal=False, q_pos=None, relpos=None,
@@ -664,50 +614,20 @@ def attn_forward(q, k, v, key_mask=None, scale=None, causal=False, q_pos=None, r
 
     A query without a key gets zeros and lse = -inf.  Runs on the current stream
     of q's device."""
-    import torch
-    fn = load_library().attn_forward
-    shape, _, dev, head, args = _attn_inputs(q, k, v, key_mask, scale, causal, q_pos, relpos, table)
-    rows = (shape[0], shape[2], shape[1])
-    if out is None:
-        out = q.new_empty(shape)
-    if lse is None:
-        lse = q.new_empty(rows, dtype=torch.float32)
-    packed = _ATTN_FORWARD_SHAPE.pack(*head, *_attn_strides("out", out, shape, q.dtype, dev))
-    _attn_call(fn, packed,
-               (*args, out.data_ptr(), _attn_plain("lse", lse, rows, torch.float32, dev)), 0, dev)
-    return out, lse
+    fn = (_attn_module or _attn_setup()).forward
+    r = fn(q, k, v, key_mask, scale, causal, q_pos, relpos, table, out, lse)
+    return r if r.__class__ is tuple else _attn_on(r, fn, q, k, v, key_mask, scale, causal, q_pos,
+                                                   relpos, table, out, lse)
 
 
 def attn_backward(q, k, v, out, lse, dout, key_mask=None, scale=None, causal=False, q_pos=None,
                   relpos=None, table=None, dq=None, dk=None, dv=None, dtable=None):
     """Gradients of <out, dout> for attn_forward's arguments, out and lse: returns
     dq, dk, dv and dtable (None without a table), written where given."""
-    import torch
-    fn = load_library().attn_backward
-    q_shape, kv_shape, dev, head, args = _attn_inputs(q, k, v, key_mask, scale, causal, q_pos,
-                                                      relpos, table)
-    B, Sq, H, _ = q_shape
-    dtype = q.dtype
-    if dq is None:
-        dq = q.new_empty(q_shape)
-    if dk is None:
-        dk = q.new_empty(kv_shape)
-    if dv is None:
-        dv = q.new_empty(kv_shape)
-    if table is None and dtable is not None:
-        _refuse("dtable without a table")
-    if table is not None and dtable is None:
-        dtable = torch.empty_like(table)
-    packed = _ATTN_SHAPE.pack(*head, *_attn_strides("out", out, q_shape, dtype, dev),
-                              *_attn_strides("dout", dout, q_shape, dtype, dev),
-                              *_attn_strides("dq", dq, q_shape, dtype, dev),
-                              *_attn_strides("dk", dk, kv_shape, dtype, dev),
-                              *_attn_strides("dv", dv, kv_shape, dtype, dev))
-    to = None if dtable is None else _attn_plain("dtable", dtable, table.shape, torch.float32, dev)
-    _attn_call(fn, packed,
-               (*args, out.data_ptr(), _attn_plain("lse", lse, (B, H, Sq), torch.float32, dev),
-                dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), to), 1, dev)
-    return dq, dk, dv, dtable
+    fn = (_attn_module or _attn_setup()).backward
+    r = fn(q, k, v, out, lse, dout, key_mask, scale, causal, q_pos, relpos, table, dq, dk, dv, dtable)
+    return r if r.__class__ is tuple else _attn_on(r, fn, q, k, v, out, lse, dout, key_mask, scale,
+                                                   causal, q_pos, relpos, table, dq, dk, dv, dtable)
 
 
 # ---------------------------------------------------------------------------

@@ -2,7 +2,8 @@
 
 Compiles every ``csrc/*.hip`` with hipcc for gfx950 (and the host-only
 ``csrc/*.cpp``) and links them into
-``paper_2202_11836_amd/libskystage.so``.  Always recompiles (the caller asks
+``paper_2202_11836_amd/libskystage.so``, and ``csrc/py`` into the Python module
+``_attn_call.so`` beside it.  Always recompiles (the caller asks
 for a fresh build); sources compile in parallel.
 """
 from __future__ import annotations
@@ -47,6 +48,20 @@ def _compile(src: str) -> str:
     return obj
 
 
+def build_binding() -> str:
+    """The Python module that marshals the attention operators' calls (host code)."""
+    import sysconfig
+    src = os.path.join(CSRC, "py", "attn_call.cpp")
+    path = os.path.join(PKG, "_attn_call.so")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+           "-I" + sysconfig.get_paths()["include"], src, "-o", path + ".tmp"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{src}:\n{r.stderr}")
+    os.replace(path + ".tmp", path)
+    return path
+
+
 def build(verbose: bool = False) -> str:
     if shutil.which(HIPCC) is None and not os.path.exists(HIPCC):
         raise RuntimeError(f"hipcc not found ({HIPCC})")
@@ -60,6 +75,7 @@ def build(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, LIB_PATH)
+    build_binding()
     if verbose:
         print(f"built {LIB_PATH} from {len(srcs)} sources", file=sys.stderr)
     return LIB_PATH

@@ -185,3 +185,20 @@ def test_spans_beyond_any_memory_refused(name):
     assert st == 1 and "spans" in msg
     st, msg = call(1, shape(batch=5000, **{"dq" if name == "out" else name: (1 << 52, *inner)}))
     assert st == 1 and "spans" in msg
+
+
+def test_module_of_the_binding():
+    """What the marshalling module says before any tensor is looked at."""
+    P.RelPos()
+    with pytest.raises(P.StageError):
+        import torch
+        P.attn_forward(*(torch.zeros(1, 2, 1, 64),) * 3)  # (sets the module up, refuses the CPU)
+    from paper_2202_11836_amd import _attn_call as m
+    for fn, n in ((m.forward, 11), (m.backward, 16), (m.setup, 12)):
+        with pytest.raises(TypeError):
+            fn(*(None,) * (n - 1))
+    with pytest.raises(ValueError):
+        m.setup(*(0,) * 12)
+    for q in (None, 3, "q"):
+        with pytest.raises(AttributeError):
+            P.attn_forward(q, q, q)

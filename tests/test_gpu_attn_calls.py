@@ -360,3 +360,57 @@ def test_scales_beyond_fp32_refused():
         with pytest.raises(StageError) as e:
             P.attn_forward(q, q, q, scale=scale)
         assert e.value.status == 1
+
+
+def test_references_are_given_back():
+    """Calls that pass and calls that are refused, anywhere in their checks, keep no
+    reference to what they were given, and none to what they made."""
+    import gc
+    import sys
+
+    q, k = rand((2, 5, 4, 64), 1, "bf16"), rand((2, 7, 2, 64), 2, "bf16")
+    v, do = rand((2, 7, 2, 64), 3, "bf16"), rand((2, 5, 4, 64), 4, "bf16")
+    m, pos = torch.ones((2, 7), dtype=torch.uint8, device="cuda"), torch.zeros(2, dtype=torch.int32,
+                                                                              device="cuda")
+    rp, table = P.RelPos(8, 20), torch.zeros((8, 4), device="cuda")
+    out, lse = P.attn_forward(q, k, v)
+    grads = [torch.empty_like(t) for t in (q, k, v)] + [torch.empty_like(table)]
+    kw = dict(key_mask=m, scale=0.2, causal=True, q_pos=pos, relpos=rp, table=table)
+    things = [q, k, v, do, m, pos, rp, table, out, lse, *grads, None, torch.float32, torch.bfloat16,
+              torch.uint8, torch.int32, StageError]
+
+    def calls():
+        P.attn_forward(q, k, v)
+        P.attn_forward(q, k, v, out=out, lse=lse, **kw)
+        P.attn_backward(q, k, v, out, lse, do)
+        P.attn_backward(q, k, v, out, lse, do, dq=grads[0], dk=grads[1], dv=grads[2], dtable=grads[3],
+                        **kw)
+        bad = torch.zeros(3, device="cuda")
+        for a, b in [((q, k, bad), {}), ((bad, k, v), {}), ((q, bad, v), {}), ((q, k, v), dict(out=bad)),
+                     ((q, k, v), dict(lse=bad)), ((q, k, v), dict(key_mask=bad)),
+                     ((q, k, v), dict(q_pos=bad)), ((q, k, v), dict(relpos=rp, table=bad)),
+                     ((q, k, v), dict(scale=-1.0)), ((q, k, v), dict(out=q))]:
+            with pytest.raises(StageError):
+                P.attn_forward(*a, **b)
+        for b in (dict(dq=bad), dict(dk=bad), dict(dv=bad), dict(relpos=rp, table=table, dtable=bad),
+                  dict(dtable=bad), dict(dq=out)):
+            with pytest.raises(StageError):
+                P.attn_backward(q, k, v, out, lse, do, **b)
+        with pytest.raises(AttributeError):
+            P.attn_forward(q, 3, v)
+        with pytest.raises(TypeError):
+            P.attn_forward(q, k, v, scale="much")
+
+    # (tracebacks of refused calls are cycles that hold tensors until they are collected)
+    calls()
+    gc.collect()
+    torch.cuda.synchronize()
+    held, before = torch.cuda.memory_allocated(), [sys.getrefcount(t) for t in things]
+    for _ in range(50):
+        calls()
+    gc.collect()
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() == held
+    # (None and the types are held all over the interpreter)
+    for t, n in zip(things, before):
+        assert abs(sys.getrefcount(t) - n) < 20, t
