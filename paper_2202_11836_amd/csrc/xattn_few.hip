@@ -344,14 +344,14 @@ hipError_t few_t(const XAttnArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// A time model of both forward kernels in us, fitted to 470 timed launches (one token
-// to 2500 queries, 77 to 32768 keys; its choice is on average 2% off the best, at
-// worst 18%).  A work-group of this kernel costs its set-up and, per 32-key block of
-// a wavefront, more the more wavefronts share a SIMD; a work-group of the other one
-// (128 rows) the same per 64-key block.  Splits add a launch and their partial
-// results.  For instance 16 heads, one token and 8192 keys: 147 us with the other
-// kernel, 37 with one split of 8 wavefronts, 14 with 16; 32 x 16 heads of 128 queries
-// and 512 keys: 21 with the other kernel, 34 with this one.
+// A time model of this kernel in us, beside xattn_fwd_time, fitted to 700 timed launches
+// (one token to 2500 queries, 51 to 32768 keys; over 40 shapes its choice is on average 2%
+// off the best, at worst 12%).  A work-group costs its set-up and, per 32-key block of a
+// wavefront, more the more wavefronts share a SIMD.  Splits add a launch and their partial
+// results.  For instance 16 heads, one token and 8192 keys: 147 us with the other kernel,
+// 38 with one split of 8 wavefronts, 16 with 8; 8 x 8 heads, one token over 700 keys 7.8
+// with 8 wavefronts, 8.2 with 4; 32 x 16 heads of 128 queries and 512 keys: 21 with the
+// other kernel, 34 with this one.
 XFewPlan xattn_few_plan(int B, int G, int rep, int Sq, int Sk, int buckets, int reach,
                         stage_dtype dt) {
   const bool bf16 = dt == STAGE_BF16;
@@ -363,7 +363,7 @@ XFewPlan xattn_few_plan(int B, int G, int rep, int Sq, int Sk, int buckets, int 
   double best = xattn_fwd_time(B, G * rep, Sq, Sk, 0, dt, &ks);
   // No faster than the memory: of several that are bound by it, the fewest
   // wavefronts (16 x 16 heads over 8192 keys: 97 us with 4, 112 with 8).
-  const double floor = 2.0 + 2.0 * B * G * (double)Sk * (bf16 ? 128 : 256) / 5.2e6;
+  const double floor = 2.0 + 2.0 * B * G * (double)Sk * (bf16 ? 128 : 256) / 5.5e6;
   XFewPlan plan = {0, 0, 0};
   const int blocks = (Sk + FB - 1) / FB;
   for (int waves = 4; waves <= (bf16 ? 8 : 4); waves += 4) {
@@ -375,9 +375,14 @@ XFewPlan xattn_few_plan(int B, int G, int rep, int Sq, int Sk, int buckets, int 
       if (splits > 1 && (splits * waves > blocks || tiles * splits > 2 * cus)) continue;
       const double grid = tiles * splits, n = std::min(wcap, std::ceil(grid / cus));
       const double per = std::ceil((double)blocks / (waves * splits));
-      double t = std::ceil(grid / (wcap * cus)) *
-                 (bf16 ? 2.9 + per * (0.75 + 0.27 * (waves / 4 * n - 1)) : 2.6 + per * 2.8);
-      if (splits > 1) t += 5.3 + 0.025e-3 * (double)B * G * rep * Sq * splits;
+      const double rounds = std::ceil(grid / (wcap * cus));
+      double t = rounds * (bf16 ? 4.5 + (buckets ? 2.1 : 0.0) +
+                                      per * (0.67 + 0.4 * (waves / 4 * n - 1))
+                                : 2.6 + per * 2.8);
+      if (bf16) t -= 1.3;
+      if (splits > 1)
+        t += bf16 ? 2.4 + 0.3 * splits + 0.25e-3 * (double)B * G * rep * Sq * splits
+                  : 5.3 + 0.025e-3 * (double)B * G * rep * Sq * splits;
       t = std::max(t, floor);
       if (t < best) {
         best = t;
