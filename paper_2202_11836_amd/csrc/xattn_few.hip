@@ -295,19 +295,40 @@ __global__ __launch_bounds__(256) void xattn_few_join_kernel(XAttnArgs a, int n_
   const int bg = (int)(id / R), row = (int)(id % R), c = (threadIdx.x & 15) * 4;
   const int64_t step = (int64_t)a.B * a.G * n_rt * 32 * XFEW_ROW;
   const float* p = a.part + ((int64_t)bg * n_rt * 32 + row) * XFEW_ROW;
+  // Eight splits' values are requested together, none of them waiting for another's.
   float top = -INFINITY, l = 0.0f;
-  for (int s = threadIdx.x & 15; s < a.few_splits; s += 16) top = fmaxf(top, p[s * step + 64]);
-#pragma unroll
-  for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
   f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
-  for (int s = 0; s < a.few_splits; ++s) {
-    const float ms = p[s * step + 64];
-    const float f = ms == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ms - top);
-    const f32x4_t v = *(const f32x4_t*)(p + s * step + c);
-    l = fmaf(p[s * step + 65], f, l);
+  for (int s0 = 0; s0 < a.few_splits; s0 += 8) {
+    float m[8], ls[8];
+    f32x4_t v[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], f, o[e]);
+    for (int j = 0; j < 8; ++j) {
+      const float* ps = p + (int64_t)min(s0 + j, a.few_splits - 1) * step;
+      m[j] = ps[64];
+      ls[j] = ps[65];
+      v[j] = *(const f32x4_t*)(ps + c);
+    }
+    const float was = top;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (s0 + j >= a.few_splits) {  // (the last one again)
+        m[j] = -INFINITY;
+        ls[j] = 0.0f;
+        v[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+      top = fmaxf(top, m[j]);
+    }
+    const float off = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(was - off);
+    l *= keep;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= keep;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float f = __builtin_amdgcn_exp2f(m[j] - off);
+      l = fmaf(ls[j], f, l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(v[j][e], f, o[e]);
+    }
   }
   const int b = bg / a.G, g = bg % a.G, i = row / a.rep, h = g * a.rep + row % a.rep;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
