@@ -920,7 +920,17 @@ __global__ __launch_bounds__(256) void xattn_kv_sum_kernel(XAttnArgs a) {
   const int splits = max(1, (n_it + a.kv_chunk - 1) / a.kv_chunk);
   f32x4_t t = {0.0f, 0.0f, 0.0f, 0.0f};
   const float* p = a.part + row * 2 * XHD + c;
-  for (int i = 0; i < splits; ++i) t += *(const f32x4_t*)(p + (int64_t)i * n * 2 * XHD);
+  // (four loads on their way at a time: 2 x 8 heads over 1, fp32, 8 splits and more, 6.8 -> 4
+  // us)
+  for (int i = 0; i < splits; i += 4) {
+    f32x4_t v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      v[j] = *(const f32x4_t*)(p + (int64_t)min(i + j, splits - 1) * n * 2 * XHD);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i + j < splits) t += v[j];
+  }
   T* to = c < XHD ? (T*)a.dk + b * a.sdk[0] + (int64_t)key * a.sdk[1] + g * a.sdk[2] + c
                   : (T*)a.dv + b * a.sdv[0] + (int64_t)key * a.sdv[1] + g * a.sdv[2] + c - XHD;
   if constexpr (sizeof(T) == 2)

@@ -175,6 +175,14 @@ def test_shared_work(dtype, shape, mask, garbage, causal, relpos):
     run(dtype, *shape, mask=mask, garbage=garbage, causal=causal, relpos=relpos)
 
 
+# (more splits of the keys than are joined at once)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,G,Sq,Sk", [(1, 1, 1, 1, 20000), (1, 2, 1, 2, 33000)])
+@pytest.mark.parametrize("mask", ["none", "last", "holes"])
+def test_tokens_over_long_caches(dtype, B, H, G, Sq, Sk, mask):
+    run(dtype, B, H, G, Sq, Sk, mask=mask, backward=False)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_no_queries_no_keys_no_batch(dtype):
     rp, dt = P.RelPos(8, 20), DT[dtype]
