@@ -564,6 +564,9 @@ class RelPos:
                                                     int(self.bidirectional), ctypes.byref(self.c)))
         self.ref, self.addr = ctypes.byref(self.c), ctypes.addressof(self.c)
 
+    def __reduce__(self):  # (a copy holds buckets of its own)
+        return RelPos, (self.num_buckets, self.max_distance, self.bidirectional)
+
     def bucket(self, distance: int) -> int:
         """Bucket of key position - query position."""
         return load_library().attn_relpos_bucket(ctypes.byref(self.c), int(distance))

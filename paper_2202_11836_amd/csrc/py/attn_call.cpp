@@ -27,7 +27,7 @@ ErrorFn error_fn;
 // Set by setup(): what is taken from torch and the binding.
 PyObject *stage_error, *bf16, *f32, *u8, *i32, *current_device, *current_stream, *new_workspace;
 // Names of attributes
-PyObject *n_shape, *n_stride, *n_dtype, *n_get_device, *n_data_ptr, *n_new_empty, *n_addr, *n_buckets;
+PyObject *n_shape, *n_stride, *n_dtype, *n_get_device, *n_data_ptr, *n_new_empty, *n_addr;
 PyObject* kw_dtype;
 
 // Owns a reference.
@@ -200,11 +200,11 @@ bool inputs(PyObject* q, PyObject* k, PyObject* v, PyObject* key_mask, PyObject*
   if (s.causal < 0) return false;
   if ((relpos == Py_None) != (table == Py_None)) return refuse("relpos and table go together");
   if (relpos != Py_None) {
-    Ref n(PyObject_GetAttr(relpos, n_buckets)), addr(n.p ? PyObject_GetAttr(relpos, n_addr) : nullptr);
+    Ref addr(PyObject_GetAttr(relpos, n_addr));
     if (!addr.p) return false;
-    in->buckets = PyLong_AsLongLong(n.p);
     in->rp = (const attn_relpos*)PyLong_AsVoidPtr(addr.p);
-    if (PyErr_Occurred()) return false;
+    if (!in->rp) return PyErr_Occurred() ? false : refuse("relpos holds no buckets");
+    in->buckets = in->rp->num_buckets;
     if (!plain("table", table, 2, in->buckets, t.size[2], 1, f32, t.dev, &in->table)) return false;
   }
   if (key_mask != Py_None &&
@@ -395,7 +395,7 @@ PyMODINIT_FUNC PyInit__attn_call(void) {
   } const names[] = {{&n_shape, "shape"},         {&n_stride, "stride"},
                      {&n_dtype, "dtype"},         {&n_get_device, "get_device"},
                      {&n_data_ptr, "data_ptr"},   {&n_new_empty, "new_empty"},
-                     {&n_addr, "addr"},           {&n_buckets, "num_buckets"}};
+                     {&n_addr, "addr"}};
   for (const auto& e : names)
     if (!(*e.to = PyUnicode_InternFromString(e.name))) return nullptr;
   if (!(kw_dtype = PyTuple_Pack(1, n_dtype))) return nullptr;

@@ -202,3 +202,13 @@ def test_module_of_the_binding():
     for q in (None, 3, "q"):
         with pytest.raises(AttributeError):
             P.attn_forward(q, q, q)
+
+
+def test_copies_of_the_buckets():
+    import copy
+    import pickle
+
+    rp = P.RelPos(16, 50, False)
+    for other in (copy.copy(rp), copy.deepcopy(rp), pickle.loads(pickle.dumps(rp))):
+        assert other.addr != rp.addr and other.bidirectional is False
+        assert [other.bucket(d) for d in range(-80, 9)] == [rp.bucket(d) for d in range(-80, 9)]
