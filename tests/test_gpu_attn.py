@@ -184,6 +184,14 @@ def test_tokens_over_long_caches(dtype, B, H, G, Sq, Sk, mask):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,G,Sq,Sk", [(1, 2, 1, 150000, 5), (1, 2, 1, 5, 150000)])
+@pytest.mark.parametrize("causal,q_pos,relpos", [(False, None, None), (False, [40], (32, 128, True)),
+                                                 (True, [149990], (32, 128, False))])
+def test_one_long_side(dtype, B, H, G, Sq, Sk, causal, q_pos, relpos):
+    run(dtype, B, H, G, Sq, Sk, causal=causal, q_pos=q_pos, relpos=relpos)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_no_queries_no_keys_no_batch(dtype):
     rp, dt = P.RelPos(8, 20), DT[dtype]
     for B, Sq, Sk in [(2, 0, 70), (2, 70, 0), (0, 5, 5), (2, 0, 0)]:

@@ -414,3 +414,39 @@ def test_references_are_given_back():
     # (None and the types are held all over the interpreter)
     for t, n in zip(things, before):
         assert abs(sys.getrefcount(t) - n) < 20, t
+
+
+def test_threads():
+    """Calls from several threads at once, each on a stream of its own."""
+    import threading
+
+    cases = [Case(*c) for c in (CASES[0], CASES[2], CASES[4], CASES[5])]
+    for i, c in enumerate(cases):
+        c.fill(i)
+    want = [c.eager() for c in cases]
+    torch.cuda.synchronize()
+    got, errors = [None] * len(cases), []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for n in range(30):
+                    cases[i].call()
+                    if n % 7 == 0:  # (and refused ones between them, with their messages)
+                        try:
+                            P.attn_forward(cases[i].q, cases[i].k, cases[i].v, scale=-1.0)
+                        except StageError as e:
+                            assert "scale" in str(e)
+                got[i] = cases[i].results()
+                torch.cuda.current_stream().synchronize()
+        except BaseException as e:
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(cases))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    for g, w in zip(got, want):
+        assert len(g) == len(w) and all(torch.equal(x, y) for x, y in zip(g, w))
