@@ -397,7 +397,7 @@ XFewPlan xattn_few_plan(int B, int G, int rep, int Sq, int Sk, int buckets, int 
       const double grid = tiles * splits, n = std::min(wcap, std::ceil(grid / cus));
       const double per = std::ceil((double)blocks / (waves * splits));
       const double rounds = std::ceil(grid / (wcap * cus));
-      double t = rounds * (bf16 ? 4.5 + (buckets ? 2.1 : 0.0) +
+      double t = rounds * (bf16 ? 4.5 + (buckets ? 2.1 : 0.0) + (waves == 8 ? 0.5 : 0.0) +
                                       per * (0.67 + 0.4 * (waves / 4 * n - 1))
                                 : 2.6 + per * 2.8);
       if (bf16) t -= 1.3;
