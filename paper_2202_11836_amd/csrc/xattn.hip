@@ -31,7 +31,7 @@ constexpr int XQB = 128;  // rows (queries or keys) of a work-group
 // Work-group w of n -> (row block, batch * head): as attn_block, or, with `causal`, the
 // first row block of every head, then the second of every head, and so on (those with
 // the most work first).  Work-groups go round the CUs, and with a head's row blocks in
-// a row a CU got the same one of every head: 13 x 16 heads of 512 (with a bias) were as
+// a row a CU got the same one of every head: 13 x 16 heads of 387 (with a bias) were as
 // slow as without `causal`, forward 25.5 -> 19.7 us, dQ 58.6 -> 41.2, dK and dV 45.4 ->
 // 31.7 in this order.  (A head stays on one XCD where the heads are a multiple of 8.)
 __device__ __forceinline__ void x_block(const XAttnArgs& a, int w, int n, int nq, int& rb,
