@@ -105,7 +105,7 @@ Workspace workspace_of(const attn_shape* s, const attn_relpos* rp, bool backward
     w.tpart = ((int64_t)s->batch * s->heads * ((s->seq_q + qb - 1) / qb) * rp->num_buckets * 4 + 15) /
               16 * 16;
   w.kv = xattn_kv_plan(s->batch, s->kv_heads, rep, s->seq_q, s->seq_k, s->causal, rp != nullptr,
-                       s->dtype);
+                       w.dq, s->dtype);
   if (w.kv.splits > 1)
     w.part = (int64_t)w.kv.splits * s->batch * s->kv_heads * s->seq_k * 2 * XHD * 4;
   if (w.dq.splits > 1)  // (its partial results are summed before those of dK, dV are made)

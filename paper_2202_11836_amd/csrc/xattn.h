@@ -46,8 +46,6 @@ struct XAttnArgs {
 struct XKvPlan {
   int rows, chunk, splits, qs;
 };
-XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, bool bias,
-                      stage_dtype dt);
 
 // About how long the forward kernel for many queries takes, in us, and by how many (1 or
 // 2) of its wavefronts 32 queries are shared.
@@ -61,7 +59,9 @@ struct XDqPlan {
   int ks, splits;
 };
 XDqPlan xattn_dq_plan(int B, int H, int Sq, int Sk, int causal, bool bias, stage_dtype dt);
-// Whether one kernel makes all of a backward's results.
+XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, bool bias,
+                      const XDqPlan& dq, stage_dtype dt);
+// Whether one kernel makes all of a backward's results (up to the sum of dK's splits).
 int xattn_one_launch(int B, int H, int G, int Sq, int Sk, bool bias, const XDqPlan& dq,
                      const XKvPlan& kv, stage_dtype dt);
 inline int xattn_dq_row(stage_dtype dt) { return dt == STAGE_BF16 ? 132 : 64; }

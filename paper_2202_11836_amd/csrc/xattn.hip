@@ -609,7 +609,7 @@ __global__ __launch_bounds__(256) void xattn_dq_sum_kernel(XAttnArgs a) {
 // gradient: one to eight buckets of a head.
 // ---------------------------------------------------------------------------
 template <typename T> constexpr int x_qb() { return sizeof(T) == 2 ? 128 : 64; }
-constexpr int XOWN = 256;  // most queries (of all heads of a key head) whose D a work-group forms
+constexpr int XOWN = 256;  // most queries (of all its heads) whose D a work-group forms
 // LDS: [2][Q, dO], per stage lse and -D of QB rows, a word per wavefront; with a bias
 // its table by distance follows.
 template <typename T> constexpr int kv_lds() {
@@ -716,7 +716,7 @@ __device__ __forceinline__ void x_own_d(const XAttnArgs& a, int b, int g, int h,
 
 // QS = 2: two wavefronts share 32 keys, each with every other tile of queries, and add
 // up at the end; a work-group has 64 keys then.
-// OWN_D: D is formed here, for all queries of the key head, and not read.
+// OWN_D: D is formed here, for all queries of the work-group, and not read.
 template <typename T, bool BIAS, int QS, bool OWN_D>
 __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char* lds) {
   constexpr int QB = x_qb<T>(), TILE = QB * XT<T>::ROWB, KB = XQB / QS, KW = 4 / QS;
@@ -768,7 +768,7 @@ __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char
   auto row_raw = [&](int it) {
     const int r = qrow(it) + (tid & (QB - 1));
     if (!row_thread || r >= a.Sq) return tid < QB ? INFINITY : 0.0f;
-    if (OWN_D && tid >= QB) return own[it * QB + (tid & (QB - 1))];
+    if (OWN_D && tid >= QB) return own[(it - it0) * QB + (tid & (QB - 1))];
     return (tid < QB ? a.lse : a.dsum)[((int64_t)b * a.H + head(it)) * a.Sq + r];
   };
   auto row_store = [&](float raw, int st) {
@@ -782,8 +782,8 @@ __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char
       (const T*)a.v + b * a.sv[0] + (int64_t)key * a.sv[1] + g * a.sv[2], kvalid && it0 < n_it, hf);
   if (it0 < n_it) dma(it0, lds);
   if constexpr (OWN_D) {
-    for (int it = 0; it < n_it; ++it)
-      x_own_d<T>(a, b, g, head(it), qrow(it), qp, lds + 2 * TILE, own + it * QB, wave, lane);
+    for (int it = it0; it < n_it; ++it)
+      x_own_d<T>(a, b, g, head(it), qrow(it), qp, lds + 2 * TILE, own + (it - it0) * QB, wave, lane);
     __syncthreads();
   }
   if (it0 < n_it) {
@@ -991,7 +991,8 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
       hipLaunchKernelGGL((xattn_bwd_kernel<T, 1>), grid, dim3(256), lds, st, a, (int)n_kv);
     else
       hipLaunchKernelGGL((xattn_bwd_kernel<T, QS2>), grid, dim3(256), lds, st, a, (int)n_kv);
-    return hipGetLastError();
+    if ((e = hipGetLastError()) != hipSuccess || a.kv_splits == 1) return e;
+    return launch(xattn_kv_sum_kernel<T>, ((int64_t)a.B * a.G * a.Sk + 7) / 8, 0, st, a);
   }
   if (gq > 0) {
     // The bias gradient is a sum of many dS that nearly cancel, in fp32: with D from
@@ -1084,8 +1085,28 @@ double xattn_fwd_time(int B, int H, int Sq, int Sk, int causal, stage_dtype dt, 
   return std::min(t1, t2);
 }
 
+// Few work-groups and no bias: both parts of the backward in one launch, which saves the
+// second one and the wait for the first.  us in one and in two: 2 x 8 heads of 64 queries
+// and keys 9.4 and 12.1, fp32 13.9 and 22.6; 3 x 12 of 77 over 201 14 and 16.5; fp32, 10 x
+// 16 of 128 35.9 and 47.9.  bf16 work-groups go through all keys for D: 4 x 16 of 32 over
+// 300 14.5 and 15.6, of 100 over 700 33.6 and 26; two blocks of queries (4 x 16 of 256) 26.5
+// and 20.6.
+int xattn_one_launch(int B, int H, int G, int Sq, int Sk, bool bias, const XDqPlan& dq,
+                     const XKvPlan& kv, stage_dtype dt) {
+  if (bias || dq.splits != 1 || dq.ks != 2 || Sq == 0 || Sk == 0) return 0;
+  if (kv.chunk * kv.rows > XOWN) return 0;
+  if (dt == STAGE_BF16 && (kv.chunk > 1 || Sk > 6 * XKT)) return 0;
+  const int kb = XQB / kv.qs;
+  const int64_t n = (int64_t)B * G * ((Sk + kb - 1) / kb) * kv.splits +
+                    (int64_t)B * H * ((Sq + XQB / 2 - 1) / (XQB / 2));
+  // (bf16, chunks that each go through many keys: 11 x 8 heads over 2 of 32 over 300, 352
+  // work-groups, 24.9 in one launch, 17.8 in two; 4 x 8 over 2 of 77 over 201, 128, 17 and 22)
+  const bool long_d = dt == STAGE_BF16 && kv.splits > 1 && Sk > 2 * XKT;
+  return n <= (long_d ? 1 : 2) * device_cus();
+}
+
 XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, bool bias,
-                      stage_dtype dt) {
+                      const XDqPlan& dq, stage_dtype dt) {
   const int rows = dt == STAGE_BF16 ? x_qb<bf16_t>() : x_qb<float>();
   const int64_t its = (int64_t)((Sq + rows - 1) / rows) * rep;
   const int64_t wgs = (int64_t)B * G * ((Sk + XQB - 1) / XQB);
@@ -1095,15 +1116,17 @@ XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, bool bi
   // queries 3 us: 1 x 4 key heads of 4 x 2500 queries and 2500 keys 369 us in one piece
   // (80 work-groups), 96 + 8 in chunks; 8 x 12 heads of 128 (two blocks, fp32) 29 and
   // 22 + 5.
-  // (A block of few queries costs less, so at least four full ones: 8 x 16 heads over 4, 32
-  // queries over 300 keys, 30 us in four chunks, 19 in one; 2 x 8 over 1 21 and 23.  With a
-  // bias each head's table is made: 3 x 8 over 2, 56 queries and keys, 20 in one piece,
-  // 9.6 + 3.9 in four.)
-  const int64_t full = (int64_t)((std::min(Sq, rows) + 31) / 32) * 32 * its;
-  if (wgs * 2 <= slots && wgs > 0 && its >= 4 && (bias || full >= 4 * rows)) {
+  // (A block of few queries costs less, so four full ones: 8 x 16 heads over 4, 32 queries
+  // over 300 keys, 30 us in four chunks, 19 in one.  But with a bias each head's table is
+  // made: 3 x 8 over 2, 56 queries and keys, 20 and 9.6 + 3.9; and what one launch holds
+  // runs beside dQ: 4 x 8 over 2, 22 over 27, dQ and all 14.3 and 10.4, fp32 26 and 13.)
+  if (wgs * 2 <= slots && wgs > 0 && its >= 4) {
+    const int64_t full = (int64_t)((std::min(Sq, rows) + 31) / 32) * 32 * its;
     const int64_t all = wgs * its / (causal ? 2 : 1);
     const int64_t chunk = std::max<int64_t>((all + slots - 1) / slots, 1);
-    plan = {rows, (int)chunk, (int)((its + chunk - 1) / chunk), 1};
+    const XKvPlan split = {rows, (int)chunk, (int)((its + chunk - 1) / chunk), 1};
+    if (bias || full >= 4 * rows || xattn_one_launch(B, G * rep, G, Sq, Sk, bias, dq, split, dt))
+      plan = split;
   }
   // fp32: half as many keys to a work-group, two wavefronts to 32 of them, where that
   // leaves at most two to a CU.  us by work-groups per CU and blocks of queries, fitted
@@ -1118,23 +1141,6 @@ XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, bool bi
     if (t2 < t1) plan = {rows, (int)std::max<int64_t>(its, 1), 1, 2};
   }
   return plan;
-}
-
-// Few work-groups and no bias: both parts of the backward in one launch, which saves the
-// second one and the wait for the first.  us in one and in two: 2 x 8 heads of 64 queries
-// and keys 9.4 and 12.1, fp32 13.9 and 22.6; 3 x 12 of 77 over 201 14 and 16.5; fp32, 10 x
-// 16 of 128 35.9 and 47.9.  bf16 work-groups go through all keys for D: 4 x 16 of 32 over
-// 300 14.5 and 15.6, of 100 over 700 33.6 and 26; two blocks of queries (4 x 16 of 256) 26.5
-// and 20.6.
-int xattn_one_launch(int B, int H, int G, int Sq, int Sk, bool bias, const XDqPlan& dq,
-                     const XKvPlan& kv, stage_dtype dt) {
-  if (bias || dq.splits != 1 || dq.ks != 2 || kv.splits != 1 || Sq == 0 || Sk == 0) return 0;
-  if (kv.chunk * kv.rows > XOWN) return 0;
-  if (dt == STAGE_BF16 && (kv.chunk > 1 || Sk > 6 * XKT)) return 0;
-  const int kb = XQB / kv.qs;
-  const int64_t n = (int64_t)B * G * ((Sk + kb - 1) / kb) +
-                    (int64_t)B * H * ((Sq + XQB / 2 - 1) / (XQB / 2));
-  return n <= 2 * device_cus();
 }
 
 hipError_t xattn_forward(const XAttnArgs& a, stage_dtype dt, hipStream_t st) {
