@@ -391,8 +391,8 @@ XFewPlan xattn_few_plan(int B, int G, int rep, int Sq, int Sk, int buckets, int 
     const size_t lds = waves * 4 * FB * (bf16 ? 128 : 256) + few_near_bytes(buckets, reach);
     if (lds > 160 * 1024) continue;
     const double wcap = lds <= 80 * 1024 ? 2 : 1;
-    for (int i = 0; i < 14; ++i) {
-      const int splits = i & 1 ? 3 << (i / 2) : 2 << (i / 2) >> 1;  // 1, 3, 2, 6, 4, 12 ... 192
+    for (const int splits :
+         {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128, 192}) {
       if (splits > 1 && (splits * waves > blocks || tiles * splits > 2 * cus)) continue;
       const double grid = tiles * splits, n = std::min(wcap, std::ceil(grid / cus));
       const double per = std::ceil((double)blocks / (waves * splits));
