@@ -191,6 +191,19 @@ def test_one_long_side(dtype, B, H, G, Sq, Sk, causal, q_pos, relpos):
     run(dtype, B, H, G, Sq, Sk, causal=causal, q_pos=q_pos, relpos=relpos)
 
 
+# (the heads of a key head go to several work-groups, beside those of dQ)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(2, 8, 1, 20, 60), (3, 8, 2, 70, 130), (1, 16, 2, 40, 90),
+                                   (2, 12, 2, 129, 33)])
+@pytest.mark.parametrize("mask,garbage", [("none", False), ("empty", True), ("holes", True),
+                                          ("last", False)])
+@pytest.mark.parametrize("causal,q_pos", [(False, None), (True, [7, -3, 40])])
+@pytest.mark.parametrize("relpos", [None, (8, 20, True)])
+def test_shared_key_heads_of_few_queries(dtype, shape, mask, garbage, causal, q_pos, relpos):
+    run(dtype, *shape, mask=mask, garbage=garbage, causal=causal,
+        q_pos=None if q_pos is None else q_pos[:shape[0]], relpos=relpos)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_no_queries_no_keys_no_batch(dtype):
     rp, dt = P.RelPos(8, 20), DT[dtype]
