@@ -62,8 +62,8 @@ XDqPlan xattn_dq_plan(int B, int H, int Sq, int Sk, int causal, bool bias, stage
 XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, bool bias,
                       const XDqPlan& dq, stage_dtype dt);
 // Whether one kernel makes all of a backward's results (up to the sum of dK's splits).
-int xattn_one_launch(int B, int H, int G, int Sq, int Sk, bool bias, const XDqPlan& dq,
-                     const XKvPlan& kv, stage_dtype dt);
+int xattn_one_launch(int B, int H, int G, int Sq, int Sk, const XDqPlan& dq, const XKvPlan& kv,
+                     stage_dtype dt);
 inline int xattn_dq_row(stage_dtype dt) { return dt == STAGE_BF16 ? 132 : 64; }
 
 // The forward kernel that serves few queries (xattn_few.hip): wavefronts of a

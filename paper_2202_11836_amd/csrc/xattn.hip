@@ -642,9 +642,11 @@ __device__ __forceinline__ void x_dtable_sum(const XAttnArgs& a, int w, float* r
 // D of the x_qb<T>() queries of head h from q0 on, into own (0 behind the last): fp32
 // rowsum(dO * out); bf16 sum(P dP) / sum(P) over all keys, since out's rounding would go
 // into dK (9 queries over 17 keys: its error 1.6 times that of fp32 sums rounded once).
-template <typename T>
+// With a bias, dist and far_l, far_r are head h's.
+template <typename T, bool BIAS>
 __device__ __forceinline__ void x_own_d(const XAttnArgs& a, int b, int g, int h, int q0, int qp,
-                                        char* ring, float* own, int wave, int lane) {
+                                        char* ring, float* own, const float* dist, float far_l,
+                                        float far_r, int wave, int lane) {
   constexpr int QB = x_qb<T>(), TILE = XKT * XT<T>::ROWB;
   const int hf = lane >> 5, rr = lane & 31, w0 = q0 + 32 * wave, q = w0 + rr;
   const bool qv = q < a.Sq && 32 * wave < QB;
@@ -697,9 +699,19 @@ __device__ __forceinline__ void x_own_d(const XAttnArgs& a, int b, int g, int h,
         const f32x16_t dp = x_mma_rows(kv + TILE, 32 * sub, dof, zero16(), lane);
         uint32_t bits = x_lane_bits(rows, hf);
         if (a.causal) bits &= x_upto(p0 + rr - k0 - 4 * hf);
+        if (BIAS && k0 + 31 - p0 > -a.reach && k0 - p0 - 31 < a.reach) {
+          const float* d = dist + x_idx(k0 + 4 * hf - p0 - rr + a.reach + XPAD);
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, d[8 * (r >> 2) + (r & 3)]) - lse2);
+        } else {
+          const float add = (!BIAS ? 0.0f : k0 > p0 ? far_r : far_l) - lse2;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, add));
+        }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = x_or_zero(__builtin_amdgcn_exp2f(fmaf(s[r], a.c, -lse2)), bits, r);
+          s[r] = x_or_zero(s[r], bits, r);
           D = fmaf(s[r], dp[r], D);
           rsum += s[r];
         }
@@ -721,8 +733,8 @@ template <typename T, bool BIAS, int QS, bool OWN_D>
 __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char* lds) {
   constexpr int QB = x_qb<T>(), TILE = QB * XT<T>::ROWB, KB = XQB / QS, KW = 4 / QS;
   float* rowv = (float*)(lds + 4 * TILE);
-  float* dist = (float*)(lds + kv_lds<T>());
-  float* own = dist;  // OWN_D: [iteration][QB]
+  float* own = (float*)(lds + kv_lds<T>());  // OWN_D: [iteration][QB]
+  float* dist = own + (OWN_D ? XOWN : 0);
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, rr = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int kblk, bg;
@@ -781,19 +793,30 @@ __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char
   const typename XT<T>::Frag vf = x_frag(
       (const T*)a.v + b * a.sv[0] + (int64_t)key * a.sv[1] + g * a.sv[2], kvalid && it0 < n_it, hf);
   if (it0 < n_it) dma(it0, lds);
+  const int mid = a.reach + XPAD;
+  float far_l = 0.0f, far_r = 0.0f;
+  int cur_h = -1;  // whose tables are there
+  auto tables = [&](int h) {
+    cur_h = h;
+    x_fill_dist(a, h, dist);
+    far_l = a.table[(int64_t)x_bucket(a, -a.reach) * a.H + h] * XLOG2E;
+    far_r = a.table[(int64_t)x_bucket(a, a.reach) * a.H + h] * XLOG2E;
+  };
   if constexpr (OWN_D) {
-    for (int it = it0; it < n_it; ++it)
-      x_own_d<T>(a, b, g, head(it), qrow(it), qp, lds + 2 * TILE, own + (it - it0) * QB, wave, lane);
+    for (int it = it0; it < n_it; ++it) {
+      if constexpr (BIAS && sizeof(T) == 2) {
+        if (cur_h != head(it)) tables(head(it));
+      }
+      x_own_d<T, BIAS>(a, b, g, head(it), qrow(it), qp, lds + 2 * TILE, own + (it - it0) * QB, dist,
+                       far_l, far_r, wave, lane);
+    }
     __syncthreads();
   }
   if (it0 < n_it) {
     row_store(row_raw(it0), 0);
     if (it0 + 1 < n_it) raw = row_raw(it0 + 1);
   }
-  const int mid = a.reach + XPAD;
-  float far_l = 0.0f, far_r = 0.0f;
   f32x16_t dv[2] = {zero16(), zero16()}, dk[2] = {zero16(), zero16()};
-  int cur_h = -1;
   for (int it = it0; it < n_it; ++it) {
     const int st = (it - it0) & 1;
     const int h = head(it), qr = qrow(it);
@@ -802,10 +825,7 @@ __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char
     if constexpr (BIAS) {
       if (h != cur_h) {
         // (every wavefront is past its last use of the previous head's table)
-        cur_h = h;
-        x_fill_dist(a, h, dist);
-        far_l = a.table[(int64_t)x_bucket(a, -a.reach) * a.H + h] * XLOG2E;
-        far_r = a.table[(int64_t)x_bucket(a, a.reach) * a.H + h] * XLOG2E;
+        tables(h);
         __syncthreads();
       }
     }
@@ -910,17 +930,23 @@ __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_k
 }
 
 // The whole backward pass in one launch: work-groups from n_kv on make dQ.
-template <typename T, int QS>
+template <typename T, bool BIAS, int QS>
 __global__ __launch_bounds__(256, 2) void xattn_bwd_kernel(XAttnArgs a, int n_kv) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  if ((int)blockIdx.x < n_kv) x_dkdv<T, false, QS, true>(a, blockIdx.x, n_kv, lds);
-  else x_dq<T, false, false, 2>(a, blockIdx.x - n_kv, gridDim.x - n_kv, lds);
+  if ((int)blockIdx.x < n_kv) x_dkdv<T, BIAS, QS, true>(a, blockIdx.x, n_kv, lds);
+  else x_dq<T, BIAS, BIAS && sizeof(T) == 2, 2>(a, blockIdx.x - n_kv, gridDim.x - n_kv, lds);
 }
 
-// dK and dV from their splits, in order: 32 threads to a key, 4 values each.
+// dK and dV from their splits, in order: 32 threads to a key, 4 values each.  Work-groups
+// from n_sum on sum the bias gradient.
 template <typename T>
-__global__ __launch_bounds__(256) void xattn_kv_sum_kernel(XAttnArgs a) {
+__global__ __launch_bounds__(256) void xattn_kv_sum_kernel(XAttnArgs a, int n_sum) {
   constexpr int QB = x_qb<T>();
+  __shared__ float red[32];
+  if ((int)blockIdx.x >= n_sum) {
+    x_dtable_sum(a, blockIdx.x - n_sum, red);
+    return;
+  }
   const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), n = (int64_t)a.B * a.G * a.Sk;
   if (row >= n) return;
   const int key = (int)(row % a.Sk), bg = (int)(row / a.Sk), b = bg / a.G, g = bg % a.G;
@@ -983,24 +1009,34 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
   const int kb = XQB / a.kv_qs;
   const int64_t n_kv = (int64_t)a.B * a.G * ((a.Sk + kb - 1) / kb) * a.kv_splits;
   const int64_t gq = (int64_t)a.B * a.H * ((a.Sq + qb - 1) / qb) * a.dq_splits;
+  const int64_t n_red = a.dtable ? (int64_t)((a.nb + 7) / 8) * a.H : 0;
+  const int64_t n_sum = a.kv_splits > 1 ? ((int64_t)a.B * a.G * a.Sk + 7) / 8 : 0;
+  // dQ: [2][K, V]; with a bias: dist, sums by distance and by bucket of 4 wavefronts
+  size_t dq_lds = 4 * XKT * XT<T>::ROWB;
+  if (a.table) dq_lds += dist_bytes(a) + 4 * (size_t)(2 * (a.reach + XPAD) + 1 + a.nb) * 4;
+  auto sums = [&](int64_t red) {
+    hipLaunchKernelGGL(xattn_kv_sum_kernel<T>, dim3((unsigned)(n_sum + red)), dim3(256), 0, st, a,
+                       (int)n_sum);
+    return hipGetLastError();
+  };
   constexpr int QS2 = sizeof(T) == 4 ? 2 : 1;
   if (a.one_launch) {
     const dim3 grid((unsigned)(n_kv + gq));
-    const size_t lds = kv_lds<T>() + XOWN * 4;
+    const size_t lds = std::max(kv_lds<T>() + XOWN * 4 + dist_bytes(a), dq_lds);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), lds, st, a, (int)n_kv); };
     if (a.kv_qs == 1)
-      hipLaunchKernelGGL((xattn_bwd_kernel<T, 1>), grid, dim3(256), lds, st, a, (int)n_kv);
+      a.table ? go(xattn_bwd_kernel<T, true, 1>) : go(xattn_bwd_kernel<T, false, 1>);
     else
-      hipLaunchKernelGGL((xattn_bwd_kernel<T, QS2>), grid, dim3(256), lds, st, a, (int)n_kv);
-    if ((e = hipGetLastError()) != hipSuccess || a.kv_splits == 1) return e;
-    return launch(xattn_kv_sum_kernel<T>, ((int64_t)a.B * a.G * a.Sk + 7) / 8, 0, st, a);
+      a.table ? go(xattn_bwd_kernel<T, true, QS2>) : go(xattn_bwd_kernel<T, false, QS2>);
+    if ((e = hipGetLastError()) != hipSuccess || n_sum + n_red == 0) return e;
+    return sums(n_red);
   }
   if (gq > 0) {
     // The bias gradient is a sum of many dS that nearly cancel, in fp32: with D from
     // a bf16 out it would be off by out's rounding.
     constexpr bool BF = sizeof(T) == 2;
     const bool red = BF && a.dtable;
-    size_t lds = 4 * XKT * XT<T>::ROWB;
-    if (a.table) lds += dist_bytes(a) + 4 * (size_t)(2 * (a.reach + XPAD) + 1 + a.nb) * 4;
+    const size_t lds = dq_lds;
     if (a.dq_ks == 1)
       e = !a.table ? launch(xattn_dq_kernel<T, false, false, 1>, gq, lds, st, a)
           : red    ? launch(xattn_dq_kernel<T, true, BF, 1>, gq, lds, st, a)
@@ -1013,7 +1049,6 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
       e = launch(xattn_dq_sum_kernel<T>, ((int64_t)a.B * a.H * a.Sq + 15) / 16, 0, st, a);
     if (e != hipSuccess) return e;
   }
-  const int64_t n_red = a.dtable ? (int64_t)((a.nb + 7) / 8) * a.H : 0;
   if (n_kv + n_red == 0) return e;
   const size_t lds = kv_lds<T>() + dist_bytes(a);
   const dim3 grid((unsigned)(n_kv + n_red));
@@ -1029,7 +1064,7 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
       hipLaunchKernelGGL((xattn_dkdv_kernel<T, false, QS2>), grid, dim3(256), lds, st, a, (int)n_kv);
   }
   if ((e = hipGetLastError()) != hipSuccess || a.kv_splits == 1) return e;
-  return launch(xattn_kv_sum_kernel<T>, ((int64_t)a.B * a.G * a.Sk + 7) / 8, 0, st, a);
+  return sums(0);
 }
 
 }  // namespace
@@ -1091,9 +1126,9 @@ double xattn_fwd_time(int B, int H, int Sq, int Sk, int causal, stage_dtype dt, 
 // 16 of 128 35.9 and 47.9.  bf16 work-groups go through all keys for D: 4 x 16 of 32 over
 // 300 14.5 and 15.6, of 100 over 700 33.6 and 26; two blocks of queries (4 x 16 of 256) 26.5
 // and 20.6.
-int xattn_one_launch(int B, int H, int G, int Sq, int Sk, bool bias, const XDqPlan& dq,
-                     const XKvPlan& kv, stage_dtype dt) {
-  if (bias || dq.splits != 1 || dq.ks != 2 || Sq == 0 || Sk == 0) return 0;
+int xattn_one_launch(int B, int H, int G, int Sq, int Sk, const XDqPlan& dq, const XKvPlan& kv,
+                     stage_dtype dt) {
+  if (dq.splits != 1 || dq.ks != 2 || B == 0 || Sq == 0 || Sk == 0) return 0;
   if (kv.chunk * kv.rows > XOWN) return 0;
   if (dt == STAGE_BF16 && (kv.chunk > 1 || Sk > 6 * XKT)) return 0;
   const int kb = XQB / kv.qs;
@@ -1125,7 +1160,7 @@ XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, bool bi
     const int64_t all = wgs * its / (causal ? 2 : 1);
     const int64_t chunk = std::max<int64_t>((all + slots - 1) / slots, 1);
     const XKvPlan split = {rows, (int)chunk, (int)((its + chunk - 1) / chunk), 1};
-    if (bias || full >= 4 * rows || xattn_one_launch(B, G * rep, G, Sq, Sk, bias, dq, split, dt))
+    if (bias || full >= 4 * rows || xattn_one_launch(B, G * rep, G, Sq, Sk, dq, split, dt))
       plan = split;
   }
   // fp32: half as many keys to a work-group, two wavefronts to 32 of them, where that

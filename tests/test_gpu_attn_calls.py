@@ -450,3 +450,16 @@ def test_threads():
     assert not errors, errors
     for g, w in zip(got, want):
         assert len(g) == len(w) and all(torch.equal(x, y) for x, y in zip(g, w))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Sq,Sk", [(0, 5, 5), (0, 300, 700), (2, 0, 5), (2, 5, 0), (0, 0, 0)])
+@pytest.mark.parametrize("relpos", [None, (8, 20, True)])
+def test_nothing_to_do(dtype, B, Sq, Sk, relpos):
+    q, k = rand((B, Sq, 4, 64), 1, dtype), rand((B, Sk, 2, 64), 2, dtype)
+    rp = P.RelPos(*relpos) if relpos else None
+    table = rand((8, 4), 3) if relpos else None
+    out, lse = P.attn_forward(q, k, k.clone(), relpos=rp, table=table)
+    assert out.shape == q.shape and not out.any() and bool((lse == float("-inf")).all())
+    dq, dk, dv, dt = P.attn_backward(q, k, k.clone(), out, lse, q.clone(), relpos=rp, table=table)
+    assert not dq.any() and not dk.any() and not dv.any() and (dt is None or not dt.any())
