@@ -61,7 +61,8 @@ struct XDqPlan {
 XDqPlan xattn_dq_plan(int B, int H, int Sq, int Sk, int causal, bool bias, stage_dtype dt);
 XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, bool bias,
                       const XDqPlan& dq, stage_dtype dt);
-// Whether one kernel makes all of a backward's results (up to the sum of dK's splits).
+// Whether one kernel makes all of a backward's results, up to the sums of dK's splits and of
+// the bias's gradient.
 int xattn_one_launch(int B, int H, int G, int Sq, int Sk, const XDqPlan& dq, const XKvPlan& kv,
                      stage_dtype dt);
 inline int xattn_dq_row(stage_dtype dt) { return dt == STAGE_BF16 ? 132 : 64; }

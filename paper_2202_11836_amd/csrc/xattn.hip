@@ -1120,12 +1120,14 @@ double xattn_fwd_time(int B, int H, int Sq, int Sk, int causal, stage_dtype dt, 
   return std::min(t1, t2);
 }
 
-// Few work-groups and no bias: both parts of the backward in one launch, which saves the
-// second one and the wait for the first.  us in one and in two: 2 x 8 heads of 64 queries
-// and keys 9.4 and 12.1, fp32 13.9 and 22.6; 3 x 12 of 77 over 201 14 and 16.5; fp32, 10 x
-// 16 of 128 35.9 and 47.9.  bf16 work-groups go through all keys for D: 4 x 16 of 32 over
-// 300 14.5 and 15.6, of 100 over 700 33.6 and 26; two blocks of queries (4 x 16 of 256) 26.5
-// and 20.6.
+// Few work-groups: both parts of the backward in one launch, which saves the second one and
+// the wait for the first; a bias's gradient is then summed in the next launch, beside the
+// sums of the chunks.  us in two launches and in one (with a bias, in one more each): 2 x 8
+// heads of 64 queries and keys 12.1 and 9.4, fp32 22.6 and 13.9; 3 x 12 of 77 over 201 16.5
+// and 14; fp32, 10 x 16 of 128 47.9 and 35.9; with a bias 2 x 8 of 128 21.6 and 16.9, fp32
+// 36.9 and 23.6, 10 x 16 of 128 25 and 20.2.  bf16 work-groups go through all keys for D:
+// 4 x 16 of 32 over 300 15.6 and 14.5, of 100 over 700 26 and 33.6; two blocks of queries
+// (4 x 16 of 256) 20.6 and 26.5.
 int xattn_one_launch(int B, int H, int G, int Sq, int Sk, const XDqPlan& dq, const XKvPlan& kv,
                      stage_dtype dt) {
   if (dq.splits != 1 || dq.ks != 2 || B == 0 || Sq == 0 || Sk == 0) return 0;
@@ -1154,13 +1156,19 @@ XKvPlan xattn_kv_plan(int B, int G, int rep, int Sq, int Sk, int causal, bool bi
   // (A block of few queries costs less, so four full ones: 8 x 16 heads over 4, 32 queries
   // over 300 keys, 30 us in four chunks, 19 in one.  But with a bias each head's table is
   // made: 3 x 8 over 2, 56 queries and keys, 20 and 9.6 + 3.9; and what one launch holds
-  // runs beside dQ: 4 x 8 over 2, 22 over 27, dQ and all 14.3 and 10.4, fp32 26 and 13.)
-  if (wgs * 2 <= slots && wgs > 0 && its >= 4) {
+  // runs beside dQ: 4 x 8 over 2, 22 over 27, dQ and all 14.3 and 10.4, fp32 26 and 13.
+  // Two or three blocks for that alone: bf16 with a bias, 1 x 6 over 3 of 128, 25.7 and 17.4,
+  // 2 x 8 of 200 28.5 and 21.3; without, 16.9 and 14.2, but 8 x 12 over 6 of 128, more
+  // work-groups than CUs, 17 and 18.9.)
+  if (wgs * 2 <= slots && wgs > 0 && its >= 2) {
     const int64_t full = (int64_t)((std::min(Sq, rows) + 31) / 32) * 32 * its;
     const int64_t all = wgs * its / (causal ? 2 : 1);
     const int64_t chunk = std::max<int64_t>((all + slots - 1) / slots, 1);
     const XKvPlan split = {rows, (int)chunk, (int)((its + chunk - 1) / chunk), 1};
-    if (bias || full >= 4 * rows || xattn_one_launch(B, G * rep, G, Sq, Sk, dq, split, dt))
+    const int64_t both = wgs * split.splits +
+                         (int64_t)B * G * rep * ((Sq + XQB / 2 - 1) / (XQB / 2));
+    const bool one = xattn_one_launch(B, G * rep, G, Sq, Sk, dq, split, dt);
+    if (its >= 4 ? bias || full >= 4 * rows || one : one && (bias || both <= cus))
       plan = split;
   }
   // fp32: half as many keys to a work-group, two wavefronts to 32 of them, where that

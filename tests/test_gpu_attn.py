@@ -204,6 +204,17 @@ def test_shared_key_heads_of_few_queries(dtype, shape, mask, garbage, causal, q_
         q_pos=None if q_pos is None else q_pos[:shape[0]], relpos=relpos)
 
 
+# (each block to a work-group of its own, beside those of dQ)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 6, 3, 130, 128), (2, 4, 4, 200, 200), (3, 2, 1, 129, 300),
+                                   (1, 3, 1, 20, 70), (2, 3, 3, 300, 90)])
+@pytest.mark.parametrize("mask,garbage", [("none", False), ("empty", True), ("blocks", True)])
+@pytest.mark.parametrize("causal,relpos", [(False, None), (True, None), (False, (32, 128, True)),
+                                           (True, (32, 128, False))])
+def test_two_or_three_blocks_of_queries(dtype, shape, mask, garbage, causal, relpos):
+    run(dtype, *shape, mask=mask, garbage=garbage, causal=causal, relpos=relpos)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_no_queries_no_keys_no_batch(dtype):
     rp, dt = P.RelPos(8, 20), DT[dtype]
