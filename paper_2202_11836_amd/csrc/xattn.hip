@@ -351,8 +351,10 @@ __device__ __forceinline__ void x_dq(const XAttnArgs& a, int w, int n, char* lds
   const typename XT<T>::Frag dof = x_frag(
       (const T*)a.dout + b * a.sdo[0] + (int64_t)q * a.sdo[1] + h * a.sdo[2], qv, hf);
   const int64_t row = ((int64_t)b * a.H + h) * a.Sq + q;
-  float lse2 = qv ? a.lse[row] * XLOG2E : 0.0f;
-  if (lse2 == -INFINITY) lse2 = INFINITY;  // no key: P = exp2(s - inf) = 0
+  // No key, and lanes behind the last query (whose sums by bucket, over all lanes, a bias
+  // beyond 2^128 would make NaN): P = exp2(s - inf) = 0.
+  float lse2 = qv ? a.lse[row] * XLOG2E : INFINITY;
+  if (lse2 == -INFINITY) lse2 = INFINITY;
   float D = 0.0f;
   typename XT<T>::Frag of;
   if constexpr (!RED)
@@ -669,7 +671,7 @@ __device__ __forceinline__ void x_own_d(const XAttnArgs& a, int b, int g, int h,
     const int lim = a.causal ? max(0, min(a.Sk, min(q0 + QB, a.Sq) + qp)) : a.Sk;
     const typename XT<T>::Frag qf = x_frag(
         (const T*)a.q + b * a.sq[0] + (int64_t)q * a.sq[1] + h * a.sq[2], qv, hf);
-    float lse2 = qv ? a.lse[((int64_t)b * a.H + h) * a.Sq + q] * XLOG2E : 0.0f;
+    float lse2 = qv ? a.lse[((int64_t)b * a.H + h) * a.Sq + q] * XLOG2E : INFINITY;
     if (lse2 == -INFINITY) lse2 = INFINITY;
     KeyBlocks<XKT> blocks;
     int kb = x_start(a, b, K, V, lim, 0, (lim + XKT - 1) / XKT, ring, wave, lane, blocks);

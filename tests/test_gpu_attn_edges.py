@@ -1,0 +1,50 @@
+"""The attention operators where values or shapes are at an edge: biases beyond fp32's
+exponent, queries behind the last one and queries that see no key."""
+import pytest
+import torch
+
+import paper_2202_11836_amd as P
+from _attn_ref import check, reference
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def rand(shape, seed, dtype="f32"):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(shape, generator=g).to(DT[dtype]).cuda()
+
+
+def both(q, k, v, do, relpos=None, **kw):
+    """Forward and backward: results by name."""
+    rp = P.RelPos(*relpos) if relpos else None
+    out, lse = P.attn_forward(q, k, v, relpos=rp, **kw)
+    got = dict(zip(("dq", "dk", "dv", "dtable"),
+                   P.attn_backward(q, k, v, out, lse, do, relpos=rp, **kw)), out=out, lse=lse)
+    torch.cuda.synchronize()
+    return got
+
+
+# (batch, heads, key heads, queries, keys): one launch for the whole backward; two, by the
+# number of work-groups and by the number of keys; two wavefronts to 32 queries and one
+SHAPES = [(2, 2, 2, 33, 70), (2, 4, 2, 70, 33), (17, 16, 16, 33, 40), (2, 2, 1, 70, 450),
+          (9, 16, 16, 300, 130)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("relpos,causal", [((32, 128, True), False), ((8, 20, True), False),
+                                           ((32, 128, False), True)])
+def test_biases_beyond_the_exponent(dtype, shape, relpos, causal):
+    """A constant added to the bias is none to the softmax, however large: exp(100) is
+    beyond fp32, and a work-group has lanes behind the last query whose log-sum-exp nothing
+    takes off."""
+    B, H, G, Sq, Sk = shape
+    q, do = rand((B, Sq, H, 64), 1, dtype), rand((B, Sq, H, 64), 2, dtype)
+    k, v = rand((B, Sk, G, 64), 3, dtype), rand((B, Sk, G, 64), 4, dtype)
+    table = rand((relpos[0], H), 5) + 100.0
+    kw = dict(table=table, causal=causal)
+    got = both(q, k, v, do, relpos=relpos, **kw)
+    want = reference(q, k, v, relpos=relpos, dout=do, **kw)
+    for n in want:
+        check(n, got[n], want[n])
