@@ -11,7 +11,7 @@
  *     out_i = sum_j P_ij v_j,      lse_i = log sum_j exp(s_ij)
  * i sees j if key_mask[b][j] != 0 and, with `causal`, j <= i + p_b.  The bias
  * term is there only with a table.  A query that sees no key gets out = 0 and
- * lse = -inf, and adds nothing to any gradient.
+ * lse = -inf, and adds nothing to any gradient, whatever its q and dout hold.
  *
  * The backward pass of <out, dout>, with D_i = sum_j P_ij (dout_i . v_j) and
  * dS_ij = P_ij (dout_i . v_j - D_i):

@@ -5,6 +5,8 @@
 #include "../../include/attn.h"
 #include "attn_tile.h"
 
+#include <climits>
+
 struct XAttnArgs {
   const void* q;
   const void* k;
@@ -141,10 +143,11 @@ __device__ __forceinline__ int x_off(int r, int c) {
 
 // Rows [row0, row0 + NR) of a [lim][64] operand into a tile with direct-to-LDS
 // loads by NW wavefronts; rows from lim on are zero.  The buffer resource starts at
-// row0, so the operand may be of any length.  STREAM: marked as read once.
-template <typename T, int NR, int NW, bool STREAM = false>
+// row0, so the operand may be of any length.  STREAM: marked as read once.  SKIP: the
+// tile's rows before `skip` are not read, and zero.
+template <typename T, int NR, int NW, bool STREAM = false, bool SKIP = false>
 __device__ __forceinline__ void x_dma(const T* base, int64_t ld, int row0, int lim, char* tile,
-                                      int wave, int lane) {
+                                      int wave, int lane, int skip = 0) {
   constexpr int RPI = 1024 / XT<T>::ROWB, CPR = XT<T>::CPR;
   const int n = min(NR, lim - row0);
   const int bytes = n > 0 ? ((n - 1) * (int)ld + XHD) * (int)sizeof(T) : 0;
@@ -155,8 +158,9 @@ __device__ __forceinline__ void x_dma(const T* base, int64_t ld, int row0, int l
     const int q = NR / RPI / NW * wave + i;
     const int r = RPI * q + lane / CPR;
     const int c = (lane % CPR) ^ XT<T>::swz(r);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_t*)(tile + q * 1024), 16,
-                                             r * (int)ld * (int)sizeof(T) + 16 * c, 0, 0,
+    // (`bytes` is below 2^31)
+    const int at = SKIP && r < skip ? INT_MIN : r * (int)ld * (int)sizeof(T) + 16 * c;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_t*)(tile + q * 1024), 16, at, 0, 0,
                                              STREAM ? 2 /* nt */ : 0);
   }
 }

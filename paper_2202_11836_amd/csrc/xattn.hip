@@ -307,6 +307,18 @@ __device__ __forceinline__ void x_add_buckets(const XAttnArgs& a, float v, int r
   __builtin_amdgcn_wave_barrier();
 }
 
+// A query that sees no key adds nothing, whatever its dO holds (0 * NaN is NaN): its
+// fragment becomes zeros.  lse2: infinite for such a row.
+template <typename F>
+__device__ __forceinline__ void x_drop_empty(F& dof, float lse2) {
+  const bool empty = lse2 == INFINITY;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(dof) / 16); ++i) {
+    const u32x4_t w = __builtin_bit_cast(u32x4_t, dof.f[i]);
+    dof.f[i] = __builtin_bit_cast(decltype(dof.f[0] + dof.f[0]), empty ? zero4() : w);
+  }
+}
+
 // KS = 2: two wavefronts share 32 queries, one with the first 32 keys of each block
 // and one with the others, and add up at the end; a work-group has 64 queries then.
 template <typename T, bool BIAS, bool RED, int KS>
@@ -348,7 +360,7 @@ __device__ __forceinline__ void x_dq(const XAttnArgs& a, int w, int n, char* lds
 
   const typename XT<T>::Frag qf = x_frag(
       (const T*)a.q + b * a.sq[0] + (int64_t)q * a.sq[1] + h * a.sq[2], qv, hf);
-  const typename XT<T>::Frag dof = x_frag(
+  typename XT<T>::Frag dof = x_frag(
       (const T*)a.dout + b * a.sdo[0] + (int64_t)q * a.sdo[1] + h * a.sdo[2], qv, hf);
   const int64_t row = ((int64_t)b * a.H + h) * a.Sq + q;
   // No key, and lanes behind the last query (whose sums by bucket, over all lanes, a bias
@@ -363,6 +375,7 @@ __device__ __forceinline__ void x_dq(const XAttnArgs& a, int w, int n, char* lds
   KeyBlocks<XKT> blocks;
   int kb = x_start(a, b, K, V, lim, first, last, lds, wave, lane, blocks);
   if constexpr (!RED) {
+    x_drop_empty(dof, lse2);
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(of) / 16); ++i)
 #pragma unroll
@@ -380,6 +393,7 @@ __device__ __forceinline__ void x_dq(const XAttnArgs& a, int w, int n, char* lds
     for (int i = lane; i < nd; i += 64) diag[i] = 0.0f;
     for (int i = lane; i < a.nb; i += 64) bsum[i] = 0.0f;
   }
+  if constexpr (RED) x_drop_empty(dof, lse2);
 
   // Sum of a value over the wavefronts that share the queries (in the ring's place,
   // after the pass's last barrier), the same in both.
@@ -641,9 +655,10 @@ __device__ __forceinline__ void x_dtable_sum(const XAttnArgs& a, int w, float* r
         (red[threadIdx.x] + red[8 + threadIdx.x]) + (red[16 + threadIdx.x] + red[24 + threadIdx.x]);
 }
 
-// D of the x_qb<T>() queries of head h from q0 on, into own (0 behind the last): fp32
-// rowsum(dO * out); bf16 sum(P dP) / sum(P) over all keys, since out's rounding would go
-// into dK (9 queries over 17 keys: its error 1.6 times that of fp32 sums rounded once).
+// D of the x_qb<T>() queries of head h from q0 on, into own (0 behind the last, and where
+// no key is seen): fp32 rowsum(dO * out); bf16 sum(P dP) / sum(P) over all keys, since out's
+// rounding would go into dK (9 queries over 17 keys: its error 1.6 times that of fp32 sums
+// rounded once).
 // With a bias, dist and far_l, far_r are head h's.
 template <typename T, bool BIAS>
 __device__ __forceinline__ void x_own_d(const XAttnArgs& a, int b, int g, int h, int q0, int qp,
@@ -654,6 +669,8 @@ __device__ __forceinline__ void x_own_d(const XAttnArgs& a, int b, int g, int h,
   const bool qv = q < a.Sq && 32 * wave < QB;
   const typename XT<T>::Frag dof = x_frag(
       (const T*)a.dout + b * a.sdo[0] + (int64_t)q * a.sdo[1] + h * a.sdo[2], qv, hf);
+  float lse2 = qv ? a.lse[((int64_t)b * a.H + h) * a.Sq + q] * XLOG2E : INFINITY;
+  if (lse2 == -INFINITY) lse2 = INFINITY;
   float D = 0.0f;
   if constexpr (sizeof(T) == 4) {
     const typename XT<T>::Frag of = x_frag(
@@ -671,8 +688,6 @@ __device__ __forceinline__ void x_own_d(const XAttnArgs& a, int b, int g, int h,
     const int lim = a.causal ? max(0, min(a.Sk, min(q0 + QB, a.Sq) + qp)) : a.Sk;
     const typename XT<T>::Frag qf = x_frag(
         (const T*)a.q + b * a.sq[0] + (int64_t)q * a.sq[1] + h * a.sq[2], qv, hf);
-    float lse2 = qv ? a.lse[((int64_t)b * a.H + h) * a.Sq + q] * XLOG2E : INFINITY;
-    if (lse2 == -INFINITY) lse2 = INFINITY;
     KeyBlocks<XKT> blocks;
     int kb = x_start(a, b, K, V, lim, 0, (lim + XKT - 1) / XKT, ring, wave, lane, blocks);
     float rsum = 0.0f;
@@ -725,15 +740,40 @@ __device__ __forceinline__ void x_own_d(const XAttnArgs& a, int b, int g, int h,
     const float top = pr.x + pr.y, total = ps.x + ps.y;
     D = total == 0.0f ? 0.0f : top / total;
   }
-  if (hf == 0 && 32 * wave < QB) own[32 * wave + rr] = qv ? D : 0.0f;
+  if (hf == 0 && 32 * wave < QB) own[32 * wave + rr] = lse2 == INFINITY ? 0.0f : D;
+}
+
+// The first query from row0 on, of the next 256, that some head of key head g has a
+// log-sum-exp for: with `causal`, those further on that meet the work-group's keys are
+// behind one of them.  (Loads without conditions, so that they are on their way together.)
+__device__ __forceinline__ int x_first_seen(const XAttnArgs& a, int b, int g, int row0, int lane) {
+  bool none[4] = {true, true, true, true};
+  int at[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) at[j] = min(row0 + 64 * j + lane, a.Sq - 1);
+  const float* l = a.lse + ((int64_t)b * a.H + g * a.rep) * a.Sq;
+#pragma unroll 4
+  for (int h = 0; h < a.rep; ++h, l += a.Sq) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) none[j] &= l[at[j]] == -INFINITY;
+  }
+  int n = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint64_t seen = ~__ballot(none[j]);
+    if (n == 64 * j) n += seen ? __builtin_ctzll(seen) : 64;
+  }
+  return row0 + n;
 }
 
 // QS = 2: two wavefronts share 32 keys, each with every other tile of queries, and add
 // up at the end; a work-group has 64 keys then.
-// OWN_D: D is formed here, for all queries of the work-group, and not read.
-template <typename T, bool BIAS, int QS, bool OWN_D>
+// CAUSAL: a.causal may be set.  OWN_D: D is formed here, for all queries of the work-group,
+// and not read.
+template <typename T, bool BIAS, int QS, bool CAUSAL, bool OWN_D>
 __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char* lds) {
   constexpr int QB = x_qb<T>(), TILE = QB * XT<T>::ROWB, KB = XQB / QS, KW = 4 / QS;
+  const bool causal = CAUSAL && a.causal;
   float* rowv = (float*)(lds + 4 * TILE);
   float* own = (float*)(lds + kv_lds<T>());  // OWN_D: [iteration][QB]
   float* dist = own + (OWN_D ? XOWN : 0);
@@ -747,7 +787,7 @@ __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char
   const int k0 = kblk * KB + wave % KW * 32, key = k0 + rr, qs = wave / KW;
   const int qp = x_q_pos(a, b);
   // Queries from q_first on see a key of this work-group, those before it none.
-  const int q_first = a.causal ? max(0, kblk * KB - qp) : 0;
+  const int q_first = causal ? max(0, kblk * KB - qp) : 0;
   const int qb0 = q_first / QB, nqb = max(0, (a.Sq + QB - 1) / QB - qb0);
   const int it0 = split * a.kv_chunk;
   int n_it = min(nqb * a.rep, it0 + a.kv_chunk);
@@ -756,8 +796,13 @@ __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char
   // read, and a work-group without another key only writes zeros.  (The rows wait for
   // the mask this way; but few queries make this a copy of K and V to dK and dV: 32 x
   // 16 heads of 128 queries and 512 keys, half of them hidden, 40 -> 36 us.)
-  const bool kvalid = key < a.Sk && (!a.causal || key - qp < a.Sq) &&
-                      (!a.mask || a.mask[(int64_t)b * a.Sk + key] != 0);
+  const int bit = key >= a.Sk ? 0 : a.mask ? a.mask[(int64_t)b * a.Sk + key] : 1;
+  // The queries before the first visible key see none and may hold anything: their rows
+  // are not read.  (Without `causal` the queries of a sequence without a key are not gone
+  // through at all.)
+  int q_seen = !causal || nqb == 0 ? 0 : a.mask ? x_first_seen(a, b, g, qb0 * QB, lane) : -qp;
+  if (causal) asm volatile("" : "+v"(q_seen));  // (in a vector register: scalar ones are short)
+  const bool kvalid = bit != 0 && (!causal || key - qp < a.Sq);
   const bool all_valid = __all(kvalid), any_valid = __any(kvalid);
   const uint32_t kbits = kvalid ? 0xffffffffu : 0u;
   if (a.mask) {
@@ -773,8 +818,9 @@ __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char
   auto qrow = [&](int it) { return (qb0 + it % nqb) * QB; };
   auto dma = [&](int it, char* to) {
     const int h = head(it), r = qrow(it);
-    x_dma<T, QB, 4>(Q + h * a.sq[2], a.sq[1], r, a.Sq, to, wave, lane);
-    x_dma<T, QB, 4>(dO + h * a.sdo[2], a.sdo[1], r, a.Sq, to + TILE, wave, lane);
+    x_dma<T, QB, 4, false, CAUSAL>(Q + h * a.sq[2], a.sq[1], r, a.Sq, to, wave, lane, q_seen - r);
+    x_dma<T, QB, 4, false, CAUSAL>(dO + h * a.sdo[2], a.sdo[1], r, a.Sq, to + TILE, wave, lane,
+                                 q_seen - r);
   };
   // Thread t < QB carries lse (in log2 units) of row t of a block, the next QB
   // threads -D; rows that are not there have P = exp2(s - inf) = 0.
@@ -841,7 +887,7 @@ __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char
       const int sub = QS == 2 ? 2 * i + qs : i;
       const int r0 = qr + 32 * sub;   // first query
       const int p0 = r0 + qp;         // its position
-      if (!any_valid || r0 >= a.Sq || (a.causal && k0 > p0 + 31)) continue;
+      if (!any_valid || r0 >= a.Sq || (causal && k0 > p0 + 31)) continue;
       f32x16_t dp;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -851,11 +897,11 @@ __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char
       }
       f32x16_t s = x_mma_rows(Qs, 32 * sub, kf, zero16(), lane);
       dp = x_mma_rows(dOs, 32 * sub, vf, dp, lane);
-      const bool full = all_valid && (!a.causal || k0 + 31 <= p0);
+      const bool full = all_valid && (!causal || k0 + 31 <= p0);
       const bool near = BIAS && k0 + 31 - p0 > -a.reach && k0 - p0 - 31 < a.reach;
       // Key rr is seen by the queries from rr + k0 - p0 on.
       uint32_t bits = kbits;
-      if (a.causal) bits &= ~x_upto(k0 + rr - p0 - 4 * hf - 1);
+      if (causal) bits &= ~x_upto(k0 + rr - p0 - 4 * hf - 1);
       if constexpr (!BIAS) {
       } else if (near) {
         const float* d = dist + x_idx(k0 + rr - p0 - 4 * hf + mid - 27);
@@ -924,18 +970,18 @@ __device__ __forceinline__ void x_dkdv(const XAttnArgs& a, int w, int n_kv, char
   __builtin_amdgcn_wave_barrier();
   x_store<T>(dv, 1.0f, stage, (T*)a.dv + b * a.sdv[0] + g * a.sdv[2], a.sdv[1], k0, a.Sk);
 }
-template <typename T, bool BIAS, int QS>
+template <typename T, bool BIAS, int QS, bool CAUSAL>
 __global__ __launch_bounds__(256, 2) void xattn_dkdv_kernel(XAttnArgs a, int n_kv) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  if ((int)blockIdx.x < n_kv) x_dkdv<T, BIAS, QS, false>(a, blockIdx.x, n_kv, lds);
+  if ((int)blockIdx.x < n_kv) x_dkdv<T, BIAS, QS, CAUSAL, false>(a, blockIdx.x, n_kv, lds);
   else x_dtable_sum(a, blockIdx.x - n_kv, (float*)lds);
 }
 
 // The whole backward pass in one launch: work-groups from n_kv on make dQ.
-template <typename T, bool BIAS, int QS>
+template <typename T, bool BIAS, int QS, bool CAUSAL>
 __global__ __launch_bounds__(256, 2) void xattn_bwd_kernel(XAttnArgs a, int n_kv) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  if ((int)blockIdx.x < n_kv) x_dkdv<T, BIAS, QS, true>(a, blockIdx.x, n_kv, lds);
+  if ((int)blockIdx.x < n_kv) x_dkdv<T, BIAS, QS, CAUSAL, true>(a, blockIdx.x, n_kv, lds);
   else x_dq<T, BIAS, BIAS && sizeof(T) == 2, 2>(a, blockIdx.x - n_kv, gridDim.x - n_kv, lds);
 }
 
@@ -1004,6 +1050,28 @@ hipError_t forward_t(const XAttnArgs& a, hipStream_t st) {
                  : launch(xattn_fwd_kernel<T, false, KS2>, grid, lds, st, a);
 }
 
+// Kernels that take `causal` keep the first query that sees a key beside what the others
+// keep: dK and dV of 32 x 16 heads of 128 over 512 without `causal` 37.2 us with such a
+// kernel, 35.0 with one of its own.  (fp32 has none: 8 x 12 heads of 128 with a bias take
+// 33.3 either way.)
+typedef void (*KvKernel)(XAttnArgs, int);
+template <typename T, int QS>
+KvKernel dkdv_kernel(const XAttnArgs& a) {
+  if constexpr (sizeof(T) == 2) {
+    if (!a.causal)
+      return a.table ? xattn_dkdv_kernel<T, true, QS, false> : xattn_dkdv_kernel<T, false, QS, false>;
+  }
+  return a.table ? xattn_dkdv_kernel<T, true, QS, true> : xattn_dkdv_kernel<T, false, QS, true>;
+}
+template <typename T, int QS>
+KvKernel bwd_kernel(const XAttnArgs& a) {
+  if constexpr (sizeof(T) == 2) {
+    if (!a.causal)
+      return a.table ? xattn_bwd_kernel<T, true, QS, false> : xattn_bwd_kernel<T, false, QS, false>;
+  }
+  return a.table ? xattn_bwd_kernel<T, true, QS, true> : xattn_bwd_kernel<T, false, QS, true>;
+}
+
 template <typename T>
 hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
   hipError_t e = hipSuccess;
@@ -1025,11 +1093,8 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
   if (a.one_launch) {
     const dim3 grid((unsigned)(n_kv + gq));
     const size_t lds = std::max(kv_lds<T>() + XOWN * 4 + dist_bytes(a), dq_lds);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), lds, st, a, (int)n_kv); };
-    if (a.kv_qs == 1)
-      a.table ? go(xattn_bwd_kernel<T, true, 1>) : go(xattn_bwd_kernel<T, false, 1>);
-    else
-      a.table ? go(xattn_bwd_kernel<T, true, QS2>) : go(xattn_bwd_kernel<T, false, QS2>);
+    hipLaunchKernelGGL(a.kv_qs == 1 ? (bwd_kernel<T, 1>(a)) : (bwd_kernel<T, QS2>(a)), grid, dim3(256),
+                       lds, st, a, (int)n_kv);
     if ((e = hipGetLastError()) != hipSuccess || n_sum + n_red == 0) return e;
     return sums(n_red);
   }
@@ -1054,17 +1119,8 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
   if (n_kv + n_red == 0) return e;
   const size_t lds = kv_lds<T>() + dist_bytes(a);
   const dim3 grid((unsigned)(n_kv + n_red));
-  if (a.kv_qs == 1) {
-    if (a.table)
-      hipLaunchKernelGGL((xattn_dkdv_kernel<T, true, 1>), grid, dim3(256), lds, st, a, (int)n_kv);
-    else
-      hipLaunchKernelGGL((xattn_dkdv_kernel<T, false, 1>), grid, dim3(256), lds, st, a, (int)n_kv);
-  } else {
-    if (a.table)
-      hipLaunchKernelGGL((xattn_dkdv_kernel<T, true, QS2>), grid, dim3(256), lds, st, a, (int)n_kv);
-    else
-      hipLaunchKernelGGL((xattn_dkdv_kernel<T, false, QS2>), grid, dim3(256), lds, st, a, (int)n_kv);
-  }
+  hipLaunchKernelGGL(a.kv_qs == 1 ? (dkdv_kernel<T, 1>(a)) : (dkdv_kernel<T, QS2>(a)), grid, dim3(256),
+                     lds, st, a, (int)n_kv);
   if ((e = hipGetLastError()) != hipSuccess || a.kv_splits == 1) return e;
   return sums(0);
 }

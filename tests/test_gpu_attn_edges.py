@@ -48,3 +48,34 @@ def test_biases_beyond_the_exponent(dtype, shape, relpos, causal):
     want = reference(q, k, v, relpos=relpos, dout=do, **kw)
     for n in want:
         check(n, got[n], want[n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES + [(2, 6, 2, 150, 190), (1, 4, 4, 600, 700)], ids=str)
+@pytest.mark.parametrize("relpos", [None, (32, 128, False), (8, 20, True)])
+@pytest.mark.parametrize("left", [False, True])
+def test_queries_that_see_no_key(dtype, shape, relpos, left):
+    """Before position 0, and before the first key that a mask leaves (sequences padded
+    at their left), a query's q and dout may hold anything."""
+    B, H, G, Sq, Sk = shape
+    q, do = rand((B, Sq, H, 64), 1, dtype), rand((B, Sq, H, 64), 2, dtype)
+    k, v = rand((B, Sk, G, 64), 3, dtype), rand((B, Sk, G, 64), 4, dtype)
+    pos = torch.tensor([(-21, 5, -1, 0, -64)[b % 5] for b in range(B)], dtype=torch.int32)
+    first = torch.zeros(B, dtype=torch.int32)  # visible key
+    mask = None
+    if left:
+        first = torch.tensor([(0, 17, 32, Sk - 1, Sk)[b % 5] for b in range(B)], dtype=torch.int32)
+        mask = (torch.arange(Sk)[None, :] >= first[:, None]).to(torch.uint8).cuda()
+    none = (torch.arange(Sq)[None, :] + pos[:, None] < first[:, None]).cuda()
+    none |= (first == Sk)[:, None].cuda()
+    assert none.any() and not none.all()
+    table = rand((relpos[0], H), 5) if relpos else None
+    kw = dict(causal=True, q_pos=pos.cuda(), key_mask=mask, table=table)
+    bad_q, bad_do = q.clone(), do.clone()
+    bad_q[none], bad_do[none] = float("inf"), float("nan")
+    got = both(bad_q, k, v, bad_do, relpos=relpos, **kw)
+    q[none], do[none] = 0, 0
+    kw["mask"] = kw.pop("key_mask")
+    want = reference(q, k, v, relpos=relpos, dout=do, **kw)
+    for n in want:
+        check(n, got[n], want[n])
