@@ -1072,6 +1072,9 @@ KvKernel bwd_kernel(const XAttnArgs& a) {
   return a.table ? xattn_bwd_kernel<T, true, QS, true> : xattn_bwd_kernel<T, false, QS, true>;
 }
 
+// Floats of 32 fp32 rows for each of a work-group's wavefronts (x_store<float>).
+constexpr size_t XSTAGE = 4 * 32 * XT<float>::LD;
+
 template <typename T>
 hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
   hipError_t e = hipSuccess;
@@ -1081,8 +1084,10 @@ hipError_t backward_t(const XAttnArgs& a, hipStream_t st) {
   const int64_t gq = (int64_t)a.B * a.H * ((a.Sq + qb - 1) / qb) * a.dq_splits;
   const int64_t n_red = a.dtable ? (int64_t)((a.nb + 7) / 8) * a.H : 0;
   const int64_t n_sum = a.kv_splits > 1 ? ((int64_t)a.B * a.G * a.Sk + 7) / 8 : 0;
-  // dQ: [2][K, V]; with a bias: dist, sums by distance and by bucket of 4 wavefronts
+  // dQ: [2][K, V], with splits as large as the wavefronts' fp32 rows; with a bias: dist,
+  // sums by distance and by bucket of 4 wavefronts
   size_t dq_lds = 4 * XKT * XT<T>::ROWB;
+  if (a.dq_splits > 1) dq_lds = std::max<size_t>(dq_lds, XSTAGE * 4);
   if (a.table) dq_lds += dist_bytes(a) + 4 * (size_t)(2 * (a.reach + XPAD) + 1 + a.nb) * 4;
   auto sums = [&](int64_t red) {
     hipLaunchKernelGGL(xattn_kv_sum_kernel<T>, dim3((unsigned)(n_sum + red)), dim3(256), 0, st, a,
