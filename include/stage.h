@@ -194,8 +194,10 @@ stage_status stage_backward_noalloc(stage_t* s, const void* dy, void* dx);
  * the stage's layers (a model that shares one table over several stages sums theirs).
  * A sequence without a valid key attends to nothing, as without the bias.  The
  * table, its gradient and the operators' workspace are held besides what
- * stage_memory_model counts.  EINVAL for buckets attn_relpos_init rejects or a stage
- * without an attention half.
+ * stage_memory_model counts, but past 64 tokens no scores or probabilities on fp32
+ * stages and no rounding residual of the context on bf16 stages: memory is linear in
+ * the sequence length.  EINVAL for buckets attn_relpos_init rejects or a stage without an
+ * attention half.
  */
 stage_status stage_set_relpos(stage_t* s, int num_buckets, int max_distance);
 /* Device pointers (fp32) of the table and of its gradient, and their element count;
@@ -216,7 +218,7 @@ stage_status stage_relpos(stage_t* s, float** table, float** grad, int64_t* nume
  * stage_forward and stage_backward; a context of one kind is not taken by the other
  * kind's backward (ESTATE).  STAGE_SAVED_QKV of such a context is Q alone, [T, h].
  * The memory's copy, keys and values with their gradient are held besides what
- * stage_memory_model counts.
+ * stage_memory_model counts, but no scores, as with a bias.
  */
 stage_status stage_forward_cross(stage_t* s, const void* x, const void* memory,
                                  const uint8_t* key_mask, int batch, int seq, int mem_seq, void* y);

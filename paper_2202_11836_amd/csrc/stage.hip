@@ -107,7 +107,9 @@ struct Saved {
   void* X = nullptr;     // layer input [T, h]
   void* QKV = nullptr;   // [T, 3h]
   void* P = nullptr;     // softmax probabilities [B*H, S, S] (fp32 stages)
-  float* lse = nullptr;  // log2-sum-exp of the scaled scores [B*H, S] (bf16 stages)
+  // log-sum-exp of the scaled scores [B*H, S]: of the attention operators to base e, else
+  // (bf16 stages) to base 2
+  float* lse = nullptr;
   void* C = nullptr;     // context [T, h]
   void* Clo = nullptr;   // its bf16 rounding residual [T, h] (bf16 stages)
   void* xhat1 = nullptr; // [T, h]
@@ -150,8 +152,9 @@ struct stage {
   int64_t bytes_param = 0, bytes_act = 0;
   bool dry_run = false;
 
-  // Activation memory, sized for cap_T tokens and cap_BSS probabilities.
-  int64_t cap_T = -1, cap_BSS = -1, cap_B = -1, cap_NQB = -1;
+  // Activation memory, sized for cap_T tokens, cap_BSS probabilities and the context's
+  // residual of cap_Tlo tokens.
+  int64_t cap_T = -1, cap_BSS = -1, cap_Tlo = -1, cap_B = -1, cap_NQB = -1;
   std::vector<void*> act_allocs;
   std::vector<Saved> saved;
   uint8_t* mask = nullptr;
@@ -337,7 +340,7 @@ void free_activations(stage_t* s) {
   s->splitk = s->scores = s->attn_ws = s->cross_buf = nullptr;
   s->splitk_elems = s->scores_elems = s->attn_ws_elems = s->cross_elems = 0;
   s->splitk_bytes = s->scores_bytes = s->attn_ws_bytes = s->cross_bytes = 0;
-  s->cap_T = s->cap_BSS = s->cap_B = s->cap_NQB = -1;
+  s->cap_T = s->cap_BSS = s->cap_Tlo = s->cap_B = s->cap_NQB = -1;
   s->have_ctx = false;
 }
 
@@ -426,16 +429,21 @@ int64_t colpart_ffn_rows(const stage_t* s, int64_t T) {
   return f32_fused_b1(T) ? (T + 31) / 32 : COL_PARTS;
 }
 
-stage_status ensure_activations(stage_t* s, int B, int S) {
+// ops: the pass takes the attention operators (attn.h), which leave no scores.  (Room for
+// those of up to 64 tokens stays: it is no more than a [T, h] tensor, and a stage whose
+// passes are now of one kind and now of the other keeps what it has.)
+stage_status ensure_activations(stage_t* s, int B, int S, bool ops) {
   const int64_t T = (int64_t)B * S;
+  ops = ops && S > HEAD_DIM;
   // Probabilities (and their gradient) are stored only on fp32 stages, scores
-  // only where their rows do not stay on chip.
-  const int64_t BSS = s->dtype == STAGE_F32 ? (int64_t)B * s->H * S * S : 0;
-  const size_t n_scores = S > ATTN_F32_MAX_S && !s->relpos ? (size_t)BSS : 0;
+  // only where their rows do not stay on chip; the context's residual only on bf16 stages.
+  const int64_t BSS = s->dtype == STAGE_F32 && !ops ? (int64_t)B * s->H * S * S : 0;
+  const int64_t Tlo = s->dtype == STAGE_BF16 && !ops ? T : 0;
+  const size_t n_scores = S > ATTN_F32_MAX_S ? (size_t)BSS : 0;
   const int64_t BHS = (int64_t)B * s->H * S;
   const int64_t NQB = (int64_t)B * ((S + 31) / 32);
   const size_t need = splitk_need(s, T);
-  if (T <= s->cap_T && BSS <= s->cap_BSS && B <= s->cap_B && NQB <= s->cap_NQB &&
+  if (T <= s->cap_T && BSS <= s->cap_BSS && Tlo <= s->cap_Tlo && B <= s->cap_B && NQB <= s->cap_NQB &&
       (int)s->saved.size() == s->L) {
     stage_status st = STAGE_OK;
     if (need > s->splitk_elems) st = grow_splitk(s, need);
@@ -458,7 +466,7 @@ stage_status ensure_activations(stage_t* s, int B, int S) {
          (st = A(&v.P, BSS * e)) || (st = A((void**)&v.lse, BHS * 4)) ||
          (st = A(&v.C, T * h * e)) || (st = A(&v.xhat1, T * h * e)) ||
          (st = A((void**)&v.rstd1, T * 4)) ||
-         (s->dtype == STAGE_BF16 && (st = A(&v.Clo, T * h * e)))))
+         (s->dtype == STAGE_BF16 && (st = A(&v.Clo, Tlo * h * e)))))
       return st;
     if (has_ffn(s, l) &&
         ((st = A(&v.H1, T * h * e)) || (st = A(&v.Gd, T * f * e)) || (st = A(&v.G, T * f * e)) ||
@@ -499,6 +507,7 @@ stage_status ensure_activations(stage_t* s, int B, int S) {
   if ((st = grow_splitk(s, need)) || (st = grow_scores(s, n_scores))) return st;
   s->cap_T = T;
   s->cap_BSS = BSS;
+  s->cap_Tlo = Tlo;
   s->cap_B = B;
   s->cap_NQB = NQB;
   return STAGE_OK;
@@ -1443,7 +1452,7 @@ int64_t dry_bytes(int first_unit, int n_units, int hidden, int heads, int ffn, i
   stage_t d;
   d.dry_run = true;
   set_units(&d, first_unit, n_units, hidden, heads, ffn, dtype);
-  if (build_params(&d, 0) != STAGE_OK || ensure_activations(&d, batch, seq) != STAGE_OK) return -1;
+  if (build_params(&d, 0) != STAGE_OK || ensure_activations(&d, batch, seq, false) != STAGE_OK) return -1;
   return d.bytes_param + d.bytes_act;
 }
 
@@ -1548,7 +1557,7 @@ stage_status stage_forward(stage_t* s, const void* x, const uint8_t* key_mask, i
     return fail(s, STAGE_EINVAL, "batch * seq too large");
   if (s->dtype == STAGE_F32 && (int64_t)batch * s->H * seq * seq >= (int64_t)1 << 40)
     return fail(s, STAGE_EINVAL, "score matrix too large");
-  stage_status st = ensure_activations(s, batch, seq);
+  stage_status st = ensure_activations(s, batch, seq, s->relpos);
   if (st) return st;
   s->B = batch;
   s->S = seq;
@@ -1663,7 +1672,7 @@ stage_status stage_set_relpos(stage_t* s, int num_buckets, int max_distance) try
   }
   s->relpos = false;
   s->have_ctx = false;
-  s->cap_T = -1;  // (fp32 stages past 512 tokens hold no score matrix with a bias)
+  s->cap_T = -1;  // (with a bias a stage holds no scores and no context residual)
   if (num_buckets == 0) return STAGE_OK;
   s->rp = rp;
   const int64_t n = (int64_t)num_buckets * s->H;
@@ -1708,7 +1717,7 @@ stage_status stage_forward_cross(stage_t* s, const void* x, const void* memory, 
   const int64_t lim = ((int64_t)1 << 31) / (s->dtype == STAGE_BF16 ? 2 : 1);
   if (T * std::max(3 * s->h, s->f) >= lim || Tm * std::max(3 * s->h, s->f) >= lim)
     return fail(s, STAGE_EINVAL, "batch * seq too large");
-  stage_status st = ensure_activations(s, batch, seq);
+  stage_status st = ensure_activations(s, batch, seq, true);
   if (st) return st;
   s->B = batch;
   s->S = seq;
