@@ -626,7 +626,8 @@ def attn_forward(q, k, v, key_mask=None, scale=None, causal=False, q_pos=None, r
 def attn_backward(q, k, v, out, lse, dout, key_mask=None, scale=None, causal=False, q_pos=None,
                   relpos=None, table=None, dq=None, dk=None, dv=None, dtable=None):
     """Gradients of <out, dout> for attn_forward's arguments, out and lse: returns
-    dq, dk, dv and dtable (None without a table), written where given."""
+    dq, dk, dv and dtable (None without a table), written where given.  dtable=False
+    leaves the table's gradient out (a table that is not trained): None is returned."""
     fn = (_attn_module or _attn_setup()).backward
     r = fn(q, k, v, out, lse, dout, key_mask, scale, causal, q_pos, relpos, table, dq, dk, dv, dtable)
     return r if r.__class__ is tuple else _attn_on(r, fn, q, k, v, out, lse, dout, key_mask, scale,

@@ -364,7 +364,7 @@ stage_status attn_backward(const attn_shape* s, const attn_relpos* rp, const flo
   a.kv_chunk = w.kv.chunk;
   a.kv_qs = w.kv.qs;
   a.kv_splits = w.kv.splits;
-  a.one_launch = (!table || dtable) && xattn_one_launch(B, H, G, Sq, Sk, w.dq, w.kv, s->dtype);
+  a.one_launch = xattn_one_launch(B, H, G, Sq, Sk, w.dq, w.kv, s->dtype);
   const hipError_t e = xattn_backward(a, s->dtype, (hipStream_t)hip_stream);
   if (e != hipSuccess) return bad(STAGE_EHIP, "attn_backward: %s", hipGetErrorString(e));
   return STAGE_OK;

@@ -300,7 +300,7 @@ PyObject* forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // backward(q, k, v, out, lse, dout, key_mask, scale, causal, q_pos, relpos, table, dq, dk, dv,
-// dtable): (dq, dk, dv, dtable), or the device as above.
+// dtable): (dq, dk, dv, dtable), or the device as above.  dtable False: none is made.
 PyObject* backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 16 || !workspace_fn) {
     PyErr_SetString(PyExc_TypeError, "backward takes 16 arguments, after setup");
@@ -308,7 +308,8 @@ PyObject* backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   Inputs in;
   if (!inputs(a[0], a[1], a[2], a[6], a[7], a[8], a[9], a[10], a[11], &in)) return nullptr;
-  if (a[11] == Py_None && a[15] != Py_None) {
+  const bool table_grad = a[11] != Py_None && a[15] != Py_False;
+  if (a[11] == Py_None && a[15] != Py_None && a[15] != Py_False) {
     refuse("dtable without a table");
     return nullptr;
   }
@@ -324,7 +325,7 @@ PyObject* backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
       dv(dk.p ? output(a[14], a[2]) : nullptr);
   if (!dv.p) return nullptr;
   Ref dtable;
-  if (a[11] != Py_None) {
+  if (table_grad) {
     dtable.set(output(a[15], a[11]));
     if (!dtable.p || !plain("dtable", dtable.p, 2, in.buckets, in.q_size[2], 1, f32, in.dev, &dt))
       return nullptr;

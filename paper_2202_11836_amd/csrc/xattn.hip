@@ -1188,7 +1188,8 @@ double xattn_fwd_time(int B, int H, int Sq, int Sk, int causal, stage_dtype dt, 
 // sums of the chunks.  us in two launches and in one (with a bias, in one more each): 2 x 8
 // heads of 64 queries and keys 12.1 and 9.4, fp32 22.6 and 13.9; 3 x 12 of 77 over 201 16.5
 // and 14; fp32, 10 x 16 of 128 47.9 and 35.9; with a bias 2 x 8 of 128 21.6 and 16.9, fp32
-// 36.9 and 23.6, 10 x 16 of 128 25 and 20.2.  bf16 work-groups go through all keys for D:
+// 36.9 and 23.6, 10 x 16 of 128 25 and 20.2 (without the bias's gradient, whose launch then
+// falls away, 21.3 and 16).  bf16 work-groups go through all keys for D:
 // 4 x 16 of 32 over 300 15.6 and 14.5, of 100 over 700 26 and 33.6; two blocks of queries
 // (4 x 16 of 256) 20.6 and 26.5.
 int xattn_one_launch(int B, int H, int G, int Sq, int Sk, const XDqPlan& dq, const XKvPlan& kv,

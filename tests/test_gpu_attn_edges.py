@@ -79,3 +79,21 @@ def test_queries_that_see_no_key(dtype, shape, relpos, left):
     want = reference(q, k, v, relpos=relpos, dout=do, **kw)
     for n in want:
         check(n, got[n], want[n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tables_gradient_left_out(dtype):
+    """dtable=False with a table, without one (where there is none to make), and into given
+    tensors."""
+    q, do = rand((2, 33, 4, 64), 1, dtype), rand((2, 33, 4, 64), 2, dtype)
+    k, v = rand((2, 50, 2, 64), 3, dtype), rand((2, 50, 2, 64), 4, dtype)
+    rp, table = P.RelPos(8, 20), rand((8, 4), 5)
+    for kw in (dict(relpos=rp, table=table), {}):
+        out, lse = P.attn_forward(q, k, v, **kw)
+        to = [torch.full_like(t, float("nan")) for t in (q, k, v)]
+        got = P.attn_backward(q, k, v, out, lse, do, dq=to[0], dk=to[1], dv=to[2], dtable=False, **kw)
+        assert got[3] is None and all(a is b for a, b in zip(got, to))
+        want = reference(q, k, v, dout=do, relpos=(8, 20, True) if kw else None,
+                         table=kw.get("table"))
+        for n, g in zip(("dq", "dk", "dv"), got):
+            check(n, g, want[n])
