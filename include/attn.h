@@ -99,7 +99,7 @@ typedef struct {
   int batch, seq_q, seq_k;
   int heads, kv_heads; /* heads a multiple of kv_heads */
   int causal;          /* 0 or 1 */
-  float scale;         /* finite, > 0 */
+  float scale;         /* > 0, below 2.35e38 (fp32's largest over log2(e)) */
   int64_t q[3], k[3], v[3], out[3];
   int64_t dout[3], dq[3], dk[3], dv[3];
 } attn_shape;

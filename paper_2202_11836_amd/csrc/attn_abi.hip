@@ -125,8 +125,9 @@ stage_status check_shape(const attn_shape* s, const attn_relpos* rp) {
   if (s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads)
     return bad(STAGE_EINVAL, "heads must be a multiple of kv_heads, both >= 1");
   if (s->causal != 0 && s->causal != 1) return bad(STAGE_EINVAL, "causal must be 0 or 1");
-  if (!(s->scale > 0.0f) || !std::isfinite(s->scale))
-    return bad(STAGE_EINVAL, "scale must be finite and positive");
+  // (the kernels take it times log2(e))
+  if (!(s->scale > 0.0f) || !std::isfinite(s->scale * XLOG2E))
+    return bad(STAGE_EINVAL, "scale must be positive and below 2.35e38");
   if (rp && !relpos_ok(rp)) return bad(STAGE_EINVAL, "rp is not one that attn_relpos_init filled");
   // A launch holds fewer than 2^32 threads, 256 to a work-group.
   // (the dQ kernel may take two for 128 queries)
