@@ -317,6 +317,8 @@ stage_status attn_backward(const attn_shape* s, const attn_relpos* rp, const flo
   CK(check_shape(s, rp));
   CK(check_table(rp, table));
   if (dtable && !table) return bad(STAGE_EINVAL, "dtable without a table");
+  if (dtable && dtable == table)
+    return bad(STAGE_EINVAL, "a gradient may not be written over an input");
   XAttnArgs a{};
   const int B = s->batch, H = s->heads, G = s->kv_heads, Sq = s->seq_q, Sk = s->seq_k;
   CK(check_operand("q", q, s->q, B, Sq, H, s->dtype, false, a.sq));

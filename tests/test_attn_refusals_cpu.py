@@ -14,3 +14,9 @@ def test_scales_whose_base_2_form_is_infinite(backward):
         assert st == 1 and "scale" in msg
     st, msg = call(backward, shape(scale=2.35e38), ws_bytes=0, q=None)
     assert st == 1 and "scale" not in msg  # (refused for the missing q)
+
+
+def test_table_over_its_gradient():
+    rp = P.RelPos(32, 128).c
+    st, msg = call(1, shape(), rp, dtable=PTR["table"])
+    assert st == 1 and "over an input" in msg
