@@ -1752,6 +1752,7 @@ stage_status stage_backward_cross(stage_t* s, const void* dy, void* dx, void* dm
   if (T > 0 && (!dy || !dx)) return fail(s, STAGE_EINVAL, "null dy or dx");
   if (Tm > 0 && !dmemory) return fail(s, STAGE_EINVAL, "null dmemory");
   if ((uintptr_t)dmemory % 16) return fail(s, STAGE_EINVAL, "dmemory is not 16-byte aligned");
+  if (T > 0 && Tm > 0 && dx == dmemory) return fail(s, STAGE_EINVAL, "dx and dmemory have the same memory");
   s->have_ctx = false;
   if (T == 0) {
     if (Tm > 0) {
