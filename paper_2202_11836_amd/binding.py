@@ -363,6 +363,7 @@ class Stage:
                  dtype: str = "bf16", first_unit: int = 0, n_units: Optional[int] = None):
         import torch
         self.hidden, self.heads, self.ffn = hidden, heads, ffn
+        self._cross = None  # shapes of x and memory of the latest forward, if of cross attention
         self.dtype_name = dtype
         self.code = STAGE_BF16 if dtype == "bf16" else STAGE_F32
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
@@ -385,6 +386,7 @@ class Stage:
         if key_mask is not None:
             assert key_mask.dtype == torch.uint8 and key_mask.shape == (B, S) and key_mask.is_contiguous()
         y = torch.empty_like(x) if out is None else out
+        self._cross = None
         self._sync_stream()
         stage_forward(self.handle, x, key_mask, B, S, y)
         return y
@@ -440,9 +442,11 @@ class Stage:
         if key_mask is not None:
             assert key_mask.dtype == torch.uint8 and key_mask.shape == (B, M) and key_mask.is_contiguous()
         y = torch.empty_like(x) if out is None else out
+        assert y.shape == x.shape and y.dtype == x.dtype and y.device == x.device and y.is_contiguous()
+        self._cross = None
         self._sync_stream()
         stage_forward_cross(self.handle, x, memory, key_mask, B, S, M, y)
-        self._mem_shape = memory.shape
+        self._cross = x.shape, memory.shape
         return y
 
     def backward_cross(self, dy, out=None, out_memory=None):
@@ -450,9 +454,12 @@ class Stage:
         import torch
         assert dy.dtype == self.torch_dtype and dy.is_cuda and dy.is_contiguous()
         dx = torch.empty_like(dy) if out is None else out
-        shape = getattr(self, "_mem_shape", (0, 0, self.hidden))
-        dmem = torch.empty(shape, dtype=dy.dtype, device=dy.device) if out_memory is None else out_memory
-        assert dmem.shape == shape and dmem.dtype == dy.dtype and dmem.is_contiguous()
+        # (without a context the library refuses the call)
+        x_shape, mem_shape = self._cross or (dy.shape, (0, 0, self.hidden))
+        dmem = torch.empty(mem_shape, dtype=dy.dtype, device=dy.device) if out_memory is None else out_memory
+        assert dy.shape == x_shape
+        for t, shape in ((dx, x_shape), (dmem, mem_shape)):
+            assert t.shape == shape and t.dtype == dy.dtype and t.device == dy.device and t.is_contiguous()
         self._sync_stream()
         stage_backward_cross(self.handle, dy, dx, dmem)
         return dx, dmem
