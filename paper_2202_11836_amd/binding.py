@@ -496,8 +496,8 @@ class Stage:
 
     def saved(self, layer: int, which: int, tokens: int):
         import torch
-        width = {0: self.hidden, 1: 3 * self.hidden, 2: self.hidden, 3: self.hidden,
-                 4: self.ffn, 5: self.ffn}[which]
+        width = {0: self.hidden, 1: (1 if self._cross else 3) * self.hidden, 2: self.hidden,
+                 3: self.hidden, 4: self.ffn, 5: self.ffn}[which]
         out = torch.empty((tokens, width), dtype=self.torch_dtype, device="cuda")
         self._sync_stream()
         stage_read(self.handle, KIND_SAVED, layer, which, out)

@@ -49,3 +49,26 @@ def test_one_tensor_for_both_gradients_refused(dtype):
     torch.cuda.synchronize()
     assert not torch.equal(dx, dmem)
     st.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_contexts_queries(dtype):
+    """Q = x W_q^T + b_q alone is what a cross-attention context holds under QKV; an
+    ordinary pass after it has all three again."""
+    st, x, mem = half(dtype), rand((2, 9, 128), 1, dtype), rand((2, 5, 128), 2, dtype)
+    st.set_param(0, PARAM_NAMES.index("b_qkv"), rand((384,), 4))
+    w, b = (st.param(0, PARAM_NAMES.index(n)).double().cpu() for n in ("W_qkv", "b_qkv"))
+    st.forward_cross(x, mem)
+    q = st.saved(0, 1, 18)
+    assert q.shape == (18, 128)
+    xs = x.double().cpu().reshape(18, 128)
+    want = xs @ w.T + b
+    # 128 products and the bias in fp32, and the rounding to the stage's type
+    t = torch.finfo(x.dtype).eps / 2
+    bound = 130 * 2.0 ** -24 * (xs.abs() @ w.T.abs() + b.abs()) * (1 + t) + t * want.abs()
+    assert bool(((q.double().cpu() - want[:, :128]).abs() <= bound[:, :128]).all())
+    st.forward(x)
+    q = st.saved(0, 1, 18)
+    assert q.shape == (18, 384)
+    assert bool(((q.double().cpu() - want).abs() <= bound).all())
+    st.close()
