@@ -590,7 +590,8 @@ def _attn_setup():
     try:
         from . import _attn_call
     except ImportError as e:
-        raise RuntimeError("_attn_call is not built; run __graft_entry__.build() first") from e
+        raise RuntimeError("_attn_call is not built; run __graft_entry__.build() first "
+                           "(it needs Python's headers)") from e
     _attn_call.setup(*(ctypes.cast(f, ctypes.c_void_p).value
                        for f in (lib.attn_workspace, lib.attn_forward, lib.attn_backward,
                                  lib.attn_last_error)),

@@ -13,6 +13,7 @@ import shutil
 import subprocess
 import sys
 from concurrent.futures import ThreadPoolExecutor
+from typing import Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
@@ -48,13 +49,22 @@ def _compile(src: str) -> str:
     return obj
 
 
-def build_binding() -> str:
-    """The Python module that marshals the attention operators' calls (host code)."""
+def build_binding() -> Optional[str]:
+    """The Python module that marshals the attention operators' calls (host code): by
+    $CXX, g++ or hipcc.  None, with no module left, where Python's headers are not
+    installed: the stage and the allocator do without, and the operators' first call
+    from Python says what is missing."""
     import sysconfig
     src = os.path.join(CSRC, "py", "attn_call.cpp")
     path = os.path.join(PKG, "_attn_call.so")
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
-           "-I" + sysconfig.get_paths()["include"], src, "-o", path + ".tmp"]
+    include = sysconfig.get_paths()["include"]
+    if not os.path.exists(os.path.join(include, "Python.h")):
+        print(f"_attn_call not built: no Python.h in {include}", file=sys.stderr)
+        if os.path.exists(path):
+            os.remove(path)
+        return None
+    cmd = [os.environ.get("CXX") or shutil.which("g++") or HIPCC, "-O2", "-std=c++17", "-fPIC",
+           "-shared", "-I" + include, src, "-o", path + ".tmp"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"{src}:\n{r.stderr}")
