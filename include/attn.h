@@ -32,7 +32,9 @@
  *     lse [batch, heads, seq_q], table and dtable [num_buckets, heads] are
  *     fp32, contiguous.  Scores, softmax statistics and sums are fp32; on bf16
  *     the probabilities and dS are rounded to bf16 where a matrix product takes
- *     them (dtable sums dS unrounded).
+ *     them (dtable sums dS unrounded).  A bias below -2.35e38 (fp32's lowest
+ *     value, -inf) hides its keys; a query all of whose keys are hidden so gets
+ *     what one that sees none gets.  Other biases are finite, below 2.35e38.
  *   - key_mask: uint8 [batch, seq_k], contiguous, nonzero = may be attended;
  *     NULL = every key.  What the k and v rows of a key hold that the mask
  *     hides, or that no query may see, reaches no result, whatever it is (NaN

@@ -6,13 +6,13 @@
 // and sums, in LDS and, with several splits, by a second launch.  Each wavefront has
 // a two-stage ring of 32-key blocks in LDS to itself and waits for nobody until the
 // join: it waits for a block, requests the next one and computes.  (Requesting before the
-// wait puts twice as much on its way and is slower for long caches: 16 x 16 heads over
-// 8192 keys 105 us, 98 like this, and a plain read of as many bytes takes 88 to 93.)
+// wait puts twice as much on its way and was slower for long caches: 16 x 16 heads over
+// 8192 keys 105 us against 98, both with ordinary loads.)
 // The scores and products are those of xattn.hip: a tile costs 0.3 us of a SIMD's time
-// whether one of its rows is in use or all, and its 8 KB take the memory 0.4 us at 256
-// CUs' share of 5.5 TB/s and 4 SIMDs.  Measured: 16 x 16 heads, one token over 8192
-// keys, 98 us (5.5 TB/s); where there is less to read, the chain of one wavefront's
-// blocks and the join (5 us) are what is left.
+// whether one of its rows is in use or all, and a SIMD's share of 5.5 TB/s (256 CUs of 4)
+// brings its 8 KB in 1.5 us.  Measured: 16 x 16 heads, one token over 8192 keys, 92 us
+// (5.8 TB/s; a plain read of as many bytes takes 88 to 93); where there is less to read,
+// the chain of one wavefront's blocks and the join (4 us) are what is left.
 #include <algorithm>
 #include <cmath>
 

@@ -97,3 +97,22 @@ def test_tables_gradient_left_out(dtype):
                          table=kw.get("table"))
         for n, g in zip(("dq", "dk", "dv"), got):
             check(n, g, want[n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES + [(2, 4, 2, 1, 300)], ids=str)
+@pytest.mark.parametrize("low", [float("-inf"), torch.finfo(torch.float32).min])
+def test_biases_that_hide(dtype, shape, low):
+    """Buckets of -inf, or of fp32's lowest value, hide their keys in both passes, far and
+    near: here those behind the query, and, where a query has no others, all of them."""
+    B, H, G, Sq, Sk = shape
+    q, do = rand((B, Sq, H, 64), 1, dtype), rand((B, Sq, H, 64), 2, dtype)
+    k, v = rand((B, Sk, G, 64), 3, dtype), rand((B, Sk, G, 64), 4, dtype)
+    pos = torch.tensor([(0, -20, 7)[b % 3] for b in range(B)], dtype=torch.int32)
+    table = rand((8, H), 5)
+    hidden = table.clone()
+    hidden[4:] = low  # (8 buckets both ways: from 4 on of keys behind the query)
+    got = both(q, k, v, do, relpos=(8, 20, True), table=hidden, q_pos=pos.cuda())
+    want = reference(q, k, v, relpos=(8, 20, True), dout=do, table=table, q_pos=pos.cuda(), causal=True)
+    for n in want:
+        check(n, got[n], want[n])
