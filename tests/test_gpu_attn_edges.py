@@ -116,3 +116,27 @@ def test_biases_that_hide(dtype, shape, low):
     want = reference(q, k, v, relpos=(8, 20, True), dout=do, table=table, q_pos=pos.cuda(), causal=True)
     for n in want:
         check(n, got[n], want[n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv", [(2, 2), (8, 1), (10, 2)])
+@pytest.mark.parametrize("relpos", [None, (32, 128, False)])
+def test_long_paddings_at_the_left(dtype, heads, kv, relpos):
+    """Sequences of up to 600 tokens padded at their left by whole blocks and more, whose
+    padding holds anything in every operand."""
+    first = [300, 130, 512, 0, 599]
+    B, S = len(first), 600
+    pad = (torch.arange(S)[None, :] < torch.tensor(first)[:, None]).cuda()
+    q, do = rand((B, S, heads, 64), 1, dtype), rand((B, S, heads, 64), 2, dtype)
+    k, v = rand((B, S, kv, 64), 3, dtype), rand((B, S, kv, 64), 4, dtype)
+    table = rand((relpos[0], heads), 5) if relpos else None
+    bad = [t.clone() for t in (q, k, v, do)]
+    for t, x in zip(bad, ("nan", "inf", "nan", "-inf")):
+        t[pad] = float(x)
+    mask = (~pad).to(torch.uint8)
+    got = both(*bad, relpos=relpos, key_mask=mask, causal=True, table=table)
+    for t in (q, k, v, do):
+        t[pad] = 0
+    want = reference(q, k, v, mask=mask, relpos=relpos, dout=do, causal=True, table=table)
+    for n in want:
+        check(n, got[n], want[n])
