@@ -192,7 +192,9 @@ stage_status stage_backward_noalloc(stage_t* s, const void* dy, void* dx);
  * stream, drops the saved context and any earlier table; the next stage_forward
  * allocates anew.  stage_backward also overwrites the table's gradient, the sum over
  * the stage's layers (a model that shares one table over several stages sums theirs).
- * A sequence without a valid key attends to nothing, as without the bias.  The
+ * A sequence without a valid key attends to nothing, as without the bias.  On bf16
+ * stages P is rounded to bf16 where it meets V (attn.h), which the stage's own
+ * attention avoids: a table of zeros gives a context less exact than no bias.  The
  * table, its gradient and the operators' workspace are held besides what
  * stage_memory_model counts, but past 64 tokens no scores or probabilities on fp32
  * stages and no rounding residual of the context on bf16 stages: memory is linear in
@@ -213,7 +215,7 @@ stage_status stage_relpos(stage_t* s, float** table, float** grad, int64_t* nume
  * key_mask: uint8 [batch, mem_seq] or NULL.  x, memory and the mask are copied into
  * the saved context; y may not be one of them.  Lengths of 0 are valid (a query
  * without a key attends to nothing).  stage_backward_cross takes the gradient of y
- * and writes those of x and of memory (dmemory: 16-byte aligned) and the half's
+ * and writes those of x and of memory (dmemory: 16-byte aligned, not dx) and the half's
  * parameter gradients; it consumes the context.  EINVAL, ESTATE and ENOMEM as
  * stage_forward and stage_backward; a context of one kind is not taken by the other
  * kind's backward (ESTATE).  STAGE_SAVED_QKV of such a context is Q alone, [T, h].
