@@ -1052,7 +1052,7 @@ hipError_t forward_t(const XAttnArgs& a, hipStream_t st) {
 
 // Kernels that take `causal` keep the first query that sees a key beside what the others
 // keep: dK and dV of 32 x 16 heads of 128 over 512 without `causal` 37.2 us with such a
-// kernel, 35.0 with one of its own.  (fp32 has none: 8 x 12 heads of 128 with a bias take
+// kernel, 34.8 with one of its own.  (fp32 has none: 8 x 12 heads of 128 with a bias take
 // 33.3 either way.)
 typedef void (*KvKernel)(XAttnArgs, int);
 template <typename T, int QS>
