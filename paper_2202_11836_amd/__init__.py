@@ -2,12 +2,14 @@
 contiguous block of post-LN BERT encoder layers on one GPU, in hand-written
 HIP kernels behind a C ABI (include/stage.h); attention over another
 sequence's keys and with a relative position bias by buckets (include/attn.h);
-and the host-side layer allocator that sizes such blocks per device
+layer norm (include/norm.h), rotary positions (include/rotary.h) and AdamW over
+many tensors (include/adamw.h); and the host-side layer allocator that sizes such blocks per device
 (include/alloc.h)."""
 from .binding import (ALLOC_CT_PER_DEVICE, ALLOC_CT_PER_LAYER, ALLOC_EINVAL, ALLOC_ENOFIT,
                       ALLOC_OK, PARAM_NAMES, SAVED_NAMES, STAGE_BF16, STAGE_F32, AllocError,
-                      RelPos, Stage, StageError, alloc_coarse, alloc_fine, alloc_workloads,
-                      attn_backward, attn_forward, load_library,
+                      AdamW, RelPos, Rotary, Stage, StageError, alloc_coarse, alloc_fine,
+                      alloc_workloads, attn_backward, attn_forward, layer_norm_backward,
+                      layer_norm_forward, load_library, rotary_backward, rotary_forward,
                       stage_backward, stage_backward_cross,
                       stage_backward_noalloc, stage_destroy, stage_device_bytes, stage_forward, stage_forward_cross, stage_grad, stage_init,
                       stage_init_units, stage_memory_model_units,
@@ -25,5 +27,7 @@ __all__ = ["Stage", "StageError", "load_library", "PARAM_NAMES", "SAVED_NAMES", 
            "stage_mfma_peak", "stage_record_grads",
            "stage_set_relpos", "stage_relpos", "stage_forward_cross", "stage_backward_cross",
            "RelPos", "attn_forward", "attn_backward",
+           "layer_norm_forward", "layer_norm_backward", "Rotary", "rotary_forward",
+           "rotary_backward", "AdamW",
            "AllocError", "ALLOC_OK", "ALLOC_EINVAL", "ALLOC_ENOFIT", "ALLOC_CT_PER_LAYER",
            "ALLOC_CT_PER_DEVICE", "alloc_coarse", "alloc_fine", "alloc_workloads"]

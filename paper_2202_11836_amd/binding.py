@@ -1,6 +1,7 @@
 """Thin ctypes binding of the C ABI of libskystage.so: the encoder stage
-(include/stage.h), the attention operators (include/attn.h) and the host-side
-layer allocator (include/alloc.h).
+(include/stage.h), the attention operators (include/attn.h), layer norm
+(include/norm.h), rotary positions (include/rotary.h), AdamW (include/adamw.h) and
+the host-side layer allocator (include/alloc.h).
 
 Argument marshalling only: torch tensors supply device memory and the HIP
 stream (torch.cuda.current_stream()); every step of the stage runs in the
@@ -42,6 +43,11 @@ EXPORTED = ("alloc_coarse", "alloc_fine", "alloc_workloads", "stage_init", "stag
 EXPORTED_ATTN = ("attn_relpos_init", "attn_relpos_bucket", "attn_workspace", "attn_forward",
                  "attn_backward", "attn_last_error")
 
+EXPORTED_OPS = ("layer_norm_workspace", "layer_norm_forward", "layer_norm_backward",
+                "layer_norm_last_error", "rotary_init", "rotary_init_freqs", "rotary_forward",
+                "rotary_backward", "rotary_last_error", "adamw_init", "adamw_step", "adamw_destroy",
+                "adamw_last_error")
+
 _lib = None
 
 
@@ -67,6 +73,19 @@ class _RelPos(ctypes.Structure):  # attn_relpos
 # attn_shape: dtype, batch, seq_q, seq_k, heads, kv_heads, causal, scale and the
 # strides of q, k, v, out, dout, dq, dk, dv
 _ATTN_SHAPE = struct.Struct("@7if24q")
+
+
+class _RotaryFreqs(ctypes.Structure):  # rotary_freqs
+    _fields_ = [("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int),
+                ("amplitude", ctypes.c_float), ("turns", ctypes.c_double * 32)]
+
+
+class _AdamWTensor(ctypes.Structure):  # adamw_tensor
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale",
+                                               "master")] + \
+               [("numel", ctypes.c_int64), ("dtype", ctypes.c_int), ("grad_dtype", ctypes.c_int),
+                ("state_bits", ctypes.c_int), ("weight_decay", ctypes.c_float),
+                ("lr_scale", ctypes.c_float)]
 
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -159,6 +178,19 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.attn_backward.restype = i32
     lib.attn_last_error.argtypes = []
     lib.attn_last_error.restype = ctypes.c_char_p
+    dbl, fr = ctypes.c_double, ctypes.POINTER(_RotaryFreqs)
+    lib.rotary_init.argtypes = [i32, i32, dbl, i32, dbl, i32, dbl, dbl, dbl, fr]
+    lib.rotary_init.restype = i32
+    lib.rotary_init_freqs.argtypes = [i32, i32, dp, dbl, fr]
+    lib.rotary_init_freqs.restype = i32
+    lib.adamw_init.argtypes = [ctypes.POINTER(_AdamWTensor), i32, vp, ctypes.POINTER(vp)]
+    lib.adamw_init.restype = i32
+    lib.adamw_destroy.argtypes = [vp]
+    lib.adamw_destroy.restype = None
+    for f in (lib.rotary_last_error, lib.layer_norm_last_error, lib.adamw_last_error):
+        f.argtypes = []
+        f.restype = ctypes.c_char_p
+    # (the other calls of the three are marshalled by csrc/py/ops_call.cpp)
     _lib = lib
     return lib
 
@@ -640,6 +672,267 @@ def attn_backward(q, k, v, out, lse, dout, key_mask=None, scale=None, causal=Fal
     r = fn(q, k, v, out, lse, dout, key_mask, scale, causal, q_pos, relpos, table, dq, dk, dv, dtable)
     return r if r.__class__ is tuple else _attn_on(r, fn, q, k, v, out, lse, dout, key_mask, scale,
                                                    causal, q_pos, relpos, table, dq, dk, dv, dtable)
+
+
+# ---------------------------------------------------------------------------
+# Layer norm (include/norm.h), rotary positions (include/rotary.h), AdamW (include/adamw.h)
+# ---------------------------------------------------------------------------
+_ops_module = None
+
+
+def _ops_setup():
+    """csrc/py/ops_call.cpp, which checks and marshals the tensors of a call."""
+    global _ops_module
+    import torch
+    lib = load_library()
+    try:
+        from . import _ops_call
+    except ImportError as e:
+        raise RuntimeError("_ops_call is not built; run __graft_entry__.build() first "
+                           "(it needs Python's headers)") from e
+    _ops_call.setup(*(ctypes.cast(f, ctypes.c_void_p).value
+                      for f in (lib.layer_norm_workspace, lib.layer_norm_forward,
+                                lib.layer_norm_backward, lib.layer_norm_last_error,
+                                lib.rotary_forward, lib.rotary_backward, lib.rotary_last_error,
+                                lib.adamw_step, lib.adamw_last_error)),
+                    StageError, torch.bfloat16, torch.float32, torch.uint8, torch.int32,
+                    torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
+                    lambda n, dev: torch.empty(n, dtype=torch.uint8, device=dev))
+    _ops_module = _ops_call
+    return _ops_module
+
+
+def layer_norm_forward(x, gamma=None, beta=None, residual=None, eps=1e-12, out=None, total=None,
+                       mean=None, rstd=None):
+    """Layer norm over the last dimension of x (fp32 or bf16, rows that may lie apart): returns
+    out, total, mean and rstd, of which layer_norm_backward takes the last three.
+
+    gamma, beta   fp32 [width] (None: 1 and 0)
+    residual      added to x first; total is then that sum, as it is stored, else x
+    out, total, mean, rstd   where to write; out and total may be x or residual
+
+    Runs on the current stream of x's device."""
+    fn = (_ops_module or _ops_setup()).norm_forward
+    r = fn(x, gamma, beta, residual, eps, out, total, mean, rstd)
+    return r if r.__class__ is tuple else _attn_on(r, fn, x, gamma, beta, residual, eps, out, total,
+                                                   mean, rstd)
+
+
+def layer_norm_backward(dy, total, gamma, mean, rstd, dtotal=None, dx=None, dgamma=None, dbeta=None):
+    """Gradients of <out, dy> + <total, dtotal> for layer_norm_forward's total, mean and rstd:
+    returns dx (x's and the residual's), dgamma and dbeta (fp32), written where given; dx may be
+    dy, dtotal or total.  False for one of them leaves it out: None is returned in its place."""
+    fn = (_ops_module or _ops_setup()).norm_backward
+    r = fn(dy, total, gamma, mean, rstd, dtotal, dx, dgamma, dbeta)
+    return r if r.__class__ is tuple else _attn_on(r, fn, dy, total, gamma, mean, rstd, dtotal, dx,
+                                                   dgamma, dbeta)
+
+
+class Rotary:
+    """Frequencies of rotary positions (rotary_freqs): the first rot_dim of a head's 64 values
+    turn in pairs, (i, rot_dim / 2 + i) (layout "half") or (2 i, 2 i + 1) ("interleaved"), pair i
+    by base^(-2 i / rot_dim) a position, all times amplitude.
+
+    scaling   for contexts `factor` times those of original_len positions: "linear" (positions
+              squeezed), "base" (a larger base) or "parts" (pairs that make fewer than `low`
+              turns in original_len squeezed, those of more than `high` not, others in part)
+    freqs     rot_dim / 2 frequencies of the caller's instead, in radians a position"""
+
+    LAYOUTS = ("half", "interleaved")
+    SCALINGS = (None, "linear", "base", "parts")
+
+    def __init__(self, rot_dim: int = 64, base: float = 10000.0, layout: str = "half", scaling=None,
+                 factor: float = 1.0, original_len: int = 0, low: float = 1.0, high: float = 32.0,
+                 amplitude: float = 1.0, freqs=None):
+        self._args = (rot_dim, base, layout, scaling, factor, original_len, low, high, amplitude,
+                      None if freqs is None else tuple(float(f) for f in freqs))
+        freqs = self._args[-1]
+        if layout not in self.LAYOUTS:
+            raise StageError(STAGE_EINVAL, f"layout must be one of {self.LAYOUTS}")
+        if scaling not in self.SCALINGS:
+            raise StageError(STAGE_EINVAL, f"scaling must be one of {self.SCALINGS}")
+        if freqs is not None and (scaling is not None or len(freqs) != rot_dim // 2):
+            raise StageError(STAGE_EINVAL, "freqs takes rot_dim / 2 frequencies and no scaling")
+        self.rot_dim, self.layout, self.amplitude = int(rot_dim), layout, float(amplitude)
+        self.c = _RotaryFreqs()
+        lib, inter = load_library(), self.LAYOUTS.index(layout)
+        if freqs is None:
+            st = lib.rotary_init(self.rot_dim, inter, base, self.SCALINGS.index(scaling), factor,
+                                 int(original_len), low, high, amplitude, ctypes.byref(self.c))
+        else:
+            st = lib.rotary_init_freqs(self.rot_dim, inter, (ctypes.c_double * max(len(freqs), 1))(*freqs),
+                                       amplitude, ctypes.byref(self.c))
+        if st != STAGE_OK:
+            raise StageError(st, (lib.rotary_last_error() or b"").decode())
+        self.addr = ctypes.addressof(self.c)
+
+    def __reduce__(self):  # (a copy holds frequencies of its own)
+        return Rotary, self._args
+
+
+def rotary_forward(rotary, q, k=None, pos=None, q_out=None, k_out=None):
+    """q [batch, seq, heads, 64] and k [batch, seq, kv_heads, 64] (fp32 or bf16, any strides
+    that leave a head's 64 values side by side) turned by their positions: returns q_out and
+    k_out (None without k), written where given; q_out may be q and k_out k.
+
+    pos   int32 [batch], position of token 0 of each sequence, or [batch, seq], of each token
+          (None: 0, 1, ...)
+
+    Runs on the current stream of q's device."""
+    fn = (_ops_module or _ops_setup()).rotary
+    r = fn(False, rotary, q, k, pos, q_out, k_out)
+    return r if r.__class__ is tuple else _attn_on(r, fn, False, rotary, q, k, pos, q_out, k_out)
+
+
+def rotary_backward(rotary, dq, dk=None, pos=None, q_out=None, k_out=None):
+    """Gradients of rotary_forward's q and k from those of its outputs, dq and dk (turned back,
+    times the same amplitude), with the same rotary and pos: returns both, written where given."""
+    fn = (_ops_module or _ops_setup()).rotary
+    r = fn(True, rotary, dq, dk, pos, q_out, k_out)
+    return r if r.__class__ is tuple else _attn_on(r, fn, True, rotary, dq, dk, pos, q_out, k_out)
+
+
+class AdamW:
+    """AdamW over many tensors at once (adamw.h): step() updates params, each with the gradient
+    in grads, in place, in one launch (two with max_norm).
+
+    params, grads   lists of contiguous fp32 or bf16 tensors of one GPU; the gradients' memory
+                    is read by every step
+    weight_decay, lr_scale   a number, or one for each tensor
+    state_bits      32 or 8, or a list of them: fp32 states, or e4m3 and e5m2 with a scale for
+                    each 256 elements
+    master          bf16 parameters have fp32 copies that take the updates (False: none, the
+                    parameters are rounded at random in proportion)
+    state           the states to go on with (another AdamW's .state, say), held in place; None:
+                    new ones
+
+    state: a dict of lists, an entry for each tensor: "exp_avg", "exp_avg_sq" (fp32, or
+    float8_e4m3fn and float8_e5m2), "exp_avg_scale", "exp_avg_sq_scale" (8 bits: fp32, one for
+    256 elements, else None), "master" (fp32 or None); and "steps", int64 [1] on the GPU."""
+
+    LISTS = ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale", "master")
+
+    def __init__(self, params, grads, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, lr_scale=1.0,
+                 state_bits=32, master=True, state=None):
+        import torch
+        self.handle = None
+        self.params, self.grads, n = list(params), list(grads), len(params)
+        self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
+        self.device = self.params[0].device if n else torch.device("cuda", torch.cuda.current_device())
+
+        def each(name, v):
+            v = list(v) if isinstance(v, (list, tuple)) else [v] * n
+            if len(v) != n:
+                raise StageError(STAGE_EINVAL, f"{name}: {len(v)} values for {n} tensors")
+            return v
+
+        decay, scale = each("weight_decay", weight_decay), each("lr_scale", lr_scale)
+        self.state_bits = [int(b) for b in each("state_bits", state_bits)]
+        if len(self.grads) != n:
+            raise StageError(STAGE_EINVAL, f"{len(self.grads)} gradients for {n} tensors")
+        if any(b not in (8, 32) for b in self.state_bits):
+            raise StageError(STAGE_EINVAL, "state_bits must be 32 or 8")
+        types = (torch.float32, torch.bfloat16)
+        for i, (p, g) in enumerate(zip(self.params, self.grads)):
+            self._fits(f"params[{i}]", p, p.shape, types)
+            self._fits(f"grads[{i}]", g, p.shape, types)
+        self.state = self._new_state(bool(master)) if state is None else self._given_state(state)
+        self.norm = torch.zeros(1, device=self.device)
+        self._make(decay, scale)
+
+    def _fits(self, name, t, shape, types):
+        if t.dtype not in types or t.device != self.device or not t.is_cuda or not t.is_contiguous() or \
+                tuple(t.shape) != tuple(shape):
+            raise StageError(STAGE_EINVAL, f"{name} must be contiguous {' or '.join(map(str, types))} "
+                                           f"{list(shape)} on {self.device}")
+
+    def _types(self, i):
+        """(type and shape of each state of tensor i or None) by name."""
+        import torch
+        p, eight = self.params[i], self.state_bits[i] == 8
+        blocks = ((p.numel() + 255) // 256,)
+        return {"exp_avg": (torch.float8_e4m3fn if eight else torch.float32, p.shape),
+                "exp_avg_sq": (torch.float8_e5m2 if eight else torch.float32, p.shape),
+                "exp_avg_scale": (torch.float32, blocks) if eight else None,
+                "exp_avg_sq_scale": (torch.float32, blocks) if eight else None,
+                "master": (torch.float32, p.shape) if p.dtype == torch.bfloat16 else None}
+
+    def _new_state(self, master):
+        import torch
+        s = {n: [] for n in self.LISTS}
+        for i, p in enumerate(self.params):
+            for n, t in self._types(i).items():
+                if t is None or (n == "master" and not master):
+                    s[n].append(None)
+                elif n == "master":
+                    s[n].append(p.detach().float())
+                else:
+                    s[n].append(torch.zeros(t[1], device=self.device).to(t[0]))
+        s["steps"] = torch.zeros(1, dtype=torch.int64, device=self.device)
+        return s
+
+    def _given_state(self, state):
+        import torch
+        s = {n: list(state[n]) for n in self.LISTS}
+        s["steps"] = state["steps"]
+        self._fits("steps", s["steps"], (1,), (torch.int64,))
+        for n in self.LISTS:
+            if len(s[n]) != len(self.params):
+                raise StageError(STAGE_EINVAL, f"{n}: {len(s[n])} entries for {len(self.params)} tensors")
+        for i in range(len(self.params)):
+            for n, t in self._types(i).items():
+                if t is None or (n == "master" and s[n][i] is None):
+                    if s[n][i] is not None:
+                        raise StageError(STAGE_EINVAL, f"{n}[{i}] must be None")
+                elif s[n][i] is None:
+                    raise StageError(STAGE_EINVAL, f"{n}[{i}] is missing")
+                else:
+                    self._fits(f"{n}[{i}]", s[n][i], t[1], (t[0],))
+        return s
+
+    def _make(self, decay, scale):
+        import torch
+        code = {torch.float32: STAGE_F32, torch.bfloat16: STAGE_BF16}
+        table = (_AdamWTensor * max(len(self.params), 1))()
+        for i, (p, g) in enumerate(zip(self.params, self.grads)):
+            m, v, ms, vs, w = (self.state[n][i] for n in self.LISTS)
+            table[i] = _AdamWTensor(_ptr(p), _ptr(g), _ptr(m), _ptr(v), _ptr(ms), _ptr(vs), _ptr(w), p.numel(),
+                                    code[p.dtype], code[g.dtype], self.state_bits[i], decay[i], scale[i])
+        out, lib = ctypes.c_void_p(), load_library()
+        with torch.cuda.device(self.device):
+            st = lib.adamw_init(table, len(self.params), _ptr(self.state["steps"]), ctypes.byref(out))
+        if st != STAGE_OK:
+            raise StageError(st, (lib.adamw_last_error() or b"").decode())
+        self.handle = out.value
+
+    def step(self, lr, max_norm=None):
+        """One step at rate lr (a number, or fp32 [1] on the GPU that the step reads, so that a
+        captured one follows it) on the current stream.  max_norm: gradients are clipped by their
+        global norm; returns that norm before clipping (fp32 [1] on the GPU, the same tensor for
+        every step), else None.  With max_norm a step whose norm is not finite changes nothing."""
+        fn, dev = (_ops_module or _ops_setup()).adamw, self.device.index
+        a = (self.handle or 0, dev, lr, self.betas[0], self.betas[1], self.eps, max_norm, self.norm)
+        r = fn(*a)
+        if r is not None:
+            _attn_on(r, fn, *a)
+        return None if max_norm is None else self.norm
+
+    def reset_master(self):
+        """The master copies as the parameters now are (after something else changed those)."""
+        for p, w in zip(self.params, self.state["master"]):
+            if w is not None:
+                w.copy_(p)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            load_library().adamw_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 # ---------------------------------------------------------------------------

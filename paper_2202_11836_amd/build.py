@@ -2,8 +2,8 @@
 
 Compiles every ``csrc/*.hip`` with hipcc for gfx950 (and the host-only
 ``csrc/*.cpp``) and links them into
-``paper_2202_11836_amd/libskystage.so``, and ``csrc/py`` into the Python module
-``_attn_call.so`` beside it.  Always recompiles (the caller asks
+``paper_2202_11836_amd/libskystage.so``, and ``csrc/py`` into the Python modules
+``_attn_call.so`` and ``_ops_call.so`` beside it.  Always recompiles (the caller asks
 for a fresh build); sources compile in parallel.
 """
 from __future__ import annotations
@@ -49,27 +49,33 @@ def _compile(src: str) -> str:
     return obj
 
 
+# Python modules of host code (csrc/py) that marshal the operators' calls.
+BINDINGS = {"_attn_call": "attn_call.cpp", "_ops_call": "ops_call.cpp"}
+
+
 def build_binding() -> Optional[str]:
-    """The Python module that marshals the attention operators' calls (host code): by
-    $CXX, g++ or hipcc.  None, with no module left, where Python's headers are not
-    installed: the stage and the allocator do without, and the operators' first call
-    from Python says what is missing."""
+    """The Python modules that marshal the operators' calls (host code): by $CXX, g++ or
+    hipcc; the path of the attention operators' one.  None, with no module left, where
+    Python's headers are not installed: the stage and the allocator do without, and the
+    operators' first call from Python says what is missing."""
     import sysconfig
-    src = os.path.join(CSRC, "py", "attn_call.cpp")
-    path = os.path.join(PKG, "_attn_call.so")
     include = sysconfig.get_paths()["include"]
+    paths = {name: os.path.join(PKG, name + ".so") for name in BINDINGS}
     if not os.path.exists(os.path.join(include, "Python.h")):
-        print(f"_attn_call not built: no Python.h in {include}", file=sys.stderr)
-        if os.path.exists(path):
-            os.remove(path)
+        print(f"{', '.join(BINDINGS)} not built: no Python.h in {include}", file=sys.stderr)
+        for path in paths.values():
+            if os.path.exists(path):
+                os.remove(path)
         return None
-    cmd = [os.environ.get("CXX") or shutil.which("g++") or HIPCC, "-O2", "-std=c++17", "-fPIC",
-           "-shared", "-I" + include, src, "-o", path + ".tmp"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"{src}:\n{r.stderr}")
-    os.replace(path + ".tmp", path)
-    return path
+    for name, path in paths.items():
+        src = os.path.join(CSRC, "py", BINDINGS[name])
+        cmd = [os.environ.get("CXX") or shutil.which("g++") or HIPCC, "-O2", "-std=c++17", "-fPIC",
+               "-shared", "-I" + include, src, "-o", path + ".tmp"]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"{src}:\n{r.stderr}")
+        os.replace(path + ".tmp", path)
+    return paths["_attn_call"]
 
 
 def build(verbose: bool = False) -> str:

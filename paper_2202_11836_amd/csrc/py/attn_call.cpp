@@ -3,14 +3,8 @@
 // interpreter would (one token: 9.2 us a call with these checks in Python, 5.9 here, of
 // which the launch takes about 3.5).
 // The library's functions come as addresses, so this module links to neither it nor torch.
-#define PY_SSIZE_T_CLEAN
-#include <Python.h>
-
-#include <climits>
-#include <cstdarg>
-#include <cstdio>
-
 #include "../../../include/attn.h"
+#include "call.h"
 
 namespace {
 
@@ -24,96 +18,8 @@ ForwardFn forward_fn;
 BackwardFn backward_fn;
 ErrorFn error_fn;
 
-// Set by setup(): what is taken from torch and the binding.
-PyObject *stage_error, *bf16, *f32, *u8, *i32, *current_device, *current_stream, *new_workspace;
-// Names of attributes
-PyObject *n_shape, *n_stride, *n_dtype, *n_get_device, *n_data_ptr, *n_new_empty, *n_addr;
-PyObject* kw_dtype;
-
-// Owns a reference.
-struct Ref {
-  PyObject* p;
-  explicit Ref(PyObject* p_ = nullptr) : p(p_) {}
-  ~Ref() { Py_XDECREF(p); }
-  Ref(const Ref&) = delete;
-  Ref& operator=(const Ref&) = delete;
-  void set(PyObject* q) {
-    Py_XDECREF(p);
-    p = q;
-  }
-  PyObject* release() {
-    PyObject* q = p;
-    p = nullptr;
-    return q;
-  }
-};
-
-bool raise(int status, const char* msg) {
-  Ref e(PyObject_CallFunction(stage_error, "is", status, msg));
-  if (e.p) PyErr_SetObject(stage_error, e.p);
-  return false;
-}
-bool refuse(const char* fmt, ...) {
-  char msg[256];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(msg, sizeof(msg), fmt, ap);
-  va_end(ap);
-  return raise(STAGE_EINVAL, msg);
-}
 // The library's status as an exception.
 bool done(stage_status st) { return st == STAGE_OK || raise((int)st, error_fn()); }
-
-// What a call needs to know of a tensor.
-struct Tensor {
-  int nd = 0, dev = -1;
-  int64_t size[4], stride[4];
-  PyObject* dtype = nullptr;  // (borrowed: compared only)
-  void* p = nullptr;
-};
-
-bool ints(PyObject* t, int n, int64_t* out) {
-  for (int i = 0; i < n; ++i) {
-    out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
-    if (out[i] == -1 && PyErr_Occurred()) return false;
-  }
-  return true;
-}
-
-bool load(const char* name, PyObject* t, Tensor* o) {
-  Ref shape(PyObject_GetAttr(t, n_shape));
-  if (!shape.p) return false;
-  Ref stride(PyObject_CallMethodNoArgs(t, n_stride));
-  if (!stride.p) return false;
-  if (!PyTuple_Check(shape.p) || !PyTuple_Check(stride.p) ||
-      PyTuple_GET_SIZE(shape.p) != PyTuple_GET_SIZE(stride.p))
-    return refuse("%s is not a tensor", name);
-  if (PyTuple_GET_SIZE(shape.p) > 4) return refuse("%s has more than four dimensions", name);
-  o->nd = (int)PyTuple_GET_SIZE(shape.p);
-  if (!ints(shape.p, o->nd, o->size) || !ints(stride.p, o->nd, o->stride)) return false;
-  Ref dtype(PyObject_GetAttr(t, n_dtype));
-  if (!dtype.p) return false;
-  o->dtype = dtype.p;
-  Ref dev(PyObject_CallMethodNoArgs(t, n_get_device));
-  if (!dev.p) return false;
-  o->dev = (int)PyLong_AsLong(dev.p);
-  if (o->dev == -1 && PyErr_Occurred()) return false;
-  Ref p(PyObject_CallMethodNoArgs(t, n_data_ptr));
-  if (!p.p) return false;
-  o->p = PyLong_AsVoidPtr(p.p);
-  return o->p || !PyErr_Occurred();
-}
-
-const char* name_of(PyObject* dtype) {
-  return dtype == bf16 ? "bfloat16" : dtype == f32 ? "float32" : dtype == u8 ? "uint8" : "int32";
-}
-
-bool same(const Tensor& t, int nd, const int64_t* size, PyObject* dtype, int dev) {
-  if (t.nd != nd || t.dtype != dtype || t.dev != dev) return false;
-  for (int i = 0; i < nd; ++i)
-    if (t.size[i] != size[i]) return false;
-  return true;
-}
 
 // Whether a tensor is an operand [batch, length, heads, 64] of this shape and type; its
 // strides into st.
@@ -128,27 +34,6 @@ bool fits(const char* name, const Tensor& t, const int64_t* size, PyObject* dtyp
 bool operand(const char* name, PyObject* obj, const int64_t* size, PyObject* dtype, int dev, Tensor* t,
              int64_t* st) {
   return load(name, obj, t) && fits(name, *t, size, dtype, dev, st);
-}
-
-// A contiguous tensor of nd dimensions; None leaves *p alone where it may.
-bool plain(const char* name, PyObject* obj, int nd, int64_t a, int64_t b, int64_t c, PyObject* dtype,
-           int dev, void** p) {
-  const int64_t size[3] = {a, b, c};
-  Tensor t;
-  if (!load(name, obj, &t)) return false;
-  bool ok = same(t, nd, size, dtype, dev);
-  int64_t step = 1;
-  const bool empty = a == 0 || (nd > 1 && b == 0) || (nd > 2 && c == 0);
-  for (int i = nd - 1; ok && i >= 0; --i) {
-    if (!empty && size[i] > 1) ok = t.stride[i] == step;
-    step *= size[i];
-  }
-  if (!ok)
-    return refuse("%s must be contiguous %s, %d dimensions of %lld, %lld, %lld, on cuda:%d", name,
-                  name_of(dtype), nd, (long long)a, (long long)(nd > 1 ? b : 1),
-                  (long long)(nd > 2 ? c : 1), dev);
-  *p = t.p;
-  return true;
 }
 
 // What both calls take.
@@ -213,49 +98,9 @@ bool inputs(PyObject* q, PyObject* k, PyObject* v, PyObject* key_mask, PyObject*
   return q_pos == Py_None || plain("q_pos", q_pos, 1, t.size[0], 1, 1, i32, t.dev, &in->pos);
 }
 
-// The current device as 1 where it is dev, 0 where not, -1 for an error.
-int on_device(int dev) {
-  Ref now(PyObject_CallNoArgs(current_device));
-  if (!now.p) return -1;
-  const long d = PyLong_AsLong(now.p);
-  return d == -1 && PyErr_Occurred() ? -1 : d == dev;
-}
-
-// A call's stream and workspace.  The workspace comes from torch's allocator, which gives
-// no memory of a stream (or of a captured graph) away while work on it may still use it.
-struct Room {
-  Ref ws;
-  void* p = nullptr;
-  size_t bytes = 0;
-  void* stream = nullptr;
-};
 bool room(const Inputs& in, int backward, Room* r) {
-  if (!done(workspace_fn(&in.s, in.rp, backward, &r->bytes))) return false;
-  Ref dev(PyLong_FromLong(in.dev));
-  if (!dev.p) return false;
-  if (r->bytes) {
-    Ref n(PyLong_FromSize_t(r->bytes));
-    if (!n.p) return false;
-    r->ws.set(PyObject_CallFunctionObjArgs(new_workspace, n.p, dev.p, nullptr));
-    if (!r->ws.p) return false;
-    Ref p(PyObject_CallMethodNoArgs(r->ws.p, n_data_ptr));
-    if (!p.p) return false;
-    r->p = PyLong_AsVoidPtr(p.p);
-  }
-  Ref st(PyObject_CallOneArg(current_stream, dev.p));
-  if (!st.p) return false;
-  r->stream = PyLong_AsVoidPtr(st.p);
-  return !PyErr_Occurred();
-}
-
-// given, or an uninitialised tensor shaped like `like` if it is None.
-PyObject* output(PyObject* given, PyObject* like) {
-  if (given != Py_None) {
-    Py_INCREF(given);
-    return given;
-  }
-  Ref shape(PyObject_GetAttr(like, n_shape));
-  return shape.p ? PyObject_CallMethodOneArg(like, n_new_empty, shape.p) : nullptr;
+  size_t bytes = 0;
+  return done(workspace_fn(&in.s, in.rp, backward, &bytes)) && take_room(in.dev, bytes, r);
 }
 
 // forward(q, k, v, key_mask, scale, causal, q_pos, relpos, table, out, lse): (out, lse), or the
@@ -358,20 +203,8 @@ PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return nullptr;
   }
   void* f[4];
-  for (int i = 0; i < 4; ++i) {
-    f[i] = PyLong_AsVoidPtr(a[i]);
-    if (!f[i]) {
-      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a null address");
-      return nullptr;
-    }
-  }
-  PyObject** const to[8] = {&stage_error, &bf16, &f32, &u8, &i32, &current_device, &current_stream,
-                            &new_workspace};
-  for (int i = 0; i < 8; ++i) {
-    Py_INCREF(a[4 + i]);
-    Py_XDECREF(*to[i]);
-    *to[i] = a[4 + i];
-  }
+  if (!addresses(a, 4, f)) return nullptr;
+  set_common(a + 4);
   forward_fn = (ForwardFn)f[1];
   backward_fn = (BackwardFn)f[2];
   error_fn = (ErrorFn)f[3];
@@ -390,15 +223,5 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_attn_call", nullptr, -1, methods,
 }  // namespace
 
 PyMODINIT_FUNC PyInit__attn_call(void) {
-  struct {
-    PyObject** to;
-    const char* name;
-  } const names[] = {{&n_shape, "shape"},         {&n_stride, "stride"},
-                     {&n_dtype, "dtype"},         {&n_get_device, "get_device"},
-                     {&n_data_ptr, "data_ptr"},   {&n_new_empty, "new_empty"},
-                     {&n_addr, "addr"}};
-  for (const auto& e : names)
-    if (!(*e.to = PyUnicode_InternFromString(e.name))) return nullptr;
-  if (!(kw_dtype = PyTuple_Pack(1, n_dtype))) return nullptr;
-  return PyModule_Create(&module);
+  return intern_names() ? PyModule_Create(&module) : nullptr;
 }
