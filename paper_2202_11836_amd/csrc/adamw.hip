@@ -20,7 +20,7 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int CHUNK = THREADS * 8;  // elements: eight a thread, a block of 8-bit states 32 threads
-constexpr int MOST_GROUPS = 2048;   // work-groups: 8 to a CU
+constexpr int MOST_GROUPS = 512;    // work-groups, 2 to a CU
 constexpr int MOST_PARTS = 1024;    // work-groups of the norm
 
 enum Kind : int { P_F32, P_BF16_MASTER, P_BF16 };
@@ -38,9 +38,12 @@ struct Tensor {
 struct Chunk {
   int tensor, index;  // elements [index * CHUNK, ...) of the tensor
 };
+// (the tables never change, and all threads of a work-group read the same entry: scalar loads)
+typedef const __attribute__((address_space(4))) Tensor* TensorTable;
+typedef const __attribute__((address_space(4))) Chunk* ChunkTable;
 struct StepArgs {
-  const Tensor* tensors;
-  const Chunk* chunks;
+  TensorTable tensors;
+  ChunkTable chunks;
   int n_chunks;
   int64_t* steps;
   unsigned* ticket;     // 0 between launches
@@ -54,22 +57,34 @@ struct StepArgs {
   float eps;
 };
 
-// Eight elements, element-aligned 16-byte accesses; n >= 8 of them, or the first n.
+// The tensors' addresses come from memory: accesses through them are told to be global.
+template <typename V, typename T>
+__device__ __forceinline__ V get(const T* p) {
+  return *(const __attribute__((address_space(1))) V*)(uintptr_t)p;
+}
+template <typename V, typename T>
+__device__ __forceinline__ void put(T* p, V v) {
+  *(__attribute__((address_space(1))) V*)(uintptr_t)p = v;
+}
+
+// Eight elements, element-aligned accesses of 8 and 16 bytes; FULL, or the first n.
+template <bool FULL>
 __device__ __forceinline__ void load8(const float* p, int64_t n, float v[8]) {
   typedef f32x4_t __attribute__((aligned(4))) any_t;
-  if (n >= 8) {
-    const f32x4_t a = *(const any_t*)p, b = *(const any_t*)(p + 4);
+  if (FULL || n >= 8) {
+    const f32x4_t a = get<any_t>(p), b = get<any_t>(p + 4);
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = a[k], v[4 + k] = b[k];
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < n ? p[k] : 0.0f;
+    for (int k = 0; k < 8; ++k) v[k] = k < n ? get<float>(p + k) : 0.0f;
   }
 }
+template <bool FULL>
 __device__ __forceinline__ void load8(const bf16_t* p, int64_t n, float v[8]) {
   typedef u32x4_t __attribute__((aligned(2))) any_t;
-  if (n >= 8) {
-    const u32x4_t a = *(const any_t*)p;
+  if (FULL || n >= 8) {
+    const u32x4_t a = get<any_t>(p);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       v[2 * k] = __uint_as_float(a[k] << 16);
@@ -77,96 +92,130 @@ __device__ __forceinline__ void load8(const bf16_t* p, int64_t n, float v[8]) {
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < n ? bf2f(p[k]) : 0.0f;
+    for (int k = 0; k < 8; ++k) v[k] = k < n ? bf2f(get<bf16_t>(p + k)) : 0.0f;
   }
 }
+template <bool FULL>
+__device__ __forceinline__ u32x2_t load8(const uint8_t* p, int64_t n) {
+  typedef u32x2_t __attribute__((aligned(1))) any_t;
+  if (FULL || n >= 8) return get<any_t>(p);
+  u32x2_t r = {0, 0};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) r[k >> 2] |= (k < n ? (uint32_t)get<uint8_t>(p + k) : 0) << (8 * (k & 3));
+  return r;
+}
+template <bool FULL>
 __device__ __forceinline__ void store8(float* p, int64_t n, const float v[8]) {
   typedef f32x4_t __attribute__((aligned(4))) any_t;
-  if (n >= 8) {
-    *(any_t*)p = f32x4_t{v[0], v[1], v[2], v[3]};
-    *(any_t*)(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+  if (FULL || n >= 8) {
+    put<any_t>(p, f32x4_t{v[0], v[1], v[2], v[3]});
+    put<any_t>(p + 4, f32x4_t{v[4], v[5], v[6], v[7]});
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (k < n) p[k] = v[k];
+      if (k < n) put<float>(p + k, v[k]);
   }
 }
-__device__ __forceinline__ void store8(bf16_t* p, int64_t n, const bf16_t v[8]) {
+template <bool FULL>
+__device__ __forceinline__ void store8(bf16_t* p, int64_t n, u32x4_t r) {
   typedef u32x4_t __attribute__((aligned(2))) any_t;
-  if (n >= 8) {
-    u32x4_t r;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = v[2 * k] | (uint32_t)v[2 * k + 1] << 16;
-    *(any_t*)p = r;
+  if (FULL || n >= 8) {
+    put<any_t>(p, r);
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (k < n) p[k] = v[k];
+      if (k < n) put<bf16_t>(p + k, (bf16_t)(r[k >> 1] >> (16 * (k & 1))));
   }
 }
-__device__ __forceinline__ void load8(const uint8_t* p, int64_t n, uint8_t v[8]) {
+template <bool FULL>
+__device__ __forceinline__ void store8(uint8_t* p, int64_t n, const uint32_t c[8]) {
   typedef u32x2_t __attribute__((aligned(1))) any_t;
-  if (n >= 8) {
-    const u32x2_t a = *(const any_t*)p;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = (uint8_t)(a[k >> 2] >> (8 * (k & 3)));
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < n ? p[k] : 0;
-  }
-}
-__device__ __forceinline__ void store8(uint8_t* p, int64_t n, const uint32_t v[8]) {
-  typedef u32x2_t __attribute__((aligned(1))) any_t;
-  if (n >= 8) {
-    u32x2_t r;
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-      r[k] = v[4 * k] | v[4 * k + 1] << 8 | v[4 * k + 2] << 16 | v[4 * k + 3] << 24;
-    *(any_t*)p = r;
+  if (FULL || n >= 8) {
+    put<any_t>(p, u32x2_t{c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24,
+                          c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24});
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (k < n) p[k] = (uint8_t)v[k];
+      if (k < n) put<uint8_t>(p + k, (uint8_t)c[k]);
   }
 }
 
-// e4m3 and e5m2 codes (no infinities or NaNs among them: codes stay below) by their bits: a
-// normal one is a float's exponent and leading mantissa bits, a subnormal one counts
-// 2^-9 or 2^-16.
-__device__ __forceinline__ float from_e4m3(uint32_t c) {
-  const uint32_t a = c & 0x7f;
-  const float f = a < 8 ? (float)a * 0x1p-9f : __uint_as_float((a + (120 << 3)) << 20);
-  return c & 0x80 ? -f : f;
+// The values of eight codes times their scale: the device's own conversions, exact.
+__device__ __forceinline__ void from_e4m3(u32x2_t c, float scale, float v[8]) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[k], false);
+    const f32x2_t b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[k], true);
+    v[4 * k] = a[0] * scale, v[4 * k + 1] = a[1] * scale;
+    v[4 * k + 2] = b[0] * scale, v[4 * k + 3] = b[1] * scale;
+  }
 }
-__device__ __forceinline__ float from_e5m2(uint32_t c) {
-  return c < 4 ? (float)c * 0x1p-16f : __uint_as_float((c + (112 << 2)) << 21);
+__device__ __forceinline__ void from_e5m2(u32x2_t c, float scale, float v[8]) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_bf8((int)c[k], false);
+    const f32x2_t b = __builtin_amdgcn_cvt_pk_f32_bf8((int)c[k], true);
+    v[4 * k] = a[0] * scale, v[4 * k + 1] = a[1] * scale;
+    v[4 * k + 2] = b[0] * scale, v[4 * k + 3] = b[1] * scale;
+  }
 }
-// The code of |x| <= 448 (x times a block's scale): up where its part beyond the last bit and
-// r / 2^16 come to a step.
-__device__ __forceinline__ uint32_t to_e4m3(float x, uint32_t r) {
-  const float a = fabsf(x);
-  const uint32_t c = a < 0x1p-6f ? ((uint32_t)(a * 0x1p25f) + r) >> 16
-                                 : ((__float_as_uint(a) + (r << 4)) >> 20) - (120 << 3);
-  return min(c, 0x7eu) | (__float_as_uint(x) >> 31 << 7);
+// Codes of eight x with |x| <= 448 (values times their block's inverse scale): up where the
+// part beyond the last bit and r / 2^16 come to a step.  A normal code is a float's exponent
+// and leading mantissa bits, so the sum may carry into either; a subnormal one counts 2^-9,
+// and few meet one (below 2^-15 of a block's largest), so a wavefront branches for it.
+__device__ __forceinline__ void to_e4m3(const float x[8], const uint32_t r[8], uint32_t c[8]) {
+  float least = fabsf(x[0]);
+#pragma unroll
+  for (int k = 1; k < 8; ++k) least = fminf(least, fabsf(x[k]));
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t b = __float_as_uint(x[k]);
+    c[k] = min(((b & 0x7fffffffu) + ((r[k] & 0xffffu) << 4)) >> 20, 0x7eu + 960u) - 960u | (b >> 24 & 0x80u);
+  }
+  if (__builtin_amdgcn_ballot_w64(least < 0x1p-6f)) {
+    asm volatile("");  // (not to be made part of the way without)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t b = __float_as_uint(x[k]), n = ((uint32_t)(fabsf(x[k]) * 0x1p25f) + (r[k] & 0xffffu)) >> 16;
+      if (fabsf(x[k]) < 0x1p-6f) c[k] = n | (b >> 24 & 0x80u);
+    }
+  }
 }
-// The same for 0 <= x <= 57344; x > 0 has a code above 0.
-__device__ __forceinline__ uint32_t to_e5m2(float x, uint32_t r) {
-  const uint32_t c = x < 0x1p-14f ? ((uint32_t)(x * 0x1p32f) + r) >> 16
-                                  : ((__float_as_uint(x) + (r << 5)) >> 21) - (112 << 2);
-  return min(max(c, x > 0.0f ? 1u : 0u), 0x7bu);
+// The same for 0 <= x <= 57344 and the high halves of r; x > 0 has a code above 0.
+__device__ __forceinline__ void to_e5m2(const float x[8], const uint32_t r[8], uint32_t c[8]) {
+  float least = x[0];
+#pragma unroll
+  for (int k = 1; k < 8; ++k) least = fminf(least, x[k]);
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    c[k] = min((__float_as_uint(x[k]) + (r[k] >> 16 << 5)) >> 21, 0x7bu + 448u) - 448u;
+  if (__builtin_amdgcn_ballot_w64(least < 0x1p-14f)) {
+    asm volatile("");
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t n = ((uint32_t)(x[k] * 0x1p32f) + (r[k] >> 16)) >> 16;
+      if (x[k] < 0x1p-14f) c[k] = max(n, x[k] > 0.0f ? 1u : 0u);
+    }
+  }
 }
-// A block's scale and its inverse from the bits of its largest |value| (NaN above all): 0 for
-// values too small for the inverse, NaN where one is not finite.
-__device__ __forceinline__ float2 scale_of(uint32_t top, float most) {
+// A block's scale and its inverse from the bits of its largest |value| (NaN above all), both
+// rounded as a division is: 0 for values too small for the inverse, NaN where one is not
+// finite.  The scale's quotient by `most`, 7 times a power of 2, is a product with its rounded
+// reciprocal and one correction, which is exact there (P. Markstein, 1990).
+__device__ __forceinline__ float2 scale_of(uint32_t top, float most, float reciprocal) {
   const float f = __uint_as_float(top);
   if (top >= 0x7f800000u) return {__uint_as_float(0x7fc00000u), 0.0f};
   if (f < 0x1p-110f) return {0.0f, 0.0f};
-  return {f / most, most / f};
+  const float q = f * reciprocal;
+  return {fmaf(fmaf(-most, q, f), reciprocal, q), most / f};
 }
-__device__ __forceinline__ uint32_t max32(uint32_t v) {  // over 32 lanes
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-  return v;
+// The largest over 32 lanes, to all of them.
+__device__ __forceinline__ uint32_t max32(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true));   // lane ^ 1
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true));   // lane ^ 2
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true));  // lane ^ 7
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xf, 0xf, true));  // lane ^ 15
+  return max(v, (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x401F));           // lane ^ 16
 }
 // Random bits of element i at step t (adamw.h).
 __device__ __forceinline__ uint32_t random_bits(uint32_t i, uint32_t t) {
@@ -184,86 +233,108 @@ struct Step {  // what all elements of a step share
   uint32_t t;
 };
 
-// Eight elements from i of a tensor.
-template <int KIND, bool GRAD_BF16, int BITS>
-__device__ __forceinline__ void update8(const Tensor& x, int64_t i, const Step& s) {
-  // (the states' operations are rounded one by one, as they are defined)
+// New states of eight elements, from gradients g: each operation rounded by itself, as they
+// are defined.
+__device__ __forceinline__ void new_states(const float g[8], const Step& s, float m[8], float v[8]) {
 #pragma clang fp contract(off)
-  const int64_t n = x.n - i;
-  float w[8], g[8], m[8], v[8];
-  if constexpr (KIND == P_F32) load8((const float*)x.p + i, n, w);
-  else if constexpr (KIND == P_BF16_MASTER) load8(x.master + i, n, w);
-  else load8((const bf16_t*)x.p + i, n, w);
-  if constexpr (GRAD_BF16) load8((const bf16_t*)x.g + i, n, g);
-  else load8((const float*)x.g + i, n, g);
-  const int64_t block = i / ADAMW_BLOCK;
-  if constexpr (BITS == 8) {
-    uint8_t cm[8], cv[8];
-    load8((const uint8_t*)x.m + i, n, cm);
-    load8((const uint8_t*)x.v + i, n, cv);
-    const float sm = n > 0 ? x.m_scale[block] : 0.0f, sv = n > 0 ? x.v_scale[block] : 0.0f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) m[k] = from_e4m3(cm[k]) * sm, v[k] = from_e5m2(cv[k]) * sv;
-  } else {
-    load8((const float*)x.m + i, n, m);
-    load8((const float*)x.v + i, n, v);
-  }
-  const float keep = 1.0f - s.lr * x.lr_scale * x.decay, rate = s.lr_bias * x.lr_scale;
-  uint32_t top_m = 0, top_v = 0;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const float d = g[k] * s.clip;
     m[k] = m[k] * s.b1 + d * s.c1;
     v[k] = v[k] * s.b2 + d * d * s.c2;
+  }
+}
+
+// Eight elements from i of a tensor: all of them (FULL), or those of it.
+template <int KIND, bool GRAD_BF16, int BITS, bool FULL>
+__device__ __forceinline__ void update8(const Tensor& x, int64_t i, const Step& s) {
+  const int64_t n = x.n - i;
+  float w[8], g[8], m[8], v[8];
+  if constexpr (KIND == P_F32) load8<FULL>((const float*)x.p + i, n, w);
+  else if constexpr (KIND == P_BF16_MASTER) load8<FULL>(x.master + i, n, w);
+  else load8<FULL>((const bf16_t*)x.p + i, n, w);
+  if constexpr (GRAD_BF16) load8<FULL>((const bf16_t*)x.g + i, n, g);
+  else load8<FULL>((const float*)x.g + i, n, g);
+  const int64_t block = i / ADAMW_BLOCK;
+  if constexpr (BITS == 8) {
+    const u32x2_t cm = load8<FULL>((const uint8_t*)x.m + i, n), cv = load8<FULL>((const uint8_t*)x.v + i, n);
+    const bool here = FULL || n > 0;
+    from_e4m3(cm, here ? get<float>(x.m_scale + block) : 0.0f, m);
+    from_e5m2(cv, here ? get<float>(x.v_scale + block) : 0.0f, v);
+  } else {
+    load8<FULL>((const float*)x.m + i, n, m);
+    load8<FULL>((const float*)x.v + i, n, v);
+  }
+  new_states(g, s, m, v);
+  const float keep = 1.0f - s.lr * x.lr_scale * x.decay, rate = s.lr_bias * x.lr_scale;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
     // (square root and reciprocal of 1 ulp: a change of w, not w, is off by that)
-    const float den = __builtin_amdgcn_sqrtf(v[k]) * s.inv_root + s.eps;
-    w[k] = w[k] * keep - rate * m[k] * __builtin_amdgcn_rcpf(den);
-    top_m = max(top_m, __float_as_uint(m[k]) & 0x7fffffffu);
-    top_v = max(top_v, __float_as_uint(v[k]) & 0x7fffffffu);
+    const float den = fmaf(__builtin_amdgcn_sqrtf(v[k]), s.inv_root, s.eps);
+    w[k] = fmaf(w[k], keep, -(rate * m[k] * __builtin_amdgcn_rcpf(den)));
   }
   uint32_t r[8];
   if constexpr (BITS == 8 || KIND == P_BF16)
 #pragma unroll
     for (int k = 0; k < 8; ++k) r[k] = random_bits((uint32_t)i + k, s.t);
   if constexpr (KIND == P_F32) {
-    store8((float*)x.p + i, n, w);
+    store8<FULL>((float*)x.p + i, n, w);
   } else {
-    bf16_t b[8];
+    u32x4_t b;
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      b[k] = KIND == P_BF16 ? (bf16_t)((__float_as_uint(w[k]) + (r[k] >> 16)) >> 16) : f2bf(w[k]);
-    store8((bf16_t*)x.p + i, n, b);
-    if constexpr (KIND == P_BF16_MASTER) store8(x.master + i, n, w);
+    for (int k = 0; k < 4; ++k)
+      b[k] = KIND == P_BF16 ? (__float_as_uint(w[2 * k]) + (r[2 * k] >> 16)) >> 16 |
+                                  ((__float_as_uint(w[2 * k + 1]) + (r[2 * k + 1] >> 16)) & 0xffff0000u)
+                            : pack_bf16x2(w[2 * k], w[2 * k + 1]);
+    store8<FULL>((bf16_t*)x.p + i, n, b);
+    if constexpr (KIND == P_BF16_MASTER) store8<FULL>(x.master + i, n, w);
   }
   if constexpr (BITS == 8) {
-    const float2 sm = scale_of(max32(top_m), 448.0f), sv = scale_of(max32(top_v), 57344.0f);
-    uint32_t cm[8], cv[8];
+    uint32_t top_m = 0, top_v = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      cm[k] = sm.y == 0.0f ? 0 : to_e4m3(m[k] * sm.y, r[k] & 0xffff);
-      cv[k] = sv.y == 0.0f ? 0 : to_e5m2(v[k] * sv.y, r[k] >> 16);
+      top_m = max(top_m, __float_as_uint(m[k]) & 0x7fffffffu);
+      top_v = max(top_v, __float_as_uint(v[k]));  // (a NaN is above all with either sign)
     }
-    store8((uint8_t*)x.m + i, n, cm);
-    store8((uint8_t*)x.v + i, n, cv);
-    if ((threadIdx.x & 31) == 0 && n > 0) {
-      x.m_scale[block] = sm.x;
-      x.v_scale[block] = sv.x;
+    const float2 sm = scale_of(max32(top_m), 448.0f, 1.0f / 448.0f);
+    const float2 sv = scale_of(max32(top_v), 57344.0f, 1.0f / 57344.0f);
+    uint32_t cm[8], cv[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m[k] *= sm.y, v[k] *= sv.y;
+    to_e4m3(m, r, cm);
+    to_e5m2(v, r, cv);
+    if (sm.y == 0.0f || sv.y == 0.0f)  // (a block of zeros, or one that is not finite)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (sm.y == 0.0f) cm[k] = 0;
+        if (sv.y == 0.0f) cv[k] = 0;
+      }
+    store8<FULL>((uint8_t*)x.m + i, n, cm);
+    store8<FULL>((uint8_t*)x.v + i, n, cv);
+    if ((threadIdx.x & 31) == 0 && (FULL || n > 0)) {
+      put<float>(x.m_scale + block, sm.x);
+      put<float>(x.v_scale + block, sv.x);
     }
   } else {
-    store8((float*)x.m + i, n, m);
-    store8((float*)x.v + i, n, v);
+    store8<FULL>((float*)x.m + i, n, m);
+    store8<FULL>((float*)x.v + i, n, v);
   }
 }
 
+template <int KIND, bool GRAD_BF16, int BITS>
+__device__ __forceinline__ void update_chunk(const Tensor& x, int64_t i, bool full, const Step& s) {
+  if (full) update8<KIND, GRAD_BF16, BITS, true>(x, i, s);
+  else update8<KIND, GRAD_BF16, BITS, false>(x, i, s);
+}
 template <int KIND, bool GRAD_BF16>
-__device__ __forceinline__ void update_bits(const Tensor& x, int64_t i, const Step& s) {
-  if (x.bits == 8) update8<KIND, GRAD_BF16, 8>(x, i, s);
-  else update8<KIND, GRAD_BF16, 32>(x, i, s);
+__device__ __forceinline__ void update_bits(const Tensor& x, int64_t i, bool full, const Step& s) {
+  if (x.bits == 8) update_chunk<KIND, GRAD_BF16, 8>(x, i, full, s);
+  else update_chunk<KIND, GRAD_BF16, 32>(x, i, full, s);
 }
 template <int KIND>
-__device__ __forceinline__ void update_grad(const Tensor& x, int64_t i, const Step& s) {
-  if (x.grad_bf16) update_bits<KIND, true>(x, i, s);
-  else update_bits<KIND, false>(x, i, s);
+__device__ __forceinline__ void update_grad(const Tensor& x, int64_t i, bool full, const Step& s) {
+  if (x.grad_bf16) update_bits<KIND, true>(x, i, full, s);
+  else update_bits<KIND, false>(x, i, full, s);
 }
 
 // beta^t by squaring, in 64 bits.
@@ -286,10 +357,24 @@ __device__ __forceinline__ double group_sum(double v, double* lds) {
   return v;
 }
 
+__device__ __forceinline__ Tensor tensor_at(const StepArgs& a, int j) {
+  TensorTable t = a.tensors + j;
+  return {t->p, t->g, t->m, t->v, t->m_scale, t->v_scale, t->master, t->n, t->decay, t->lr_scale,
+          t->kind, t->grad_bf16, t->bits, 0};
+}
+__device__ __forceinline__ Chunk chunk_at(const StepArgs& a, int c) {
+  return {a.chunks[c].tensor, a.chunks[c].index};
+}
+
+// Two work-groups to a CU that take chunk after chunk: 128 bytes a thread in flight are enough, and
+// what each has to set up (the powers, the norm's parts, a ticket) is done 512 times.  us by
+// work-groups a CU, 1 / 2 / 3 / 4: 50M weights with 8-bit states (0.8 GB) 240 / 150 / 165 / 166, 504M
+// in bf16 (15 GB, clipped) 3365 / 3363 / 3385 / 3383, 5M in fp32 (139 MB, clipped) 31.6 / 32.2 /
+// 31.9 / 33.5; numbers between leave CUs with unequal shares (1.25: 205, 4322, 33.8).
 __global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
   __shared__ double lds[THREADS / 64];
-  __shared__ int64_t steps;
-  if (threadIdx.x == 0) steps = *a.steps;
+  const int64_t t = *a.steps + 1;
+  Chunk ch = chunk_at(a, blockIdx.x);  // (the table has an entry to read where there are no chunks)
   Step s;
   s.clip = 1.0f;
   bool go = true;
@@ -300,17 +385,7 @@ __global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
     go = norm < INFINITY;
     s.clip = norm > a.max_norm ? (float)(a.max_norm / norm) : 1.0f;
     if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
-  } else {
-    __syncthreads();
   }
-  // Every work-group reads the number of steps before it takes a ticket, so the one with the
-  // last ticket may raise it.
-  const int64_t t = steps + 1;
-  if (threadIdx.x == 0 && atomicAdd(a.ticket, 1u) == gridDim.x - 1) {
-    if (go) *a.steps = t;
-    *a.ticket = 0;
-  }
-  if (!go) return;
   const float lr = a.lr_ptr ? *a.lr_ptr : a.lr;
   s.b1 = (float)a.beta1;
   s.c1 = (float)(1.0 - a.beta1);
@@ -321,13 +396,23 @@ __global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
   s.inv_root = (float)(1.0 / sqrt(1.0 - power(a.beta2, t)));
   s.eps = a.eps;
   s.t = (uint32_t)t;
-  for (int c = blockIdx.x; c < a.n_chunks; c += gridDim.x) {
-    const Chunk ch = a.chunks[c];
-    const Tensor& x = a.tensors[ch.tensor];
-    const int64_t i = (int64_t)ch.index * CHUNK + 8 * threadIdx.x;
-    if (x.kind == P_F32) update_grad<P_F32>(x, i, s);
-    else if (x.kind == P_BF16_MASTER) update_grad<P_BF16_MASTER>(x, i, s);
-    else update_grad<P_BF16>(x, i, s);
+  for (int c = blockIdx.x; go && c < a.n_chunks; c += gridDim.x) {
+    const Chunk next = chunk_at(a, min(c + (int)gridDim.x, a.n_chunks - 1));
+    const Tensor x = tensor_at(a, ch.tensor);
+    const int64_t first = (int64_t)ch.index * CHUNK, i = first + 8 * threadIdx.x;
+    const bool full = first + CHUNK <= x.n;
+    if (x.kind == P_F32) update_grad<P_F32>(x, i, full, s);
+    else if (x.kind == P_BF16_MASTER) update_grad<P_BF16_MASTER>(x, i, full, s);
+    else update_grad<P_BF16>(x, i, full, s);
+    ch = next;
+  }
+  // All of a work-group have read the number of steps before it takes a ticket, so the one with
+  // the last ticket may raise it.  (Taken on the way in, the tickets of 2048 work-groups, 9 ns
+  // each, kept them from their work: 139 MB 34.6 -> 48 us.)
+  __syncthreads();
+  if (threadIdx.x == 0 && atomicAdd(a.ticket, 1u) == gridDim.x - 1) {
+    if (go) *a.steps = t;
+    *a.ticket = 0;
   }
 }
 
@@ -337,12 +422,12 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const StepArgs a, double*
   __shared__ double lds[THREADS / 64];
   double sum = 0.0;
   for (int c = blockIdx.x; c < a.n_chunks; c += gridDim.x) {
-    const Chunk ch = a.chunks[c];
-    const Tensor& x = a.tensors[ch.tensor];
+    const Chunk ch = chunk_at(a, c);
+    const Tensor x = tensor_at(a, ch.tensor);
     const int64_t i = (int64_t)ch.index * CHUNK + 8 * threadIdx.x;
     float g[8];
-    if (x.grad_bf16) load8((const bf16_t*)x.g + i, x.n - i, g);
-    else load8((const float*)x.g + i, x.n - i, g);
+    if (x.grad_bf16) load8<false>((const bf16_t*)x.g + i, x.n - i, g);
+    else load8<false>((const float*)x.g + i, x.n - i, g);
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum = fma((double)g[k], (double)g[k], sum);
   }
@@ -439,11 +524,15 @@ stage_status adamw_init(const adamw_tensor* tensors, int n, int64_t* steps, adam
       if (chunks.size() >= (size_t)1 << 30) return bad(STAGE_EINVAL, "too many elements");
       chunks.push_back({j, (int)i});
     }
+  const int n_chunks = (int)chunks.size();
+  // (an entry each to read where there is nothing to do)
+  if (chunks.empty()) chunks.push_back({0, 0});
+  if (host.empty()) host.push_back(Tensor{});
   adamw_t* h = new adamw_t;
   h->steps = steps;
-  h->n_chunks = (int)chunks.size();
+  h->n_chunks = n_chunks;
   const size_t at_ticket = MOST_PARTS * sizeof(double), at_tensors = at_ticket + 64;
-  const size_t at_chunks = at_tensors + (size_t)n * sizeof(Tensor);
+  const size_t at_chunks = at_tensors + host.size() * sizeof(Tensor);
   const size_t bytes = at_chunks + chunks.size() * sizeof(Chunk);
   hipError_t e = hipGetDevice(&h->device);
   if (e == hipSuccess) e = hipMalloc(&h->memory, bytes);
@@ -458,8 +547,9 @@ stage_status adamw_init(const adamw_tensor* tensors, int n, int64_t* steps, adam
   h->tensors = (Tensor*)(base + at_tensors);
   h->chunks = (Chunk*)(base + at_chunks);
   e = hipMemset(base, 0, at_tensors);
-  if (e == hipSuccess && n > 0) e = hipMemcpy(h->tensors, host.data(), n * sizeof(Tensor), hipMemcpyHostToDevice);
-  if (e == hipSuccess && !chunks.empty())
+  if (e == hipSuccess)
+    e = hipMemcpy(h->tensors, host.data(), host.size() * sizeof(Tensor), hipMemcpyHostToDevice);
+  if (e == hipSuccess)
     e = hipMemcpy(h->chunks, chunks.data(), chunks.size() * sizeof(Chunk), hipMemcpyHostToDevice);
   if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
   if (e != hipSuccess) {
@@ -489,8 +579,8 @@ stage_status adamw_step(adamw_t* h, const adamw_args* a, void* hip_stream) {
     return bad(STAGE_EINVAL, "the handle is of device %d, the current one is %d", h->device, device);
   const hipStream_t st = (hipStream_t)hip_stream;
   StepArgs k{};
-  k.tensors = h->tensors;
-  k.chunks = h->chunks;
+  k.tensors = (TensorTable)h->tensors;
+  k.chunks = (ChunkTable)h->chunks;
   k.n_chunks = h->n_chunks;
   k.steps = h->steps;
   k.ticket = h->ticket;
