@@ -35,6 +35,8 @@ struct BwdArgs {
   const float *gamma, *mean, *rstd;
   float *part, *dgamma, *dbeta;  // part [work-groups][2][w]
   int rows, seq, batch, w, rpb;  // rpb: rows of a work-group
+  int threads;                   // of a row of several wavefronts
+  int row_groups;                // COLUMNS: work-groups of rows
 };
 
 // Eight values of a row in their storage type; element-aligned 16-byte accesses (rows of
@@ -128,47 +130,53 @@ __device__ __forceinline__ T* row_at(const Rows& r, int batch, int seq, int row)
   return (T*)r.p + b * r.sb + (int64_t)(row - b * seq) * r.ss;
 }
 
-// Sums over the TPR threads of a row, N of them together.  Up to 64 threads: lanes of a
-// wavefront.  More: its wavefronts meet in LDS, twice buffered by `turn` (one barrier a sum).
+// A row has TPR threads, 8 to 64, or (TPR 0) several wavefronts, up to MOST_WAVES in a work-group.
+constexpr int MOST_WAVES = 16;
+constexpr int BWD_GROUP = 512;  // threads of a backward work-group (rows to 8192)
+
+// Sums over the threads of a row, N of them together: lanes of a wavefront, whose wavefronts meet
+// in LDS, twice buffered by `turn` (one barrier a sum).
 template <int TPR, int N>
-__device__ __forceinline__ void row_sums(float v[N], float* lds, int turn) {
+__device__ __forceinline__ void row_sums(float v[N], float* lds, int turn, int row_waves, int slot) {
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int o = (TPR < 64 ? TPR : 64) / 2; o > 0; o >>= 1) v[i] += __shfl_xor(v[i], o, 64);
-  if constexpr (TPR > 64) {
-    constexpr int W = TPR / 64;
-    float* at = lds + turn * N * W;
+    for (int o = (TPR ? TPR : 64) / 2; o > 0; o >>= 1) v[i] += __shfl_xor(v[i], o, 64);
+  if constexpr (TPR == 0) {
+    float* at = lds + turn * N * MOST_WAVES;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
-      for (int i = 0; i < N; ++i) at[i * W + (threadIdx.x >> 6)] = v[i];
+      for (int i = 0; i < N; ++i) at[i * MOST_WAVES + (threadIdx.x >> 6)] = v[i];
     __syncthreads();
+    at += slot * row_waves;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      float t = at[i * W];
-#pragma unroll
-      for (int j = 1; j < W; ++j) t += at[i * W + j];
+      float t = at[i * MOST_WAVES];
+      for (int j = 1; j < row_waves; ++j) t += at[i * MOST_WAVES + j];
       v[i] = t;
     }
   }
 }
 
-// A row a TPR threads, NC chunks of eight values each: thread j owns chunks j + TPR i.
-template <typename T, int TPR, int NC, bool RES>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void fwd_kernel(const FwdArgs g) {
-  __shared__ float lds[TPR > 64 ? 2 * (TPR / 64) : 1];
-  constexpr int RPB = TPR > 256 ? 1 : 256 / TPR;
-  const int lane = threadIdx.x % TPR;
-  const int row = blockIdx.x * RPB + threadIdx.x / TPR;
-  if (TPR <= 64 && row >= g.rows) return;  // (work-groups of whole rows have no other)
+// NC chunks of eight values a thread: thread j of a row's T owns chunks j + T i.  EARLY: gamma and
+// beta are asked for before the sums, which saves a memory latency, and costs 16 registers a
+// chunk.
+template <typename T, int TPR, int NC, bool RES, bool EARLY>
+__global__ __launch_bounds__(TPR ? 256 : 64 * MOST_WAVES) void fwd_kernel(const FwdArgs g) {
+  __shared__ float lds[TPR ? 1 : 2 * MOST_WAVES];
+  const int threads = TPR ? TPR : blockDim.x;
+  const int lane = TPR ? threadIdx.x % (TPR ? TPR : 1) : threadIdx.x;
+  const int row = TPR ? blockIdx.x * (256 / (TPR ? TPR : 256)) + threadIdx.x / (TPR ? TPR : 1) : blockIdx.x;
+  if (TPR && row >= g.rows) return;
   const T* x = row_at<T>(g.x, g.batch, g.seq, row);
   Chunk<T> c[NC], r[NC];
 #pragma unroll
-  for (int i = 0; i < NC; ++i) load_n(c[i], x + 8 * (lane + TPR * i), g.w - 8 * (lane + TPR * i));
+  for (int i = 0; i < NC; ++i) load_n(c[i], x + 8 * (lane + threads * i), g.w - 8 * (lane + threads * i));
   if constexpr (RES) {
     const T* res = row_at<T>(g.res, g.batch, g.seq, row);
 #pragma unroll
-    for (int i = 0; i < NC; ++i) load_n(r[i], res + 8 * (lane + TPR * i), g.w - 8 * (lane + TPR * i));
+    for (int i = 0; i < NC; ++i)
+      load_n(r[i], res + 8 * (lane + threads * i), g.w - 8 * (lane + threads * i));
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       float v[8];
@@ -179,37 +187,50 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void fwd_kernel(const FwdArg
     if (g.total.p) {
       T* t = row_at<T>(g.total, g.batch, g.seq, row);
 #pragma unroll
-      for (int i = 0; i < NC; ++i) store_n(c[i], t + 8 * (lane + TPR * i), g.w - 8 * (lane + TPR * i));
+      for (int i = 0; i < NC; ++i)
+        store_n(c[i], t + 8 * (lane + threads * i), g.w - 8 * (lane + threads * i));
     }
+  }
+  float ga[NC][8], be[NC][8];
+  if constexpr (EARLY) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int at = 8 * (lane + threads * i);
+      weights(g.gamma, at, g.w - at, 1.0f, ga[i]);
+      weights(g.beta, at, g.w - at, 0.0f, be[i]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
   float s[1] = {0.0f};
 #pragma unroll
   for (int i = 0; i < NC; ++i)
 #pragma unroll
     for (int k = 0; k < 8; ++k) s[0] += c[i].get(k);
-  row_sums<TPR, 1>(s, lds, 0);
+  row_sums<TPR, 1>(s, lds, 0, threads / 64, 0);
   const float mean = s[0] / (float)g.w;
   s[0] = 0.0f;
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    const int n = g.w - 8 * (lane + TPR * i);
+    const int n = g.w - 8 * (lane + threads * i);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const float d = k < n ? c[i].get(k) - mean : 0.0f;
       s[0] += d * d;
     }
   }
-  row_sums<TPR, 1>(s, lds, 1);
+  row_sums<TPR, 1>(s, lds, 1, threads / 64, 0);
   const float rstd = 1.0f / sqrtf(s[0] / (float)g.w + g.eps);
   T* out = row_at<T>(g.out, g.batch, g.seq, row);
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    const int at = 8 * (lane + TPR * i), n = g.w - at;
-    float ga[8], be[8], v[8];
-    weights(g.gamma, at, n, 1.0f, ga);
-    weights(g.beta, at, n, 0.0f, be);
+    const int at = 8 * (lane + threads * i), n = g.w - at;
+    float v[8];
+    if constexpr (!EARLY) {
+      weights(g.gamma, at, n, 1.0f, ga[i]);
+      weights(g.beta, at, n, 0.0f, be[i]);
+    }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = fmaf((c[i].get(k) - mean) * rstd, ga[k], be[k]);
+    for (int k = 0; k < 8; ++k) v[k] = fmaf((c[i].get(k) - mean) * rstd, ga[i][k], be[i][k]);
     c[i].set(v);
     store_n(c[i], out + at, n);
   }
@@ -219,41 +240,105 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void fwd_kernel(const FwdArg
   }
 }
 
-// U rows of a TPR threads at a time, so that the loads of all are on their way together.
-template <typename T, int TPR, int NC, int U, bool GRADS>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void bwd_kernel(const BwdArgs g) {
-  constexpr int THREADS = TPR > 256 ? TPR : 256;
-  constexpr int SLOTS = THREADS / TPR;  // rows side by side
-  constexpr int WAVES = THREADS / 64;
-  __shared__ float lds[TPR > 64 ? 4 * U * (TPR / 64) : 1];
-  const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+// dgamma and dbeta of 64 columns over all rows, by a work-group: 8 chunks side by side, an eighth of
+// its threads' rows at a time, four of a thread's on their way together.
+template <typename T>
+__device__ __forceinline__ void column_sums(const BwdArgs& g, int col0) {
+  __shared__ float red[2][MOST_WAVES][64];
+  const int slots = blockDim.x / 8, waves = blockDim.x / 64;
+  const int chunk = threadIdx.x & 7, at = col0 + 8 * chunk, n = g.w - at;
+  float pg[8], pb[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) pg[k] = pb[k] = 0.0f;
+  for (int first = threadIdx.x >> 3; first < g.rows; first += 4 * slots) {
+    Chunk<T> dy[4], z[4];
+    float mean[4], rstd[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int row = first + slots * u;
+      const bool live = row < g.rows;
+      load_n(dy[u], live ? row_at<T>(g.dy, g.batch, g.seq, row) + at : nullptr, live ? n : 0);
+      load_n(z[u], live ? row_at<T>(g.z, g.batch, g.seq, row) + at : nullptr, live ? n : 0);
+      mean[u] = live ? g.mean[row] : 0.0f;
+      rstd[u] = live ? g.rstd[row] : 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        pg[k] += dy[u].get(k) * ((z[u].get(k) - mean[u]) * rstd[u]);
+        pb[k] += dy[u].get(k);
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+#pragma unroll
+    for (int o = 8; o < 64; o <<= 1) {
+      pg[k] += __shfl_xor(pg[k], o, 64);
+      pb[k] += __shfl_xor(pb[k], o, 64);
+    }
+  if ((threadIdx.x & 63) < 8)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      red[0][threadIdx.x >> 6][8 * chunk + k] = pg[k];
+      red[1][threadIdx.x >> 6][8 * chunk + k] = pb[k];
+    }
+  __syncthreads();
+  const int which = threadIdx.x >> 6, col = col0 + (threadIdx.x & 63);
+  float* const to = which == 0 ? g.dgamma : which == 1 ? g.dbeta : nullptr;
+  if (to && col < g.w) {
+    float t = red[which][0][threadIdx.x & 63];
+    for (int j = 1; j < waves; ++j) t += red[which][j][threadIdx.x & 63];
+    to[col] = t;
+  }
+}
+
+// What becomes of dy xh and dy: nothing, a partial row of each work-group's, or the sums at once by
+// work-groups behind those of the rows, each for 64 columns (few rows, read twice from cache: one
+// launch less).
+enum Grads { NONE, PARTIAL, COLUMNS };
+
+// U rows of a row's threads at a time, so that the loads of all are on their way together.
+template <typename T, int TPR, int MAX_THREADS, int NC, int U, Grads G>
+__global__ __launch_bounds__(MAX_THREADS) void bwd_kernel(const BwdArgs g) {
+  __shared__ float lds[TPR ? 1 : 4 * U * MOST_WAVES];
+  constexpr bool GRADS = G == PARTIAL;
+  if constexpr (G == COLUMNS)
+    if ((int)blockIdx.x >= g.row_groups) {
+      column_sums<T>(g, 64 * (blockIdx.x - g.row_groups));
+      return;
+    }
+  const int threads = TPR ? TPR : g.threads;
+  const int slots = TPR ? BWD_GROUP / (TPR ? TPR : 1) : blockDim.x / g.threads;  // rows side by side
+  // (a wavefront is of one row: the slot is the same for all its lanes)
+  const int slot = TPR ? threadIdx.x / (TPR ? TPR : 1)
+                       : __builtin_amdgcn_readfirstlane(threadIdx.x / g.threads);
+  const int lane = threadIdx.x - slot * threads;
   const int r0 = blockIdx.x * g.rpb, r1 = min(g.rows, r0 + g.rpb);
   const float inv_w = 1.0f / (float)g.w;
-  // (rows of 1024 threads have 128 registers a thread: gamma is read again for each row)
-  constexpr bool KEEP = TPR <= 256;
   float gm[NC][8], pg[GRADS ? NC : 1][8], pb[GRADS ? NC : 1][8];
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    const int at = 8 * (lane + TPR * i);
-    if constexpr (KEEP) weights(g.gamma, at, g.w - at, 1.0f, gm[i]);
+    const int at = 8 * (lane + threads * i);
+    weights(g.gamma, at, g.w - at, 1.0f, gm[i]);
     if constexpr (GRADS)
 #pragma unroll
       for (int k = 0; k < 8; ++k) pg[i][k] = pb[i][k] = 0.0f;
   }
   int turn = 0;
   // (the same number of passes for all wavefronts of a row)
-  for (int first = r0; first < r1; first += SLOTS * U) {
+  for (int first = r0; first < r1; first += slots * U) {
     Chunk<T> dy[U][NC], z[U][NC], dt[U][NC];
     float mean[U], rstd[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int row = first + slot + SLOTS * u;
+      const int row = first + slot + slots * u;
       const bool live = row < r1;
       const T* pd = live ? row_at<T>(g.dy, g.batch, g.seq, row) : nullptr;
       const T* pz = live ? row_at<T>(g.z, g.batch, g.seq, row) : nullptr;
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
-        const int at = 8 * (lane + TPR * i), n = live ? g.w - at : 0;
+        const int at = 8 * (lane + threads * i), n = live ? g.w - at : 0;
         load_n(dy[u][i], pd + at, n);
         load_n(z[u][i], pz + at, n);
       }
@@ -261,7 +346,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void bwd_kernel(const BwdArg
         const T* pt = live ? row_at<T>(g.dtotal, g.batch, g.seq, row) : nullptr;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-          const int at = 8 * (lane + TPR * i);
+          const int at = 8 * (lane + threads * i);
           load_n(dt[u][i], pt + at, live ? g.w - at : 0);
         }
       }
@@ -275,9 +360,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void bwd_kernel(const BwdArg
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        const int at = 8 * (lane + TPR * i);
-        if constexpr (!KEEP) weights(g.gamma, at, g.w - at, 1.0f, gm[i]);
+      for (int i = 0; i < NC; ++i)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const float d = dy[u][i].get(k), xh = (z[u][i].get(k) - mean[u]) * rstd[u];
@@ -289,21 +372,19 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void bwd_kernel(const BwdArg
             pb[i][k] += d;
           }
         }
-      }
     if (g.dx.p) {
-      row_sums<TPR, 2 * U>(s, lds, turn);
+      row_sums<TPR, 2 * U>(s, lds, turn, threads / 64, slot);
       turn ^= 1;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int row = first + slot + SLOTS * u;
+        const int row = first + slot + slots * u;
         if (row >= r1) continue;
         T* px = row_at<T>(g.dx, g.batch, g.seq, row);
         const float a = s[2 * u] * inv_w, b = s[2 * u + 1] * inv_w;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-          const int at = 8 * (lane + TPR * i);
+          const int at = 8 * (lane + threads * i);
           float v[8];
-          if constexpr (!KEEP) weights(g.gamma, at, g.w - at, 1.0f, gm[i]);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             const float xh = (z[u][i].get(k) - mean[u]) * rstd[u];
@@ -317,10 +398,12 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void bwd_kernel(const BwdArg
     }
   }
   if constexpr (GRADS) {
-    // The work-group's rows side by side: lanes of a wavefront first, then wavefronts in order.
-    extern __shared__ float red[];  // TPR <= 64: [wavefront][2][w]
-    float* to = gridDim.x == 1 && g.dgamma ? nullptr : g.part + (int64_t)blockIdx.x * 2 * g.w;
-    if constexpr (TPR < 64) {
+    // The work-group's rows side by side: lanes of a wavefront first, then slots in order, one
+    // sum after the other through LDS.
+    extern __shared__ float red[];  // [TPR 0: slot, else wavefront][w]
+    constexpr bool WAVES = TPR > 0;
+    float* const part = gridDim.x == 1 && g.dgamma ? nullptr : g.part + (int64_t)blockIdx.x * 2 * g.w;
+    if constexpr (WAVES && TPR < 64) {
 #pragma unroll
       for (int i = 0; i < NC; ++i)
 #pragma unroll
@@ -331,69 +414,67 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void bwd_kernel(const BwdArg
             pb[i][k] += __shfl_xor(pb[i][k], o, 64);
           }
     }
-    if constexpr (TPR <= 64) {
-      const int wave = threadIdx.x >> 6;
-      if ((threadIdx.x & 63) < TPR) {
+    const int rows = WAVES ? BWD_GROUP / 64 : slots, mine = WAVES ? threadIdx.x >> 6 : slot;
 #pragma unroll
-        for (int i = 0; i < NC; ++i)
+    for (int which = 0; which < 2; ++which) {
+      float* const to = part ? part + which * g.w : which ? g.dbeta : g.dgamma;
+      if (!to) continue;  // (uniform)
+      if (rows > 1) {
+        if (!WAVES || (threadIdx.x & 63) < TPR) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int at = 8 * (lane + TPR * i) + k;
-            if (at < g.w) {
-              red[wave * 2 * g.w + at] = pg[i][k];
-              red[wave * 2 * g.w + g.w + at] = pb[i][k];
-            }
+          for (int i = 0; i < NC; ++i) {
+            const int at = 8 * (lane + threads * i);
+            Chunk<float> c;
+            c.set(which ? pb[i] : pg[i]);
+            store_n(c, red + mine * g.w + at, g.w - at);
           }
-      }
-      __syncthreads();
-      for (int e = threadIdx.x; e < 2 * g.w; e += THREADS) {
-        float t = red[e];
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < g.w; e += blockDim.x) {
+          float t = red[e];
+          for (int j = 1; j < rows; ++j) t += red[j * g.w + e];
+          to[e] = t;
+        }
+        __syncthreads();
+      } else {
 #pragma unroll
-        for (int j = 1; j < WAVES; ++j) t += red[j * 2 * g.w + e];
-        if (to) to[e] = t;
-        else if (e < g.w) g.dgamma[e] = t;
-        else if (g.dbeta) g.dbeta[e - g.w] = t;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        const int at = 8 * (lane + TPR * i), n = g.w - at;
-        Chunk<float> c;
-        float* dg = to ? to : g.dgamma;
-        float* db = to ? to + g.w : g.dbeta;
-        c.set(pg[i]);
-        store_n(c, dg + at, n);
-        c.set(pb[i]);
-        if (db) store_n(c, db + at, n);
+        for (int i = 0; i < NC; ++i) {
+          const int at = 8 * (lane + threads * i);
+          Chunk<float> c;
+          c.set(which ? pb[i] : pg[i]);
+          store_n(c, to + at, g.w - at);
+        }
       }
     }
   }
 }
 
-// dgamma and dbeta: the sums over the work-groups' partial rows, `parts` of them, in order within
-// each of a work-group's 16 stripes, then over the stripes.
-constexpr int RED_COLS = 64;
+// dgamma and dbeta: the sums over the work-groups' partial rows, `parts` of them: 64 stripes of
+// rows to 16 columns, each in order, then the stripes.
+constexpr int RED_COLS = 16;
 __global__ __launch_bounds__(1024) void reduce_kernel(const float* __restrict__ part, int parts, int w,
                                                       float* dgamma, float* dbeta) {
   __shared__ float lds[16][RED_COLS];
-  const int col = blockIdx.x * RED_COLS + (threadIdx.x & 63), stripe = threadIdx.x >> 6;
+  const int col = blockIdx.x * RED_COLS + (threadIdx.x & 15), stripe = threadIdx.x >> 4;
   float t = 0.0f;
   if (col < 2 * w) {
     const float* p = part + col;
     const int64_t step = (int64_t)2 * w;
-    int b = stripe;
-    for (; b + 16 * 7 < parts; b += 16 * 8) {
+    for (int b = stripe; b < parts; b += 64 * 8) {
       float v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = p[(b + 16 * j) * step];
+      for (int j = 0; j < 8; ++j) v[j] = b + 64 * j < parts ? p[(b + 64 * j) * step] : 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) t += v[j];
     }
-    for (; b < parts; b += 16) t += p[b * step];
   }
-  lds[stripe][threadIdx.x & 63] = t;
+  t += __shfl_xor(t, 16, 64);
+  t += __shfl_xor(t, 32, 64);
+  if ((threadIdx.x & 63) < RED_COLS) lds[threadIdx.x >> 6][threadIdx.x & 15] = t;
   __syncthreads();
-  if (stripe == 0 && col < 2 * w) {
+  if (threadIdx.x < RED_COLS && col < 2 * w) {
+    t = lds[0][threadIdx.x];
+#pragma unroll
     for (int j = 1; j < 16; ++j) t += lds[j][threadIdx.x];
     if (col < w) {
       if (dgamma) dgamma[col] = t;
@@ -413,37 +494,57 @@ __global__ void zero_kernel(float* a, float* b, int n) {
 // ---------------------------------------------------------------------------
 // Plan
 // ---------------------------------------------------------------------------
-// Threads of a row: a wavefront or less while its rows fit (no barriers), then 256 and 1024,
-// with at most four chunks of eight values a thread; backward, which holds dy, z, gamma and
-// both sums, two.
+constexpr int FWD_NARROW = 1536, BWD_NARROW = 1024;  // widest rows of one wavefront
+constexpr int BWD_MIDDLE = 8192;                      // of eight
+
+int round64(int n) { return (n + 63) / 64 * 64; }
+// Threads of a row: a wavefront or less while its row fits (no barriers), then as many
+// wavefronts as the row fills with two chunks a thread.
 int fwd_threads(int w) {
-  return w <= 64 ? 8 : w <= 128 ? 16 : w <= 256 ? 32 : w <= 2048 ? 64 : w <= 8192 ? 256 : 1024;
+  return w <= 64 ? 8 : w <= 128 ? 16 : w <= 256 ? 32 : w <= FWD_NARROW ? 64 : round64((w + 15) / 16);
 }
 int bwd_threads(int w) {
-  return w <= 64 ? 8 : w <= 128 ? 16 : w <= 256 ? 32 : w <= 1024 ? 64 : w <= 4096 ? 256 : 1024;
+  return w <= 64 ? 8 : w <= 128 ? 16 : w <= 256 ? 32 : w <= BWD_NARROW ? 64 : round64((w + 15) / 16);
 }
-// Rows of a work-group at a time (rows side by side times U of bwd_kernel).
-int bwd_rows(int w) {
+// Threads of a backward work-group: as many rows side by side as fit.
+int bwd_group(int w) {
   const int t = bwd_threads(w);
-  return t > 256 ? 1 : 2 * (256 / t);
+  return w <= BWD_MIDDLE ? BWD_GROUP / t * t : t;
 }
+// Work-groups, which leave a partial row each: one to a CU, or two where their registers let
+// two live there (one chunk a thread, or bf16 rows of more than one wavefront).  us with one and
+// two, bf16: 30000 x 512 30.6 / 24.9, 16384 x 1280 46.1 / 36.6, 5000 x 5120 59 / 46.6; one
+// is better for 16384 x 1024, 28.6 / 29.4, and fp32 8192 x 2048, 50.1 / 54.5.
+int bwd_most(int w, stage_dtype dt) {
+  return w <= 512 || (w > BWD_NARROW && w <= BWD_MIDDLE && dt == STAGE_BF16) ? 512 : 256;
+}
+// Up to so many rows the sums are made by work-groups of columns in the same launch: 231 x 768 in bf16
+// 10.5 -> 7.6 us, 231 x 5120 15 -> 7.6, 1024 x 1024 10.6 -> 9.4; 2000 x 1024 10.9 -> 15.5.
+constexpr int FEW_ROWS = 1024;
 struct BwdPlan {
   int blocks, rpb;
 };
-BwdPlan bwd_plan(int rows, int w) {
-  const int step = bwd_rows(w);
-  const int most = w <= 4096 ? 512 : 256;
-  int blocks = std::min(most, (rows + step - 1) / step);
+BwdPlan bwd_plan(int rows, int w, stage_dtype dt) {
+  const int step = bwd_group(w) / bwd_threads(w);  // rows at a time
+  const int blocks = std::min(bwd_most(w, dt), (rows + step - 1) / step);
   const int rpb = ((rows + blocks - 1) / blocks + step - 1) / step * step;
   return {(rows + rpb - 1) / rpb, rpb};
 }
 
 template <typename T, int TPR, int NC>
 void launch_fwd(const FwdArgs& g, hipStream_t st) {
-  constexpr int RPB = TPR > 256 ? 1 : 256 / TPR;
-  const dim3 grid((unsigned)((g.rows + RPB - 1) / RPB)), block(TPR > 256 ? TPR : 256);
-  if (g.res.p) hipLaunchKernelGGL((fwd_kernel<T, TPR, NC, true>), grid, block, 0, st, g);
-  else hipLaunchKernelGGL((fwd_kernel<T, TPR, NC, false>), grid, block, 0, st, g);
+  constexpr int RPB = TPR ? 256 / (TPR ? TPR : 1) : 1;
+  const dim3 grid((unsigned)((g.rows + RPB - 1) / RPB)), block(TPR ? 256 : fwd_threads(g.w));
+  // Early while all rows run at once: 2000 x 1024 in bf16 5.7 -> 5.1 us; 16384 x 1024 16.7 -> 17.1,
+  // in fp32 29.4 -> 32.5.
+  const bool early = (int64_t)g.rows * fwd_threads(g.w) <= 2560 * 64;
+  if (g.res.p) {
+    if (early) hipLaunchKernelGGL((fwd_kernel<T, TPR, NC, true, true>), grid, block, 0, st, g);
+    else hipLaunchKernelGGL((fwd_kernel<T, TPR, NC, true, false>), grid, block, 0, st, g);
+  } else {
+    if (early) hipLaunchKernelGGL((fwd_kernel<T, TPR, NC, false, true>), grid, block, 0, st, g);
+    else hipLaunchKernelGGL((fwd_kernel<T, TPR, NC, false, false>), grid, block, 0, st, g);
+  }
 }
 template <typename T>
 void forward(const FwdArgs& g, hipStream_t st) {
@@ -453,32 +554,34 @@ void forward(const FwdArgs& g, hipStream_t st) {
   else if (w <= 256) launch_fwd<T, 32, 1>(g, st);
   else if (w <= 512) launch_fwd<T, 64, 1>(g, st);
   else if (w <= 1024) launch_fwd<T, 64, 2>(g, st);
-  else if (w <= 2048) launch_fwd<T, 64, 4>(g, st);
-  else if (w <= 4096) launch_fwd<T, 256, 2>(g, st);
-  else if (w <= 8192) launch_fwd<T, 256, 4>(g, st);
-  else launch_fwd<T, 1024, 2>(g, st);
+  else if (w <= FWD_NARROW) launch_fwd<T, 64, 3>(g, st);
+  else launch_fwd<T, 0, 2>(g, st);
 }
 
-template <typename T, int TPR, int NC>
-void launch_bwd(const BwdArgs& g, int blocks, hipStream_t st) {
-  constexpr int U = TPR > 256 ? 1 : 2;
-  const dim3 grid((unsigned)blocks), block(TPR > 256 ? TPR : 256);
-  const size_t lds = TPR <= 64 ? (size_t)4 * 2 * g.w * 4 : 0;
-  if (g.dgamma || g.dbeta) hipLaunchKernelGGL((bwd_kernel<T, TPR, NC, U, true>), grid, block, lds, st, g);
-  else hipLaunchKernelGGL((bwd_kernel<T, TPR, NC, U, false>), grid, block, 0, st, g);
+template <typename T, int TPR, int MAX_THREADS, int NC>
+void launch_bwd(const BwdArgs& g, int blocks, Grads grads, hipStream_t st) {
+  const dim3 grid((unsigned)blocks), block(bwd_group(g.w));
+  const int rows = TPR ? BWD_GROUP / 64 : (int)block.x / g.threads;
+  const size_t lds = rows > 1 ? (size_t)rows * g.w * 4 : 0;
+  if (grads == PARTIAL) {
+    hipLaunchKernelGGL((bwd_kernel<T, TPR, MAX_THREADS, NC, 1, PARTIAL>), grid, block, lds, st, g);
+  } else if (grads == NONE) {
+    hipLaunchKernelGGL((bwd_kernel<T, TPR, MAX_THREADS, NC, 1, NONE>), grid, block, 0, st, g);
+  } else {
+    const dim3 both((unsigned)(blocks + (g.w + 63) / 64));
+    hipLaunchKernelGGL((bwd_kernel<T, TPR, MAX_THREADS, NC, 1, COLUMNS>), both, block, 0, st, g);
+  }
 }
 template <typename T>
-void backward(const BwdArgs& g, int blocks, hipStream_t st) {
+void backward(const BwdArgs& g, int blocks, Grads grads, hipStream_t st) {
   const int w = g.w;
-  if (w <= 64) launch_bwd<T, 8, 1>(g, blocks, st);
-  else if (w <= 128) launch_bwd<T, 16, 1>(g, blocks, st);
-  else if (w <= 256) launch_bwd<T, 32, 1>(g, blocks, st);
-  else if (w <= 512) launch_bwd<T, 64, 1>(g, blocks, st);
-  else if (w <= 1024) launch_bwd<T, 64, 2>(g, blocks, st);
-  else if (w <= 2048) launch_bwd<T, 256, 1>(g, blocks, st);
-  else if (w <= 4096) launch_bwd<T, 256, 2>(g, blocks, st);
-  else if (w <= 8192) launch_bwd<T, 1024, 1>(g, blocks, st);
-  else launch_bwd<T, 1024, 2>(g, blocks, st);
+  if (w <= 64) launch_bwd<T, 8, BWD_GROUP, 1>(g, blocks, grads, st);
+  else if (w <= 128) launch_bwd<T, 16, BWD_GROUP, 1>(g, blocks, grads, st);
+  else if (w <= 256) launch_bwd<T, 32, BWD_GROUP, 1>(g, blocks, grads, st);
+  else if (w <= 512) launch_bwd<T, 64, BWD_GROUP, 1>(g, blocks, grads, st);
+  else if (w <= BWD_NARROW) launch_bwd<T, 64, BWD_GROUP, 2>(g, blocks, grads, st);
+  else if (w <= BWD_MIDDLE) launch_bwd<T, 0, BWD_GROUP, 2>(g, blocks, grads, st);
+  else launch_bwd<T, 0, 1024, 2>(g, blocks, grads, st);
 }
 
 // ---------------------------------------------------------------------------
@@ -615,7 +718,7 @@ stage_status layer_norm_workspace(const layer_norm_shape* s, size_t* bytes) {
   if (!bytes) return bad(STAGE_EINVAL, "null bytes");
   CK(check_shape(s));
   const int64_t rows = (int64_t)s->batch * s->seq;
-  *bytes = rows ? (size_t)bwd_plan((int)rows, s->width).blocks * 2 * s->width * 4 : 0;
+  *bytes = rows ? (size_t)bwd_plan((int)rows, s->width, s->dtype).blocks * 2 * s->width * 4 : 0;
   return STAGE_OK;
 }
 
@@ -650,8 +753,8 @@ stage_status layer_norm_backward(const layer_norm_shape* s, const void* dy, cons
     CK(check_same("dx", g.dx, "dy", g.dy));
     CK(check_same("dx", g.dx, "total", g.z));
     CK(check_same("dx", g.dx, "dtotal", g.dtotal));
-    const BwdPlan plan = bwd_plan((int)rows, s->width);
-    const bool grads = dgamma || dbeta;
+    const BwdPlan plan = bwd_plan((int)rows, s->width, s->dtype);
+    Grads grads = dgamma || dbeta ? PARTIAL : NONE;
     if (grads) {
       const size_t need = (size_t)plan.blocks * 2 * s->width * 4;
       if (!workspace || workspace_bytes < need)
@@ -674,9 +777,23 @@ stage_status layer_norm_backward(const layer_norm_shape* s, const void* dy, cons
     g.seq = one ? g.rows : s->seq;
     g.w = s->width;
     g.rpb = plan.rpb;
-    if (s->dtype == STAGE_BF16) backward<bf16_t>(g, plan.blocks, st);
-    else backward<float>(g, plan.blocks, st);
-    if (grads && !(plan.blocks == 1 && dgamma))
+    g.threads = bwd_threads(s->width);
+    const auto run = [&](int blocks, Grads how) {
+      if (s->dtype == STAGE_BF16) backward<bf16_t>(g, blocks, how, st);
+      else backward<float>(g, blocks, how, st);
+    };
+    if (grads && rows <= FEW_ROWS) {
+      // Work-groups of columns read dy and z while those of rows write dx: over one of them, the
+      // columns go first.
+      grads = COLUMNS;
+      const bool over = dx && (dx == dy || dx == total);
+      g.row_groups = dx && !over ? plan.blocks : 0;
+      run(g.row_groups, COLUMNS);
+      if (over) run(plan.blocks, NONE);
+    } else {
+      run(plan.blocks, grads);
+    }
+    if (grads == PARTIAL && !(plan.blocks == 1 && dgamma))
       hipLaunchKernelGGL(reduce_kernel, dim3((2 * s->width + RED_COLS - 1) / RED_COLS), dim3(1024), 0, st,
                          (const float*)workspace, plan.blocks, s->width, dgamma, dbeta);
   }
