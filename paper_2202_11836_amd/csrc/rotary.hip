@@ -18,7 +18,7 @@
 namespace {
 
 constexpr int HEAD = 64;
-constexpr int THREADS = 256;
+constexpr int MOST_THREADS = 512;
 constexpr int MAX_P = 32;  // tokens of a work-group
 
 struct Operand {
@@ -37,6 +37,7 @@ struct Args {
   const int32_t* pos;
   int64_t sp[2];
   int pos_each;
+  int no_step;  // without pos all tokens are at 0
   float amp, sign;
   double turns[ROTARY_MAX_PAIRS];
 };
@@ -134,6 +135,9 @@ __device__ __forceinline__ Item item_of(const Args& g, uint32_t idx, int b, int 
     const int np = L == HALVES ? g.n / N : (g.n + N - 1) / N;
     if ((int)j < np) {
       it.pair = N * j;
+      // The last pairs, fewer than a vector holds: with some of those before them, unless these
+      // may be turned by now.
+      if (L == HALVES_ODD && it.pair + N > g.n && g.n >= N && !(g.skip >> it.which & 1)) it.pair = g.n - N;
       it.a = it.pair;
       it.b = g.n + it.pair;
     } else {
@@ -169,20 +173,23 @@ __device__ __forceinline__ void turn_item(const Args& g, const Item& it, Vec<T> 
       u.store(p + it.a);
       v.store(p + it.b);
     } else {
-      // Values a .. a + 2 N - 1, those of this head; u and v were read from HEAD - N on
-      // where the head ends before theirs do.
+      // u and v were read from HEAD - N on where the head ends before theirs do, and are stored so
+      // where that is behind the pairs.
+      const int ua = min(it.a, HEAD - N), vb = min(it.b, HEAD - N);
+      if (ua >= 2 * g.n) {
+        u.store(p + ua);
+        v.store(p + vb);
+      } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int ua = min(it.a, HEAD - N) + i, vb = min(it.b, HEAD - N) + i;
-        if (ua >= it.a) u.store1(p + min(it.a, HEAD - N), i);
-        if (it.b < HEAD && vb >= it.b) v.store1(p + min(it.b, HEAD - N), i);
+        for (int i = 0; i < N; ++i)
+          if (ua + i >= it.a) u.store1(p + ua, i);
       }
     }
     return;
   }
   const float2* c = cs + it.p * ROTARY_MAX_PAIRS + it.pair;
   if constexpr (L == INTERLEAVED) {
-    if (2 * it.pair >= 2 * g.n && (g.skip >> it.which & 1)) return;
+    if (it.pair >= g.n && (g.skip >> it.which & 1)) return;
 #pragma unroll
     for (int i = 0; i < N; i += 2) {  // pairs beyond the n go through
       const float a = u.get(i), b = u.get(i + 1), d = v.get(i), e = v.get(i + 1);
@@ -217,7 +224,7 @@ __device__ __forceinline__ void turn_item(const Args& g, const Item& it, Vec<T> 
 }
 
 template <typename T, Pairs L>
-__global__ __launch_bounds__(THREADS) void rotary_kernel(const Args g) {
+__global__ __launch_bounds__(MOST_THREADS) void rotary_kernel(const Args g) {
   __shared__ float2 cs[MAX_P * ROTARY_MAX_PAIRS];
   const int b = blockIdx.x / g.nblk;
   const int s0 = (blockIdx.x - b * g.nblk) * g.P;
@@ -231,13 +238,13 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(const Args g) {
     it = item_of<T, L>(g, idx, b, s0);
     load_item<T, L>(g, it, u, v);
   }
-  for (int i = threadIdx.x; i < np * ROTARY_MAX_PAIRS; i += THREADS) {
+  for (int i = threadIdx.x; i < np * ROTARY_MAX_PAIRS; i += blockDim.x) {
     const int p = i / ROTARY_MAX_PAIRS, pair = i % ROTARY_MAX_PAIRS;
     float2 r = {1.0f, 0.0f};
     if (pair < g.n) {
-      int64_t at = s0 + p;
+      int64_t at = g.no_step ? 0 : s0 + p;
       if (g.pos) {
-        const int32_t given = g.pos[b * g.sp[0] + (g.pos_each ? at * g.sp[1] : 0)];
+        const int32_t given = g.pos[b * g.sp[0] + (g.pos_each ? (s0 + p) * g.sp[1] : 0)];
         at = g.pos_each ? given : at + given;
       }
       r = cos_sin((double)at * g.turns[pair]);
@@ -248,7 +255,7 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(const Args g) {
   }
   __syncthreads();
   while (idx < total) {
-    const uint32_t next = idx + THREADS;
+    const uint32_t next = idx + blockDim.x;
     Item it2;
     Vec<T> u2, v2;
     if (next < total) {
@@ -334,13 +341,36 @@ stage_status check_operand(const char* name, const rotary_shape* s, int heads, c
 }
 
 template <typename T>
-void launch(const Args& g, Pairs pairs, unsigned grid, hipStream_t st) {
+void launch(const Args& g, Pairs pairs, dim3 grid, dim3 block, hipStream_t st) {
   if (pairs == INTERLEAVED)
-    hipLaunchKernelGGL((rotary_kernel<T, INTERLEAVED>), dim3(grid), dim3(THREADS), 0, st, g);
+    hipLaunchKernelGGL((rotary_kernel<T, INTERLEAVED>), grid, block, 0, st, g);
   else if (pairs == HALVES)
-    hipLaunchKernelGGL((rotary_kernel<T, HALVES>), dim3(grid), dim3(THREADS), 0, st, g);
+    hipLaunchKernelGGL((rotary_kernel<T, HALVES>), grid, block, 0, st, g);
   else
-    hipLaunchKernelGGL((rotary_kernel<T, HALVES_ODD>), dim3(grid), dim3(THREADS), 0, st, g);
+    hipLaunchKernelGGL((rotary_kernel<T, HALVES_ODD>), grid, block, 0, st, g);
+}
+
+// Tokens of a work-group and its threads: whole wavefronts, one item a thread, about 256 of them
+// (512 at most: more heads go in turns), as few idle as may be, but fewer tokens while there are too
+// few work-groups to fill the device.  us by items a thread, 32 x 512 tokens of 32 heads in bf16:
+// 1 30.4, 2 31.6, 4 32.7, 8 33.0; of 20 heads (65536 tokens), 160 of 256 threads at work 82, 240 72.7.
+struct Group {
+  int tokens, threads;
+};
+Group group_of(int batch, int S, int64_t per_token) {
+  Group best = {1, (int)std::min<int64_t>(MOST_THREADS, (per_token + 63) / 64 * 64)};
+  double most = 0.0;
+  for (int p = 1; p <= MAX_P && p <= S; ++p) {
+    const int64_t items = p * per_token, threads = (items + 63) / 64 * 64;
+    if (p > 1 && (threads > 320 || (int64_t)batch * ((S + p - 1) / p) < 1024)) break;
+    // (a few more idle threads rather than work-groups of one or two wavefronts)
+    const double used = (double)items / threads * std::min(1.0, 0.7 + threads / 640.0);
+    if (threads <= MOST_THREADS && used > most) {
+      most = used;
+      best = {p, (int)threads};
+    }
+  }
+  return best;
 }
 
 uint32_t inverse(uint32_t b) { return b == 1 ? 0 : (uint32_t)(((uint64_t)1 << 32) / b + 1); }
@@ -384,20 +414,28 @@ stage_status apply(const rotary_shape* s, const rotary_freqs* f, bool backward, 
   const int N = s->dtype == STAGE_BF16 ? 8 : 4;
   const Pairs pairs = f->interleaved ? INTERLEAVED : g.n % N == 0 ? HALVES : HALVES_ODD;
   g.items = pairs != HALVES_ODD ? HEAD / (2 * N) : (g.n + N - 1) / N + (HEAD - 2 * g.n + 2 * N - 1) / (2 * N);
-  // Tokens of a work-group: about four items a thread, but fewer tokens while there are too few
-  // work-groups to fill the device (each token's angles are formed once all the same).
-  const int64_t per_token = (int64_t)g.HG * g.items;
-  g.P = 1;
-  while (g.P < MAX_P && g.P < g.S && 2 * g.P * per_token <= 4 * THREADS &&
-         (int64_t)s->batch * ((g.S + 2 * g.P - 1) / (2 * g.P)) >= 1024)
-    g.P *= 2;
+  int batch = s->batch;
+  if (g.S == 1 && batch > 1) {
+    // Sequences of one token each are tokens of one sequence whose positions are given, or all 0.
+    g.S = batch;
+    batch = 1;
+    for (Operand& x : g.x) {
+      x.si[1] = x.si[0];
+      x.so[1] = x.so[0];
+    }
+    g.pos_each = 1;
+    g.sp[1] = g.sp[0];
+    g.no_step = !pos;
+  }
+  const Group group = group_of(batch, g.S, (int64_t)g.HG * g.items);
+  g.P = group.tokens;
   g.nblk = (g.S + g.P - 1) / g.P;
   g.inv_hg = inverse(g.HG);
   g.inv_items = inverse(g.items);
-  const int64_t grid = (int64_t)s->batch * g.nblk;
-  if (grid > 16777215) return bad(STAGE_EINVAL, "batch * length too large");
-  if (s->dtype == STAGE_BF16) launch<bf16_t>(g, pairs, (unsigned)grid, (hipStream_t)hip_stream);
-  else launch<float>(g, pairs, (unsigned)grid, (hipStream_t)hip_stream);
+  const int64_t grid = (int64_t)batch * g.nblk;
+  if (grid * group.threads >= (int64_t)1 << 32) return bad(STAGE_EINVAL, "batch * length too large");
+  if (s->dtype == STAGE_BF16) launch<bf16_t>(g, pairs, dim3((unsigned)grid), dim3(group.threads), (hipStream_t)hip_stream);
+  else launch<float>(g, pairs, dim3((unsigned)grid), dim3(group.threads), (hipStream_t)hip_stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess)
     return bad(STAGE_EHIP, "rotary_%s: %s", backward ? "backward" : "forward", hipGetErrorString(e));

@@ -114,7 +114,8 @@ def rotary_call(ptr=(), freqs=None, **kw):
     (dict(pos=(-1, 0)), "pos"), (dict(pos_each=1, pos=(1, -2)), "pos"), (dict(freqs=False), "frequencies"),
     (dict(freqs=Bn._RotaryFreqs(7, 0, 1.0)), "rot_dim"), (dict(freqs=Bn._RotaryFreqs(8, 2, 1.0)), "interleaved"),
     (dict(freqs=Bn._RotaryFreqs(8, 0, math.nan)), "amplitude"),
-    (dict(batch=1 << 24, seq=1, q=(256, 0, 64), k=(128, 0, 64), q_out=(256, 0, 64), k_out=(128, 0, 64)), "too large"),
+    (dict(batch=1 << 24, seq=2, heads=60, q=(7680, 3840, 64), k=(256, 128, 64), q_out=(7680, 3840, 64),
+          k_out=(256, 128, 64)), "too large"),
 ], ids=str)
 def test_rotary_call_refusals(kw, word):
     st, msg = rotary_call(**kw)
