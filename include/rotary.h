@@ -44,7 +44,7 @@ extern "C" {
 
 /* Frequencies of the pairs; plain host data, free to copy.  Filled by rotary_init
  * or rotary_init_freqs. */
-typedef struct {
+typedef struct rotary_freqs {
   int rot_dim;                    /* values of a head that are turned: 2 i pairs */
   int interleaved;                /* 0: pairs (i, n + i); 1: pairs (2 i, 2 i + 1) */
   float amplitude;                /* A */

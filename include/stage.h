@@ -207,8 +207,19 @@ stage_status stage_set_relpos(stage_t* s, int num_buckets, int max_distance);
 stage_status stage_relpos(stage_t* s, float** table, float** grad, int64_t* numel);
 
 /*
+ * Rotary positions (rotary.h) of the stage's self attention: the queries and keys of every
+ * attention half are turned by their positions 0 .. seq - 1 behind the projection (on bf16
+ * stages from and to bf16: a second rounding), their gradients back.  f = NULL takes them
+ * out again.  Beside a relative position bias or without one.  Drops the saved context;
+ * STAGE_SAVED_QKV holds Q and K as turned.  EINVAL for frequencies that rotary_init does not
+ * make or a stage without an attention half.
+ */
+struct rotary_freqs;
+stage_status stage_set_rotary(stage_t* s, const struct rotary_freqs* f);
+
+/*
  * Cross attention (the decoder layers of an encoder-decoder model), on a stage that
- * holds one attention half and no bias: queries from x [batch, seq, h], keys and
+ * holds one attention half, no bias and no rotary positions: queries from x [batch, seq, h], keys and
  * values from memory [batch, mem_seq, h] (an encoder's output), with the half's
  * parameters, W_qkv's row blocks applied to x, memory and memory:
  *     y = LN(x + W_o attention(x W_q^T + b_q, memory W_k^T + b_k, memory W_v^T + b_v) + b_o)

@@ -36,8 +36,8 @@ EXPORTED = ("alloc_coarse", "alloc_fine", "alloc_workloads", "stage_init", "stag
             "stage_trace_site", "stage_trace_mask", "stage_trace_read", "stage_site_count",
             "stage_site_name", "stage_device_bytes", "stage_memory_model",
             "stage_memory_model_units", "stage_mfma_peak", "stage_record_grads",
-            "stage_backward_noalloc", "stage_set_relpos", "stage_relpos", "stage_forward_cross",
-            "stage_backward_cross",
+            "stage_backward_noalloc", "stage_set_relpos", "stage_relpos", "stage_set_rotary",
+            "stage_forward_cross", "stage_backward_cross",
             "stage_last_error", "stage_destroy")
 
 EXPORTED_ATTN = ("attn_relpos_init", "attn_relpos_bucket", "attn_workspace", "attn_forward",
@@ -154,6 +154,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.stage_set_relpos.restype = i32
     lib.stage_relpos.argtypes = [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(i64)]
     lib.stage_relpos.restype = i32
+    lib.stage_set_rotary.argtypes = [vp, ctypes.POINTER(_RotaryFreqs)]
+    lib.stage_set_rotary.restype = i32
     lib.stage_forward_cross.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp]
     lib.stage_forward_cross.restype = i32
     lib.stage_backward_cross.argtypes = [vp, vp, vp, vp]
@@ -268,6 +270,11 @@ def stage_relpos(handle):
     return t.value, g.value, n.value
 
 
+def stage_set_rotary(handle, freqs) -> None:
+    """freqs: a Rotary's c, or None."""
+    _check(handle, load_library().stage_set_rotary(handle, None if freqs is None else ctypes.byref(freqs)))
+
+
 def stage_forward_cross(handle, x, memory, key_mask, batch: int, seq: int, mem_seq: int, y) -> None:
     _check(handle, load_library().stage_forward_cross(handle, _ptr(x), _ptr(memory), _ptr(key_mask),
                                                       batch, seq, mem_seq, _ptr(y)))
@@ -377,11 +384,12 @@ def stage_destroy(handle) -> None:
 # ---------------------------------------------------------------------------
 
 class _DeviceFloats:
-    """fp32 memory of a stage for torch.as_tensor; the tensor keeps the stage alive."""
+    """Memory of a stage (fp32, or any type of numpy's) for torch.as_tensor; the tensor keeps the
+    stage alive."""
 
-    def __init__(self, stage, ptr, shape):
+    def __init__(self, stage, ptr, shape, typestr="<f4"):
         self.stage = stage
-        self.__cuda_array_interface__ = {"data": (ptr, False), "shape": shape, "typestr": "<f4",
+        self.__cuda_array_interface__ = {"data": (ptr, False), "shape": shape, "typestr": typestr,
                                          "strides": None, "version": 2}
 
 
@@ -396,6 +404,7 @@ class Stage:
         import torch
         self.hidden, self.heads, self.ffn = hidden, heads, ffn
         self._cross = None  # shapes of x and memory of the latest forward, if of cross attention
+        self._tables = 0  # relative position tables that there have been
         self.dtype_name = dtype
         self.code = STAGE_BF16 if dtype == "bf16" else STAGE_F32
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
@@ -445,6 +454,7 @@ class Stage:
         """Give the self attention of the stage's layers one relative position bias
         (both directions; a table of zeros), or take it out (num_buckets 0)."""
         self._sync_stream()
+        self._tables += 1  # (the earlier one is gone, whatever comes of this)
         stage_set_relpos(self.handle, num_buckets, max_distance)
 
     def _relpos_view(self, which: int):
@@ -461,6 +471,48 @@ class Stage:
     def relpos_grad(self):
         """Its gradient of the latest backward, in the stage's own memory."""
         return self._relpos_view(1)
+
+    def set_rotary(self, rotary):
+        """Turn the queries and keys of the stage's self attention by their positions (a Rotary),
+        or no longer (None)."""
+        stage_set_rotary(self.handle, None if rotary is None else rotary.c)
+
+    def _view(self, ptr, which: int, bf16: bool):
+        """The stage's own memory of a parameter or gradient as a tensor."""
+        import torch
+        t = torch.as_tensor(_DeviceFloats(self, ptr, self._param_shape(which), "<i2" if bf16 else "<f4"),
+                            device="cuda")
+        return t.view(torch.bfloat16) if bf16 else t
+
+    def adamw(self, weight_decay=0.01, state_bits=32, **kw):
+        """An AdamW over the stage's parameters (with the bias table, where there is one) and their
+        gradients of the latest backward, where they lie; its step() goes behind backward().
+        weight_decay and 8-bit states are the matrices'; other arguments as AdamW's.  It is of use
+        until the next set_relpos and until close()."""
+        params, grads, decay, bits, names = [], [], [], [], []
+        for layer in range(self.L):
+            for which, name in enumerate(PARAM_NAMES):
+                try:
+                    p, _, d = stage_param(self.handle, layer, which)
+                except StageError:  # of the half that the stage does not hold
+                    continue
+                matrix = len(self._param_shape(which)) == 2
+                params.append(self._view(p, which, d == STAGE_BF16))
+                grads.append(self._view(stage_grad(self.handle, layer, which)[0], which, False))
+                decay.append(weight_decay if matrix else 0.0)
+                bits.append(state_bits if matrix else 32)
+                names.append((layer, name))
+        try:
+            table, grad = self.relpos_table(), self.relpos_grad()
+        except StageError:
+            pass
+        else:
+            params.append(table)
+            grads.append(grad)
+            decay.append(0.0)
+            bits.append(32)
+            names.append((None, "relpos_table"))
+        return _StageAdamW(self, names, params, grads, weight_decay=decay, state_bits=bits, **kw)
 
     def forward_cross(self, x, memory, key_mask=None, out=None):
         """Cross attention of x [batch, seq, hidden] over memory [batch, mem_seq,
@@ -933,6 +985,21 @@ class AdamW:
             self.close()
         except Exception:
             pass
+
+
+class _StageAdamW(AdamW):
+    """Of a stage's parameters: names[i] is the (layer, name) of params[i]."""
+
+    def __init__(self, stage, names, params, grads, **kw):
+        self.stage, self.names, self._tables = stage, names, stage._tables
+        super().__init__(params, grads, **kw)
+
+    def step(self, lr, max_norm=None):
+        if not self.stage.handle:
+            raise StageError(STAGE_ESTATE, "the stage is closed")
+        if self.stage._tables != self._tables:
+            raise StageError(STAGE_ESTATE, "the stage's bias table is another one since")
+        return super().step(lr, max_norm)
 
 
 # ---------------------------------------------------------------------------

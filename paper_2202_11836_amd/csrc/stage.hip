@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "../../include/attn.h"
+#include "../../include/rotary.h"
 #include "../../include/stage.h"
 #include "kernels.h"
 
@@ -197,6 +198,9 @@ struct stage {
   attn_relpos rp = {};
   float* rp_table = nullptr;
   float* rp_grad = nullptr;
+  // Rotary positions of the attention halves (stage_set_rotary).
+  bool rotary = false;
+  rotary_freqs rot = {};
   // Workspace of the attention operators (with a bias also the layers' table
   // gradients) and, of a cross-attention pass, what belongs to the memory: its copy
   // [Tm, h], K | V and their gradient [Tm, 2h], its mask and column partial sums.
@@ -728,11 +732,46 @@ stage_status attn_op_backward(stage_t* s, const void* q, const void* k, const vo
   return st ? fail(s, st, attn_last_error()) : STAGE_OK;
 }
 
+// Q and K of a packed QKV [T, 3h] turned by their positions, or their gradients back, in place.
+template <typename T>
+stage_status turn_qk(stage_t* s, T* qkv, bool back) {
+  rotary_shape a{};
+  a.dtype = s->dtype;
+  a.batch = s->B;
+  a.seq = s->S;
+  a.heads = a.kv_heads = s->H;
+  for (int64_t* st : {a.q, a.k, a.q_out, a.k_out}) {
+    st[0] = (int64_t)s->S * 3 * s->h;
+    st[1] = 3 * s->h;
+    st[2] = HEAD_DIM;
+  }
+  T* k = qkv + s->h;
+  const stage_status st = back ? rotary_backward(&a, &s->rot, qkv, k, nullptr, qkv, k, s->stream)
+                               : rotary_forward(&a, &s->rot, qkv, k, nullptr, qkv, k, s->stream);
+  return st ? fail(s, st, rotary_last_error()) : STAGE_OK;
+}
+// The end of a layer's attention backward that is not the fused kernels' own: dQ and dK turned
+// back, dQKV's column sums (*cj).
+template <typename T>
+stage_status dqkv_end(stage_t* s, float* db, ColJob* cj) {
+  T* d = (T*)s->dQKV;
+  if (s->rotary) {
+    const int tr = trace_begin(s, site_set(SITE_ATTN_BWD, SITE_ATTN_DQ, SITE_ATTN_DKDV));
+    const stage_status st = turn_qk(s, d, true);
+    trace_end(s, tr);
+    if (st) return st;
+  }
+  const int nblk = std::min(COL_PARTS, s->B * ((s->S + 31) / 32));
+  SITE(BQKV_SUM, col_partial<T>(d, s->B * s->S, 3 * s->h, s->colpart_qkv, nblk, s->stream));
+  *cj = ColJob{s->colpart_qkv, nblk, 1, 3 * s->h, {db, nullptr, nullptr, nullptr}};
+  return STAGE_OK;
+}
+
 // Self attention's backward with the bias: dQKV, its column sums (*cj) and the
 // layer's table gradient.
 template <typename T>
 stage_status attn_relpos_backward(stage_t* s, int l, float* db, ColJob* cj) {
-  const int h = s->h, Tn = s->B * s->S;
+  const int h = s->h;
   const Saved& v = s->saved[l];
   const T* qkv = (const T*)v.QKV;
   T* d = (T*)s->dQKV;
@@ -741,11 +780,7 @@ stage_status attn_relpos_backward(stage_t* s, int l, float* db, ColJob* cj) {
   if (!st)
     st = attn_op_backward(s, qkv, qkv + h, qkv + 2 * h, s->mask, v, d, d + h, d + 2 * h,
                           s->attn_ws + at + (size_t)l * s->rp.num_buckets * s->H, at * 4);
-  if (st) return st;
-  const int nblk = std::min(COL_PARTS, s->B * ((s->S + 31) / 32));
-  SITE(BQKV_SUM, col_partial<T>(d, Tn, 3 * h, s->colpart_qkv, nblk, s->stream));
-  *cj = ColJob{s->colpart_qkv, nblk, 1, 3 * h, {db, nullptr, nullptr, nullptr}};
-  return STAGE_OK;
+  return st ? st : dqkv_end<T>(s, db, cj);
 }
 // The table's gradient from those of the layers (those with an attention half are all
 // but the first layer of a stage that starts at a feed-forward half).
@@ -836,6 +871,12 @@ stage_status forward_impl(stage_t* s, const T* x, const uint8_t* key_mask, T* y)
         GemmArgs g = gemm_args(X, h, p[STAGE_W_QKV], h, QKV, 3 * h, Tn, 3 * h, h);
         g.bias = (const float*)p[STAGE_B_QKV];
         SITE_SET(SITE_QKV_FWD, l == 0 ? prep_site : 0, gemm_in(g, EPI_STORE, l == 0));
+      }
+      if (s->rotary) {
+        const int tr = trace_begin(s, site_set(SITE_ATTN_FWD));
+        const stage_status r = turn_qk(s, QKV, false);
+        trace_end(s, tr);
+        if (r) return r;
       }
       if (s->relpos) {
         const stage_status r = attn_op_forward(s, QKV, QKV + h, QKV + 2 * h, s->mask, v);
@@ -1051,8 +1092,12 @@ stage_status backward_f32(stage_t* s, const float* dy, float* dx) {
         SITE_SET(SITE_DV_BWD, site_set(SITE_DK_BWD, SITE_BQKV_SUM, rows ? SITE_DV_BWD : SITE_DQ_BWD),
                  gemm_f32_attn_bwd(prob(v.P, dC, h, (int64_t)S * h, 2),
                                    prob(s->dS, QKV, 3 * h, sq, 1), rows ? nullptr : &dq, BH, st));
-        tail.col[tail.ncol++] = ColJob{s->colpart_qkv, B * nqb, 1, 3 * h,
-                             {gr[STAGE_B_QKV], nullptr, nullptr, nullptr}};
+        if (s->rotary) {
+          if ((r = dqkv_end<T>(s, gr[STAGE_B_QKV], &tail.col[tail.ncol++]))) return r;
+        } else {
+          tail.col[tail.ncol++] = ColJob{s->colpart_qkv, B * nqb, 1, 3 * h,
+                               {gr[STAGE_B_QKV], nullptr, nullptr, nullptr}};
+        }
       }
       // dW_qkv = dQKV^T X
       wjobs[nw++] = {dQKV, 3 * h, v.X, h, 3 * h, h, gr[STAGE_W_QKV]};
@@ -1195,8 +1240,12 @@ stage_status backward_bf16(stage_t* s, const bf16_t* dy, bf16_t* dx) {
           SITE(ATTN_DQ, attn_backward_dq(aa, st));
           SITE(ATTN_DKDV, attn_backward_dkdv(aa, st));
         }
-        tail.col[tail.ncol++] = ColJob{s->colpart_qkv, B * ((S + 31) / 32), 1, 3 * h,
-                             {gr[STAGE_B_QKV], nullptr, nullptr, nullptr}};
+        if (s->rotary) {
+          if ((r = dqkv_end<T>(s, gr[STAGE_B_QKV], &tail.col[tail.ncol++]))) return r;
+        } else {
+          tail.col[tail.ncol++] = ColJob{s->colpart_qkv, B * ((S + 31) / 32), 1, 3 * h,
+                               {gr[STAGE_B_QKV], nullptr, nullptr, nullptr}};
+        }
       }
       // dW_qkv = dQKV^T X
       wjobs[nw++] = {dQKV, 3 * h, v.X, h, 3 * h, h, gr[STAGE_W_QKV]};
@@ -1701,6 +1750,23 @@ stage_status stage_relpos(stage_t* s, float** table, float** grad, int64_t* nume
   return STAGE_OK;
 }
 
+stage_status stage_set_rotary(stage_t* s, const rotary_freqs* f) {
+  if (!s) return STAGE_EINVAL;
+  s->err.clear();
+  if (f) {
+    rotary_shape none{};  // (an empty call: its checks alone)
+    none.heads = 1;
+    const stage_status st = rotary_forward(&none, f, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
+    if (st) return fail(s, st, rotary_last_error());
+    if (s->L == 1 && s->ffn_first)
+      return fail(s, STAGE_EINVAL, "the stage holds no attention half");
+    s->rot = *f;
+  }
+  s->rotary = f != nullptr;
+  s->have_ctx = false;
+  return STAGE_OK;
+}
+
 stage_status stage_forward_cross(stage_t* s, const void* x, const void* memory, const uint8_t* key_mask,
                                  int batch, int seq, int mem_seq, void* y) try {
   if (!s) return STAGE_EINVAL;
@@ -1708,6 +1774,7 @@ stage_status stage_forward_cross(stage_t* s, const void* x, const void* memory, 
   if (s->L != 1 || s->ffn_first || !s->attn_last)
     return fail(s, STAGE_EINVAL, "cross attention needs a stage of one attention half");
   if (s->relpos) return fail(s, STAGE_EINVAL, "cross attention takes no relative position bias");
+  if (s->rotary) return fail(s, STAGE_EINVAL, "cross attention takes no rotary positions");
   if (batch < 0 || seq < 0 || mem_seq < 0) return fail(s, STAGE_EINVAL, "negative batch or length");
   const int64_t T = (int64_t)batch * seq, Tm = (int64_t)batch * mem_seq;
   if (T > 0 && (!x || !y)) return fail(s, STAGE_EINVAL, "null x or y");
