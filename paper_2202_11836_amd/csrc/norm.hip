@@ -449,33 +449,32 @@ __global__ __launch_bounds__(MAX_THREADS) void bwd_kernel(const BwdArgs g) {
   }
 }
 
-// dgamma and dbeta: the sums over the work-groups' partial rows, `parts` of them: 64 stripes of
-// rows to 16 columns, each in order, then the stripes.
-constexpr int RED_COLS = 16;
+// dgamma and dbeta: the sums over the work-groups' partial rows, `parts` of them: 32 stripes of
+// rows to 32 columns (a cache line), each in order, then the stripes.
+constexpr int RED_COLS = 32, RED_STRIPES = 1024 / RED_COLS;
 __global__ __launch_bounds__(1024) void reduce_kernel(const float* __restrict__ part, int parts, int w,
                                                       float* dgamma, float* dbeta) {
   __shared__ float lds[16][RED_COLS];
-  const int col = blockIdx.x * RED_COLS + (threadIdx.x & 15), stripe = threadIdx.x >> 4;
+  const int at = threadIdx.x % RED_COLS, col = blockIdx.x * RED_COLS + at;
   float t = 0.0f;
   if (col < 2 * w) {
     const float* p = part + col;
     const int64_t step = (int64_t)2 * w;
-    for (int b = stripe; b < parts; b += 64 * 8) {
+    for (int b = threadIdx.x / RED_COLS; b < parts; b += RED_STRIPES * 8) {
       float v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = b + 64 * j < parts ? p[(b + 64 * j) * step] : 0.0f;
+      for (int j = 0; j < 8; ++j) v[j] = b + RED_STRIPES * j < parts ? p[(b + RED_STRIPES * j) * step] : 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) t += v[j];
     }
   }
-  t += __shfl_xor(t, 16, 64);
   t += __shfl_xor(t, 32, 64);
-  if ((threadIdx.x & 63) < RED_COLS) lds[threadIdx.x >> 6][threadIdx.x & 15] = t;
+  if ((threadIdx.x & 63) < RED_COLS) lds[threadIdx.x >> 6][at] = t;
   __syncthreads();
   if (threadIdx.x < RED_COLS && col < 2 * w) {
-    t = lds[0][threadIdx.x];
+    t = lds[0][at];
 #pragma unroll
-    for (int j = 1; j < 16; ++j) t += lds[j][threadIdx.x];
+    for (int j = 1; j < 16; ++j) t += lds[j][at];
     if (col < w) {
       if (dgamma) dgamma[col] = t;
     } else if (dbeta) {

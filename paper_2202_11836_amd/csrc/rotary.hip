@@ -98,7 +98,8 @@ enum Pairs {
 };
 
 // An item: two vectors of a head.  HALVES: Vec::N pairs, or 2 Vec::N values behind them;
-// HALVES_ODD: the same with a last one of fewer; INTERLEAVED: 2 Vec::N values in a row.
+// HALVES_ODD: the same with a last one of fewer; INTERLEAVED: Vec::N values of each half of the
+// head.  So the items of a head access 64 bytes or more in a row.
 struct Item {
   int p, which;     // token, 0: q, 1: k
   int64_t in, out;  // offsets of the head
@@ -128,9 +129,9 @@ __device__ __forceinline__ Item item_of(const Args& g, uint32_t idx, int b, int 
   it.in = b * x.si[0] + s * x.si[1] + h * x.si[2];
   it.out = b * x.so[0] + s * x.so[1] + h * x.so[2];
   if constexpr (L == INTERLEAVED) {
-    it.a = 2 * N * j;
-    it.b = it.a + N;
-    it.pair = N * j;
+    it.a = N * j;
+    it.b = HEAD / 2 + it.a;
+    it.pair = it.a / 2;
   } else {
     const int np = L == HALVES ? g.n / N : (g.n + N - 1) / N;
     if ((int)j < np) {
@@ -189,17 +190,18 @@ __device__ __forceinline__ void turn_item(const Args& g, const Item& it, Vec<T> 
   }
   const float2* c = cs + it.p * ROTARY_MAX_PAIRS + it.pair;
   if constexpr (L == INTERLEAVED) {
-    if (it.pair >= g.n && (g.skip >> it.which & 1)) return;
+    constexpr int FAR = HEAD / 4;  // pairs from the first vector's to the second's
 #pragma unroll
     for (int i = 0; i < N; i += 2) {  // pairs beyond the n go through
       const float a = u.get(i), b = u.get(i + 1), d = v.get(i), e = v.get(i + 1);
-      const float2 r = c[i / 2], w = c[N / 2 + i / 2];
-      const bool go = it.pair + i / 2 < g.n, go2 = it.pair + N / 2 + i / 2 < g.n;
+      const float2 r = c[i / 2], w = c[FAR + i / 2];
+      const bool go = it.pair + i / 2 < g.n, go2 = it.pair + FAR + i / 2 < g.n;
       u.set2(i, go ? fmaf(a, r.x, -(b * r.y)) : a, go ? fmaf(a, r.y, b * r.x) : b);
       v.set2(i, go2 ? fmaf(d, w.x, -(e * w.y)) : d, go2 ? fmaf(d, w.y, e * w.x) : e);
     }
-    u.store(p + it.a);
-    v.store(p + it.b);
+    const bool skip = g.skip >> it.which & 1;
+    if (!skip || it.pair < g.n) u.store(p + it.a);
+    if (!skip || it.pair + FAR < g.n) v.store(p + it.b);
   } else {
     Vec<T> y, z;
 #pragma unroll
@@ -342,12 +344,9 @@ stage_status check_operand(const char* name, const rotary_shape* s, int heads, c
 
 template <typename T>
 void launch(const Args& g, Pairs pairs, dim3 grid, dim3 block, hipStream_t st) {
-  if (pairs == INTERLEAVED)
-    hipLaunchKernelGGL((rotary_kernel<T, INTERLEAVED>), grid, block, 0, st, g);
-  else if (pairs == HALVES)
-    hipLaunchKernelGGL((rotary_kernel<T, HALVES>), grid, block, 0, st, g);
-  else
-    hipLaunchKernelGGL((rotary_kernel<T, HALVES_ODD>), grid, block, 0, st, g);
+  if (pairs == INTERLEAVED) hipLaunchKernelGGL((rotary_kernel<T, INTERLEAVED>), grid, block, 0, st, g);
+  else if (pairs == HALVES) hipLaunchKernelGGL((rotary_kernel<T, HALVES>), grid, block, 0, st, g);
+  else hipLaunchKernelGGL((rotary_kernel<T, HALVES_ODD>), grid, block, 0, st, g);
 }
 
 // Tokens of a work-group and its threads: whole wavefronts, one item a thread, about 256 of them
