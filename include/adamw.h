@@ -76,7 +76,7 @@ typedef struct {
 
 /*
  * A handle for n tensors of the current device.  Allocates device memory for their addresses
- * and copies them there; returns when that is done.  steps: int64 on the device, the number of
+ * and copies them there; returns when that is done (so not during a capture).  steps: int64 on the device, the number of
  * steps done so far.  EINVAL for n < 0, a negative numel (0 is valid), null or misaligned
  * pointers, unknown types, scales or a master copy that do not fit the types, values that are
  * not finite, or 2^40 elements or more in all.

@@ -482,6 +482,8 @@ class Stage:
         import torch
         t = torch.as_tensor(_DeviceFloats(self, ptr, self._param_shape(which), "<i2" if bf16 else "<f4"),
                             device="cuda")
+        if t.data_ptr() != ptr:
+            raise StageError(STAGE_ESTATE, "the stage is not of the current device")
         return t.view(torch.bfloat16) if bf16 else t
 
     def adamw(self, weight_decay=0.01, state_bits=32, **kw):
@@ -489,6 +491,8 @@ class Stage:
         gradients of the latest backward, where they lie; its step() goes behind backward().
         weight_decay and 8-bit states are the matrices'; other arguments as AdamW's.  It is of use
         until the next set_relpos and until close()."""
+        if not self.handle:
+            raise StageError(STAGE_ESTATE, "the stage is closed")
         params, grads, decay, bits, names = [], [], [], [], []
         for layer in range(self.L):
             for which, name in enumerate(PARAM_NAMES):
@@ -858,6 +862,8 @@ class AdamW:
     state           the states to go on with (another AdamW's .state, say), held in place; None:
                     new ones
 
+    Steps of one AdamW go one after the other; a captured step counts on with each replay.
+
     state: a dict of lists, an entry for each tensor: "exp_avg", "exp_avg_sq" (fp32, or
     float8_e4m3fn and float8_e5m2), "exp_avg_scale", "exp_avg_sq_scale" (8 bits: fp32, one for
     256 elements, else None), "master" (fp32 or None); and "steps", int64 [1] on the GPU."""
@@ -890,6 +896,9 @@ class AdamW:
             self._fits(f"grads[{i}]", g, p.shape, types)
         self.state = self._new_state(bool(master)) if state is None else self._given_state(state)
         self.norm = torch.zeros(1, device=self.device)
+        # (the handle has their addresses, whatever becomes of the lists)
+        self._held = self.params + self.grads + [t for n in self.LISTS for t in self.state[n]] + \
+            [self.state["steps"]]
         self._make(decay, scale)
 
     def _fits(self, name, t, shape, types):

@@ -294,6 +294,18 @@ def test_state_goes_on():
         assert all(torch.equal(a, b) for a, b in zip(x.all(), y.all()))
 
 
+def test_states_taken_out_of_the_lists():
+    """The memory of states stays the optimizer's when another tensor takes their place in a list."""
+    x, y = Tensors([50000]), Tensors([50000])
+    x.opt.state["exp_avg"][0] = x.params[0] = torch.zeros(1, device="cuda")
+    held = x.opt._held
+    junk = [torch.full((50000,), float("nan"), device="cuda") for _ in range(20)]
+    for _ in range(2):
+        x.opt.step(LR)
+        y.opt.step(LR)
+    assert torch.equal(held[0], y.params[0]) and all(j.isnan().all() for j in junk)
+
+
 def test_reset_master():
     x = Tensors([300], "bf16")
     x.params[0].copy_(rand((300,), 50))

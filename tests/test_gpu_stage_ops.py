@@ -299,3 +299,6 @@ def test_adamw_of_a_stage_that_is_gone():
     with pytest.raises(StageError) as e:
         opt.step(LR)
     assert e.value.status == 2 and "closed" in str(e.value)
+    with pytest.raises(StageError) as e:
+        st.adamw()
+    assert e.value.status == 2 and "closed" in str(e.value)
