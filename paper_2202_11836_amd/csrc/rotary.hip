@@ -4,7 +4,10 @@
 // y0 = A (x0 cos a - x1 sin a), y1 = A (x0 sin a + x1 cos a): three operations a value
 // read and written once, so HBM bounds it.  A work-group takes the tokens s0 .. s0 + P - 1
 // of one sequence, all heads of q and of k: it forms the cosines and sines of its P * n
-// angles once, in LDS, and turns every head by them, 16-byte accesses.
+// angles once, in LDS, and turns every head by them, 16-byte accesses.  bf16, 32 x 512 tokens of
+// 16 + 16 heads, part of a packed projection: 29.2 us (4.6 TB/s); 2 x 32768 of 16 + 4: 69-71 us
+// (4.7-4.8).  Stores that bypass the caches are 3-10% faster alone, and slower with the attention
+// that reads them next (86 -> 88 us).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
