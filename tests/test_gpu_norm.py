@@ -94,6 +94,32 @@ def test_rows_apart(width, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [3, 1100])
+@pytest.mark.parametrize("base", [0, 8, 56, 248, 504, 1016, 1536])
+def test_row_ends(base, rows, dtype):
+    """Each number of values behind a row's last whole eight, between NaN that no result shows."""
+    for width in range(base + 1, base + 8):
+        big = {n: torch.full((rows, width + 9), float("nan"), device="cuda").to(DT[dtype]) for n in
+               ("x", "res", "dy", "dt", "out", "dx")}
+        v = {n: t[:, 5:5 + width] for n, t in big.items()}
+        for i, n in enumerate(("x", "res", "dy", "dt")):
+            v[n].copy_(rand((rows, width), width + i))
+        ga, be = 1 + rand((width,), 8, std=0.2), rand((width,), 9)
+        # (eps of one: narrow rows' values may lie close together, and then so do their gradients' terms)
+        out, total, mean, rstd = P.layer_norm_forward(v["x"], ga, be, v["res"], eps=1.0, out=v["out"])
+        want, z, mu, rs, tol = norm_forward(v["x"], ga, be, v["res"], 1.0)
+        assert torch.equal(total.double(), z)
+        within("out", out, want, tol[0])
+        dx, dg, db = P.layer_norm_backward(v["dy"], total, ga, mean, rstd, dtotal=v["dt"], dx=v["dx"])
+        wx, wg, wb, tol = norm_backward(v["dy"], total, ga, mean, rstd, v["dt"])
+        within("dx", dx, wx, tol[0])
+        within("dgamma", dg, wg, tol[1])
+        within("dbeta", db, wb, tol[2])
+        for n, t in big.items():
+            assert t[:, :5].isnan().all() and t[:, 5 + width:].isnan().all(), n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_transposed_and_broadcast(dtype):
     """Sequences side by side in memory, a residual shared by the batch, gradients of one row."""
     B, S, w = 4, 6, 200
