@@ -22,8 +22,12 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int CHUNK = THREADS * 8;  // elements: eight a thread, a block of 8-bit states 32 threads
-constexpr int MOST_GROUPS = 512;    // work-groups, 2 to a CU
+constexpr int GROUPS = 512, GROUPS_LIGHT = 1024;  // most work-groups, 2 or 4 to a CU
+constexpr int LIGHT = 14;           // bytes to and from memory for an element, of which it is 4
 constexpr int MOST_PARTS = 1024;    // work-groups of the norm
+// The tickets: one counter, and behind it in memory those that many work-groups take first, a
+// COUNTERS'th of them each, in cache lines of their own.
+constexpr int COUNTERS = 32, TICKET_STEP = 32;
 
 enum Kind : int { P_F32, P_BF16_MASTER, P_BF16 };
 
@@ -48,7 +52,7 @@ struct StepArgs {
   ChunkTable chunks;
   int n_chunks;
   int64_t* steps;
-  unsigned* ticket;     // 0 between launches
+  unsigned* ticket;     // (and the other counters) 0 between launches
   const double* parts;  // sums of squares, or NULL: no clipping
   int n_parts;
   float max_norm;
@@ -69,11 +73,17 @@ __device__ __forceinline__ void put(T* p, V v) {
   *(__attribute__((address_space(1))) V*)(uintptr_t)p = v;
 }
 
-// Eight elements, element-aligned accesses of 8 and 16 bytes; FULL, or the first n.
-template <bool FULL>
-__device__ __forceinline__ void load8(const float* p, int64_t n, float v[8]) {
+// What a tensor has of a thread's eight elements: all (WHOLE); or the first n, behind which the tensor
+// ends (n <= 0: none), and which come as the last of the tensor's last eight (PART: no branch keeps a
+// load from starting before another is done; one tensor of 2047 in fp32 4.4 -> 4.1 us, in bf16 with
+// 8-bit states 6.7 -> 4.9); or, of a tensor of fewer than eight, one at a time (FEW).
+enum Reach { WHOLE, PART, FEW };
+
+// Eight elements from p on, element-aligned accesses of 8 and 16 bytes; FEW: the first n.
+template <Reach R>
+__device__ __forceinline__ void load8(const float* p, int n, float v[8]) {
   typedef f32x4_t __attribute__((aligned(4))) any_t;
-  if (FULL || n >= 8) {
+  if constexpr (R != FEW) {
     const f32x4_t a = get<any_t>(p), b = get<any_t>(p + 4);
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = a[k], v[4 + k] = b[k];
@@ -82,10 +92,10 @@ __device__ __forceinline__ void load8(const float* p, int64_t n, float v[8]) {
     for (int k = 0; k < 8; ++k) v[k] = k < n ? get<float>(p + k) : 0.0f;
   }
 }
-template <bool FULL>
-__device__ __forceinline__ void load8(const bf16_t* p, int64_t n, float v[8]) {
+template <Reach R>
+__device__ __forceinline__ void load8(const bf16_t* p, int n, float v[8]) {
   typedef u32x4_t __attribute__((aligned(2))) any_t;
-  if (FULL || n >= 8) {
+  if constexpr (R != FEW) {
     const u32x4_t a = get<any_t>(p);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -97,19 +107,38 @@ __device__ __forceinline__ void load8(const bf16_t* p, int64_t n, float v[8]) {
     for (int k = 0; k < 8; ++k) v[k] = k < n ? bf2f(get<bf16_t>(p + k)) : 0.0f;
   }
 }
-template <bool FULL>
-__device__ __forceinline__ u32x2_t load8(const uint8_t* p, int64_t n) {
+template <Reach R>
+__device__ __forceinline__ u32x2_t load8(const uint8_t* p, int n) {
   typedef u32x2_t __attribute__((aligned(1))) any_t;
-  if (FULL || n >= 8) return get<any_t>(p);
+  if constexpr (R != FEW) return get<any_t>(p);
   u32x2_t r = {0, 0};
 #pragma unroll
   for (int k = 0; k < 8; ++k) r[k >> 2] |= (k < n ? (uint32_t)get<uint8_t>(p + k) : 0) << (8 * (k & 3));
   return r;
 }
-template <bool FULL>
-__device__ __forceinline__ void store8(float* p, int64_t n, const float v[8]) {
+// PART: the first `gone` of eight go, zeros come in at the end (8 or more: all).
+template <Reach R>
+__device__ __forceinline__ void drop(float v[8], int gone) {
+  if constexpr (R == PART) {
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = gone & o ? (k + o < 8 ? v[k + o < 8 ? k + o : 7] : 0.0f) : v[k];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = gone < 8 ? v[k] : 0.0f;
+  }
+}
+template <Reach R>
+__device__ __forceinline__ void drop(u32x2_t& c, int gone) {
+  if constexpr (R == PART) {
+    const uint64_t r = gone < 8 ? ((uint64_t)c[1] << 32 | c[0]) >> (8 * (gone & 7)) : 0;
+    c = u32x2_t{(uint32_t)r, (uint32_t)(r >> 32)};
+  }
+}
+template <Reach R>
+__device__ __forceinline__ void store8(float* p, int n, const float v[8]) {
   typedef f32x4_t __attribute__((aligned(4))) any_t;
-  if (FULL || n >= 8) {
+  if (R == WHOLE || n >= 8) {
     put<any_t>(p, f32x4_t{v[0], v[1], v[2], v[3]});
     put<any_t>(p + 4, f32x4_t{v[4], v[5], v[6], v[7]});
   } else {
@@ -118,10 +147,10 @@ __device__ __forceinline__ void store8(float* p, int64_t n, const float v[8]) {
       if (k < n) put<float>(p + k, v[k]);
   }
 }
-template <bool FULL>
-__device__ __forceinline__ void store8(bf16_t* p, int64_t n, u32x4_t r) {
+template <Reach R>
+__device__ __forceinline__ void store8(bf16_t* p, int n, u32x4_t r) {
   typedef u32x4_t __attribute__((aligned(2))) any_t;
-  if (FULL || n >= 8) {
+  if (R == WHOLE || n >= 8) {
     put<any_t>(p, r);
   } else {
 #pragma unroll
@@ -129,10 +158,10 @@ __device__ __forceinline__ void store8(bf16_t* p, int64_t n, u32x4_t r) {
       if (k < n) put<bf16_t>(p + k, (bf16_t)(r[k >> 1] >> (16 * (k & 1))));
   }
 }
-template <bool FULL>
-__device__ __forceinline__ void store8(uint8_t* p, int64_t n, const uint32_t c[8]) {
+template <Reach R>
+__device__ __forceinline__ void store8(uint8_t* p, int n, const uint32_t c[8]) {
   typedef u32x2_t __attribute__((aligned(1))) any_t;
-  if (FULL || n >= 8) {
+  if (R == WHOLE || n >= 8) {
     put<any_t>(p, u32x2_t{c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24,
                           c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24});
   } else {
@@ -247,26 +276,35 @@ __device__ __forceinline__ void new_states(const float g[8], const Step& s, floa
   }
 }
 
-// Eight elements from i of a tensor: all of them (FULL), or those of it.
-template <int KIND, bool GRAD_BF16, int BITS, bool FULL>
+// Eight elements from i of a tensor, or what it has of them.
+template <int KIND, bool GRAD_BF16, int BITS, Reach R>
 __device__ __forceinline__ void update8(const Tensor& x, int64_t i, const Step& s) {
-  const int64_t n = x.n - i;
-  float w[8], g[8], m[8], v[8];
-  if constexpr (KIND == P_F32) load8<FULL>((const float*)x.p + i, n, w);
-  else if constexpr (KIND == P_BF16_MASTER) load8<FULL>(x.master + i, n, w);
-  else load8<FULL>((const bf16_t*)x.p + i, n, w);
-  if constexpr (GRAD_BF16) load8<FULL>((const bf16_t*)x.g + i, n, g);
-  else load8<FULL>((const float*)x.g + i, n, g);
   const int64_t block = i / ADAMW_BLOCK;
+  if (R != WHOLE && block * ADAMW_BLOCK >= x.n) return;  // (with the other lanes of the block)
+  const int n = R == WHOLE ? 8 : (int)max((int64_t)0, min((int64_t)8, x.n - i));
+  const int64_t at = R == PART ? min(i, x.n - 8) : i;
+  const int gone = (int)(i - at);
+  float w[8], g[8], m[8], v[8];
+  if constexpr (KIND == P_F32) load8<R>((const float*)x.p + at, n, w);
+  else if constexpr (KIND == P_BF16_MASTER) load8<R>(x.master + at, n, w);
+  else load8<R>((const bf16_t*)x.p + at, n, w);
+  if constexpr (GRAD_BF16) load8<R>((const bf16_t*)x.g + at, n, g);
+  else load8<R>((const float*)x.g + at, n, g);
   if constexpr (BITS == 8) {
-    const u32x2_t cm = load8<FULL>((const uint8_t*)x.m + i, n), cv = load8<FULL>((const uint8_t*)x.v + i, n);
-    const bool here = FULL || n > 0;
-    from_e4m3(cm, here ? get<float>(x.m_scale + block) : 0.0f, m);
-    from_e5m2(cv, here ? get<float>(x.v_scale + block) : 0.0f, v);
+    u32x2_t cm = load8<R>((const uint8_t*)x.m + at, n), cv = load8<R>((const uint8_t*)x.v + at, n);
+    const float sm = get<float>(x.m_scale + block), sv = get<float>(x.v_scale + block);
+    drop<R>(cm, gone);
+    drop<R>(cv, gone);
+    from_e4m3(cm, sm, m);
+    from_e5m2(cv, sv, v);
   } else {
-    load8<FULL>((const float*)x.m + i, n, m);
-    load8<FULL>((const float*)x.v + i, n, v);
+    load8<R>((const float*)x.m + at, n, m);
+    load8<R>((const float*)x.v + at, n, v);
+    drop<R>(m, gone);
+    drop<R>(v, gone);
   }
+  drop<R>(w, gone);
+  drop<R>(g, gone);
   new_states(g, s, m, v);
   const float keep = 1.0f - s.lr * x.lr_scale * x.decay, rate = s.lr_bias * x.lr_scale;
 #pragma unroll
@@ -280,7 +318,7 @@ __device__ __forceinline__ void update8(const Tensor& x, int64_t i, const Step& 
 #pragma unroll
     for (int k = 0; k < 8; ++k) r[k] = random_bits((uint32_t)i + k, s.t);
   if constexpr (KIND == P_F32) {
-    store8<FULL>((float*)x.p + i, n, w);
+    store8<R>((float*)x.p + i, n, w);
   } else {
     u32x4_t b;
 #pragma unroll
@@ -288,8 +326,8 @@ __device__ __forceinline__ void update8(const Tensor& x, int64_t i, const Step& 
       b[k] = KIND == P_BF16 ? (__float_as_uint(w[2 * k]) + (r[2 * k] >> 16)) >> 16 |
                                   ((__float_as_uint(w[2 * k + 1]) + (r[2 * k + 1] >> 16)) & 0xffff0000u)
                             : pack_bf16x2(w[2 * k], w[2 * k + 1]);
-    store8<FULL>((bf16_t*)x.p + i, n, b);
-    if constexpr (KIND == P_BF16_MASTER) store8<FULL>(x.master + i, n, w);
+    store8<R>((bf16_t*)x.p + i, n, b);
+    if constexpr (KIND == P_BF16_MASTER) store8<R>(x.master + i, n, w);
   }
   if constexpr (BITS == 8) {
     uint32_t top_m = 0, top_v = 0;
@@ -311,32 +349,33 @@ __device__ __forceinline__ void update8(const Tensor& x, int64_t i, const Step& 
         if (sm.y == 0.0f) cm[k] = 0;
         if (sv.y == 0.0f) cv[k] = 0;
       }
-    store8<FULL>((uint8_t*)x.m + i, n, cm);
-    store8<FULL>((uint8_t*)x.v + i, n, cv);
-    if ((threadIdx.x & 31) == 0 && (FULL || n > 0)) {
+    store8<R>((uint8_t*)x.m + i, n, cm);
+    store8<R>((uint8_t*)x.v + i, n, cv);
+    if ((threadIdx.x & 31) == 0 && n > 0) {
       put<float>(x.m_scale + block, sm.x);
       put<float>(x.v_scale + block, sv.x);
     }
   } else {
-    store8<FULL>((float*)x.m + i, n, m);
-    store8<FULL>((float*)x.v + i, n, v);
+    store8<R>((float*)x.m + i, n, m);
+    store8<R>((float*)x.v + i, n, v);
   }
 }
 
 template <int KIND, bool GRAD_BF16, int BITS>
-__device__ __forceinline__ void update_chunk(const Tensor& x, int64_t i, bool full, const Step& s) {
-  if (full) update8<KIND, GRAD_BF16, BITS, true>(x, i, s);
-  else update8<KIND, GRAD_BF16, BITS, false>(x, i, s);
+__device__ __forceinline__ void update_chunk(const Tensor& x, int64_t i, Reach r, const Step& s) {
+  if (r == WHOLE) update8<KIND, GRAD_BF16, BITS, WHOLE>(x, i, s);
+  else if (r == PART) update8<KIND, GRAD_BF16, BITS, PART>(x, i, s);
+  else update8<KIND, GRAD_BF16, BITS, FEW>(x, i, s);
 }
 template <int KIND, bool GRAD_BF16>
-__device__ __forceinline__ void update_bits(const Tensor& x, int64_t i, bool full, const Step& s) {
-  if (x.bits == 8) update_chunk<KIND, GRAD_BF16, 8>(x, i, full, s);
-  else update_chunk<KIND, GRAD_BF16, 32>(x, i, full, s);
+__device__ __forceinline__ void update_bits(const Tensor& x, int64_t i, Reach r, const Step& s) {
+  if (x.bits == 8) update_chunk<KIND, GRAD_BF16, 8>(x, i, r, s);
+  else update_chunk<KIND, GRAD_BF16, 32>(x, i, r, s);
 }
 template <int KIND>
-__device__ __forceinline__ void update_grad(const Tensor& x, int64_t i, bool full, const Step& s) {
-  if (x.grad_bf16) update_bits<KIND, true>(x, i, full, s);
-  else update_bits<KIND, false>(x, i, full, s);
+__device__ __forceinline__ void update_grad(const Tensor& x, int64_t i, Reach r, const Step& s) {
+  if (x.grad_bf16) update_bits<KIND, true>(x, i, r, s);
+  else update_bits<KIND, false>(x, i, r, s);
 }
 
 // beta^t by squaring, in 64 bits.
@@ -369,10 +408,12 @@ __device__ __forceinline__ Chunk chunk_at(const StepArgs& a, int c) {
 }
 
 // Two work-groups to a CU that take chunk after chunk: 128 bytes a thread in flight are enough, and
-// what each has to set up (the powers, the norm's parts, a ticket) is done 512 times.  us by
-// work-groups a CU, 1 / 2 / 3 / 4: 50M weights with 8-bit states (0.8 GB) 240 / 150 / 165 / 166, 504M
-// in bf16 (15 GB, clipped) 3365 / 3363 / 3385 / 3383, 5M in fp32 (139 MB, clipped) 31.6 / 32.2 /
-// 31.9 / 33.5; numbers between leave CUs with unequal shares (1.25: 205, 4322, 33.8).
+// what each has to set up (the powers, the norm's parts) is done 512 times.  us by work-groups a CU,
+// 1 / 2 / 3 / 4: 50M weights with 8-bit states (0.8 GB) 240 / 150 / 165 / 166, 504M in bf16 (15 GB,
+// clipped) 3365 / 3363 / 3385 / 3383, 5M in fp32 (139 MB, clipped) 31.6 / 32.2 / 31.9 / 33.5; numbers
+// between leave CUs with unequal shares (1.25: 205, 4322, 33.8).  Four where an element is LIGHT: bf16
+// without master copies and 8-bit states, 50M weights 133 / 119 with 2 / 4, with gradients in fp32
+// 138 / 128, 19M weights 63 / 52.
 __global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
   __shared__ double lds[THREADS / 64];
   const int64_t t = *a.steps + 1;
@@ -402,20 +443,38 @@ __global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
     const Chunk next = chunk_at(a, min(c + (int)gridDim.x, a.n_chunks - 1));
     const Tensor x = tensor_at(a, ch.tensor);
     const int64_t first = (int64_t)ch.index * CHUNK, i = first + 8 * threadIdx.x;
-    const bool full = first + CHUNK <= x.n;
-    if (x.kind == P_F32) update_grad<P_F32>(x, i, full, s);
-    else if (x.kind == P_BF16_MASTER) update_grad<P_BF16_MASTER>(x, i, full, s);
-    else update_grad<P_BF16>(x, i, full, s);
+    const Reach r = first + CHUNK <= x.n ? WHOLE : x.n >= 8 ? PART : FEW;
+    if (x.kind == P_F32) update_grad<P_F32>(x, i, r, s);
+    else if (x.kind == P_BF16_MASTER) update_grad<P_BF16_MASTER>(x, i, r, s);
+    else update_grad<P_BF16>(x, i, r, s);
     ch = next;
   }
   // All of a work-group have read the number of steps before it takes a ticket, so the one with
-  // the last ticket may raise it.  (Taken on the way in, the tickets of 2048 work-groups, 9 ns
-  // each, kept them from their work: 139 MB 34.6 -> 48 us.)
+  // the last ticket may raise it.  A counter serves a work-group in 9 ns, and many end together: 24
+  // fp32 tensors of 208 chunks 6.8 us with the last counter alone, 5.4 so, 900 of a chunk each 10.8 and
+  // 7.2 (and on the way in, tickets keep work-groups from their work: 139 MB 34.6 -> 48 us).
   __syncthreads();
-  if (threadIdx.x == 0 && atomicAdd(a.ticket, 1u) == gridDim.x - 1) {
-    if (go) *a.steps = t;
-    *a.ticket = 0;
+  if (threadIdx.x != 0) return;
+  unsigned last = gridDim.x;
+  if (gridDim.x > COUNTERS) {
+    last = COUNTERS;
+    const unsigned mine = blockIdx.x % COUNTERS;
+    unsigned* const first = a.ticket + TICKET_STEP * (1 + mine);
+    if (atomicAdd(first, 1u) + 1 < (gridDim.x - mine + COUNTERS - 1) / COUNTERS) return;
+    *first = 0;
   }
+  if (atomicAdd(a.ticket, 1u) + 1 < last) return;
+  *a.ticket = 0;
+  if (go) *a.steps = t;
+}
+
+template <Reach R>
+__device__ __forceinline__ void gradients(const Tensor& x, int64_t i, float g[8]) {
+  const int n = R == WHOLE ? 8 : (int)max((int64_t)0, min((int64_t)8, x.n - i));
+  const int64_t at = R == PART ? min(i, x.n - 8) : i;
+  if (x.grad_bf16) load8<R>((const bf16_t*)x.g + at, n, g);
+  else load8<R>((const float*)x.g + at, n, g);
+  drop<R>(g, (int)(i - at));
 }
 
 // Sums of squares of the gradients, a work-group's chunks together, in 64 bits (squares of
@@ -426,10 +485,11 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const StepArgs a, double*
   for (int c = blockIdx.x; c < a.n_chunks; c += gridDim.x) {
     const Chunk ch = chunk_at(a, c);
     const Tensor x = tensor_at(a, ch.tensor);
-    const int64_t i = (int64_t)ch.index * CHUNK + 8 * threadIdx.x;
+    const int64_t first = (int64_t)ch.index * CHUNK;
     float g[8];
-    if (x.grad_bf16) load8<false>((const bf16_t*)x.g + i, x.n - i, g);
-    else load8<false>((const float*)x.g + i, x.n - i, g);
+    if (first + CHUNK <= x.n) gradients<WHOLE>(x, first + 8 * threadIdx.x, g);
+    else if (x.n >= 8) gradients<PART>(x, first + 8 * threadIdx.x, g);
+    else gradients<FEW>(x, first + 8 * threadIdx.x, g);
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum = fma((double)g[k], (double)g[k], sum);
   }
@@ -452,6 +512,7 @@ stage_status bad(stage_status st, const char* fmt, ...) {
 struct adamw {
   int device = 0;
   int n_chunks = 0;
+  int groups = 0;          // most work-groups
   void* memory = nullptr;  // parts, ticket, tensors, chunks
   double* parts = nullptr;
   unsigned* ticket = nullptr;
@@ -533,7 +594,14 @@ stage_status adamw_init(const adamw_tensor* tensors, int n, int64_t* steps, adam
   adamw_t* h = new adamw_t;
   h->steps = steps;
   h->n_chunks = n_chunks;
-  const size_t at_ticket = MOST_PARTS * sizeof(double), at_tensors = at_ticket + 64;
+  int64_t elements = 0, traffic = 0;
+  for (const Tensor& t : host) {
+    elements += t.n;
+    traffic += t.n * ((t.kind == P_F32 ? 8 : t.kind == P_BF16_MASTER ? 10 : 4) + (t.grad_bf16 ? 2 : 4) +
+                      (t.bits == 8 ? 4 : 16));
+  }
+  h->groups = traffic < LIGHT * elements ? GROUPS_LIGHT : GROUPS;
+  const size_t at_ticket = MOST_PARTS * sizeof(double), at_tensors = at_ticket + (1 + COUNTERS) * TICKET_STEP * 4;
   const size_t at_chunks = at_tensors + host.size() * sizeof(Tensor);
   const size_t bytes = at_chunks + chunks.size() * sizeof(Chunk);
   hipError_t e = hipGetDevice(&h->device);
@@ -598,7 +666,7 @@ stage_status adamw_step(adamw_t* h, const adamw_args* a, void* hip_stream) {
     k.n_parts = std::max(1, std::min(MOST_PARTS, h->n_chunks));
     hipLaunchKernelGGL(norm_kernel, dim3(k.n_parts), dim3(THREADS), 0, st, k, h->parts);
   }
-  hipLaunchKernelGGL(step_kernel, dim3(std::max(1, std::min(MOST_GROUPS, h->n_chunks))), dim3(THREADS), 0, st, k);
+  hipLaunchKernelGGL(step_kernel, dim3(std::max(1, std::min(h->groups, h->n_chunks))), dim3(THREADS), 0, st, k);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return bad(STAGE_EHIP, "adamw_step: %s", hipGetErrorString(e));
   return STAGE_OK;

@@ -110,6 +110,44 @@ def test_steps(dtype, grad, master, bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype,grad", [("f32", "f32"), ("bf16", "bf16")])
+def test_ends(dtype, grad, bits):
+    """Each number of elements behind the last whole eight, in the first block, in a later one and just
+    behind a chunk, between NaN that no result shows."""
+    sizes = [b + r for b in (0, 8, 248, 1024, 2040, 2048) for r in range(1, 8)]
+    x = Tensors(sizes, dtype, grad, bits, master=False)
+    big = [[torch.full((n + 16,), float("nan"), device="cuda", dtype=t.dtype) for n, t in zip(sizes, ts)]
+           for ts in (x.params, x.grads)]
+    for views, ts in zip(big, (x.params, x.grads)):
+        for i, t in enumerate(list(ts)):
+            views[i][8:-8] = t
+            ts[i] = views[i][8:-8]
+    x.opt = P.AdamW(x.params, x.grads, **x.kw)
+    for t in range(1, 3):
+        check_step(x, t, 0.1)
+    for t in big[0] + big[1]:
+        assert t[:8].isnan().all() and t[-8:].isnan().all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_of_any_number_of_chunks(bits):
+    """The number of steps is raised once, by however many work-groups there are."""
+    for n in (1, 2, 31, 32, 33, 63, 64, 65, 100, 511, 512, 513, 1023, 1024, 1025, 2000):
+        p, g = torch.ones(2048 * n, device="cuda").bfloat16(), torch.ones(2048 * n, device="cuda").bfloat16()
+        opt = P.AdamW([p], [g], weight_decay=0.0, state_bits=bits, master=False)
+        for t in range(1, 5):
+            opt.step(0.0)
+            assert opt.state["steps"].item() == t, n
+        # 1 - 0.9^4 = 0.3439.  fp32: three roundings a step, 12 * 2^-24 * 0.35 in all.  8 bits: each
+        # step adds at most 2^-3 of the value to 0.9 of the error, 0.0125, 0.037, 0.071, 0.115.
+        m = opt.state["exp_avg"][0].float().view(-1, 256)
+        if bits == 8:
+            m = m * opt.state["exp_avg_scale"][0][:, None]
+        assert (m - (1 - 0.9 ** 4)).abs().max() < (0.115 if bits == 8 else 2.6e-7), n
+        assert (p == 1).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_late_steps(bits):
     """A step counter beyond 32 bits: no bias is left, the bits' step wraps."""
     x = Tensors([5000], bits=bits)
