@@ -753,7 +753,7 @@ def _ops_setup():
                                 lib.adamw_step, lib.adamw_last_error)),
                     StageError, torch.bfloat16, torch.float32, torch.uint8, torch.int32,
                     torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
-                    lambda n, dev: torch.empty(n, dtype=torch.uint8, device=dev))
+                    lambda n, dev: torch.empty(n, dtype=torch.uint8, device=dev), torch.empty_like)
     _ops_module = _ops_call
     return _ops_module
 

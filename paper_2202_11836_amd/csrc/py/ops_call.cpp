@@ -20,11 +20,31 @@ decltype(&rotary_backward) rotary_backward_fn;
 decltype(&rotary_last_error) rotary_error_fn;
 decltype(&adamw_step) adamw_step_fn;
 decltype(&adamw_last_error) adamw_error_fn;
+PyObject* empty_like;  // torch's
 
 bool wants(const char* name, Py_ssize_t n, Py_ssize_t takes) {
   if (n == takes && norm_forward_fn) return true;
   PyErr_Format(PyExc_TypeError, "%s takes %zd arguments, after setup", name, takes);
   return false;
+}
+
+// A new tensor shaped like `like`, of which t says what there is to know, and what there is to know of
+// the new one.  (empty_like keeps the strides of a contiguous tensor, and is faster: 1.1 us, 1.5 with
+// the shape handed over; what is new needs no checks: another 0.4.)
+PyObject* fresh(PyObject* like, const Tensor& t, Tensor* made) {
+  int64_t step = 1;
+  bool packed = true;
+  *made = t;
+  for (int i = t.nd - 1; i >= 0; --i) {
+    if (t.size[i] != 1 && t.stride[i] != step) packed = false;
+    made->stride[i] = step;
+    step *= t.size[i] > 1 ? t.size[i] : 1;
+  }
+  Ref x(packed ? PyObject_CallOneArg(empty_like, like) : output(Py_None, like));
+  Ref p(x.p ? PyObject_CallMethodNoArgs(x.p, n_data_ptr) : nullptr);
+  if (!p.p) return nullptr;
+  made->p = PyLong_AsVoidPtr(p.p);
+  return !made->p && PyErr_Occurred() ? nullptr : x.release();
 }
 
 // ---------------------------------------------------------------------------
@@ -49,9 +69,7 @@ bool rows_of(const char* name, PyObject* x, Rows* r) {
   return true;
 }
 // A tensor of the same sizes and type: its pointer, and its strides of batch and position.
-bool like_rows(const char* name, PyObject* x, const Rows& r, void** p, int64_t* st, Tensor* out = nullptr) {
-  Tensor t;
-  if (!load(name, x, &t, MAX_DIMS)) return false;
+bool like_rows(const char* name, const Tensor& t, const Rows& r, void** p, int64_t* st) {
   if (!same(t, r.like.nd, r.like.size, r.like.dtype, r.like.dev))
     return refuse("%s must be %s, on cuda:%d, with the sizes of the other tensors of the call", name,
                   name_of(r.like.dtype), r.like.dev);
@@ -77,8 +95,22 @@ bool like_rows(const char* name, PyObject* x, const Rows& r, void** p, int64_t* 
     }
   }
   *p = t.p;
-  if (out) *out = t;
   return true;
+}
+bool like_rows(const char* name, PyObject* x, const Rows& r, void** p, int64_t* st) {
+  Tensor t;
+  return load(name, x, &t, MAX_DIMS) && like_rows(name, t, r, p, st);
+}
+// The one given, or, where that is None, a new one like x, whose rows are r.
+bool rows_output(const char* name, PyObject* given, PyObject* x, const Rows& r, Ref* out, void** p, int64_t* st) {
+  if (given != Py_None) {
+    Py_INCREF(given);
+    out->set(given);
+    return like_rows(name, given, r, p, st);
+  }
+  Tensor t;
+  out->set(fresh(x, r.like, &t));
+  return out->p && like_rows(name, t, r, p, st);
 }
 // fp32 [width], or None.
 bool weight(const char* name, PyObject* x, const Rows& r, void** p) {
@@ -99,21 +131,36 @@ bool stat(const char* name, PyObject* x, const Rows& r, void** p) {
   *p = t.p;
   return true;
 }
-PyObject* new_stat(PyObject* like, const Rows& r) {
-  Ref shape(PyTuple_New(r.like.nd - 1));
-  if (!shape.p) return nullptr;
-  for (int i = 0; i < r.like.nd - 1; ++i) {
-    PyObject* n = PyLong_FromLongLong(r.like.size[i]);
-    if (!n) return nullptr;
-    PyTuple_SET_ITEM(shape.p, i, n);
+// The two statistics, of which those that are None are new.
+bool stat_outputs(PyObject* const* given, PyObject* like, const Rows& r, Ref* m, Ref* rs, void** mean, void** rstd) {
+  Tensor t, made;
+  PyObject* of = nullptr;  // the first new one, and what t tells of it
+  Ref* const out[2] = {m, rs};
+  void** const p[2] = {mean, rstd};
+  for (int i = 0; i < 2; ++i) {
+    if (given[i] != Py_None) {
+      Py_INCREF(given[i]);
+      out[i]->set(given[i]);
+      if (!stat(i ? "rstd" : "mean", given[i], r, p[i])) return false;
+    } else if (of) {
+      out[i]->set(fresh(of, t, &made));
+      if (!out[i]->p) return false;
+      *p[i] = made.p;
+    } else {
+      Ref shape(PyTuple_New(r.like.nd - 1));
+      if (!shape.p) return false;
+      for (int j = 0; j < r.like.nd - 1; ++j) {
+        PyObject* n = PyLong_FromLongLong(r.like.size[j]);
+        if (!n) return false;
+        PyTuple_SET_ITEM(shape.p, j, n);
+      }
+      PyObject* args[3] = {like, shape.p, f32};
+      out[i]->set(PyObject_VectorcallMethod(n_new_empty, args, 2, kw_dtype));
+      if (!out[i]->p || !load("mean", of = out[i]->p, &t, MAX_DIMS)) return false;
+      *p[i] = t.p;
+    }
   }
-  PyObject* args[3] = {like, shape.p, f32};
-  return PyObject_VectorcallMethod(n_new_empty, args, 2, kw_dtype);
-}
-PyObject* stat_output(PyObject* given, PyObject* like, const Rows& r) {
-  if (given == Py_None) return new_stat(like, r);
-  Py_INCREF(given);
-  return given;
+  return true;
 }
 bool norm_done(stage_status st) { return st == STAGE_OK || raise((int)st, norm_error_fn()); }
 
@@ -137,7 +184,7 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (eps == -1.0 && PyErr_Occurred()) return nullptr;
   layer_norm_shape s = norm_shape(r, (float)eps);
   void *x, *res = nullptr, *gamma, *beta, *out, *total = nullptr, *mean, *rstd;
-  if (!like_rows("x", a[0], r, &x, s.x) || !weight("gamma", a[1], r, &gamma) ||
+  if (!like_rows("x", r.like, r, &x, s.x) || !weight("gamma", a[1], r, &gamma) ||
       !weight("beta", a[2], r, &beta))
     return nullptr;
   const bool add = a[3] != Py_None;
@@ -145,14 +192,15 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!add && a[6] != Py_None) return refuse("total without a residual"), nullptr;
   const int here = on_device(r.like.dev);
   if (here <= 0) return here < 0 ? nullptr : PyLong_FromLong(r.like.dev);
-  Ref o(output(a[5], a[0])), tot(!o.p ? nullptr : add ? output(a[6], a[0]) : (Py_INCREF(a[0]), a[0]));
-  if (!tot.p) return nullptr;
-  Ref m(stat_output(a[7], a[0], r)), rs(m.p ? stat_output(a[8], a[0], r) : nullptr);
-  if (!rs.p) return nullptr;
-  if (!like_rows("out", o.p, r, &out, s.out) ||
-      (add && !like_rows("total", tot.p, r, &total, s.total)) || !stat("mean", m.p, r, &mean) ||
-      !stat("rstd", rs.p, r, &rstd))
+  Ref o, tot, m, rs;
+  if (!rows_output("out", a[5], a[0], r, &o, &out, s.out)) return nullptr;
+  if (!add) {
+    Py_INCREF(a[0]);
+    tot.set(a[0]);
+  } else if (!rows_output("total", a[6], a[0], r, &tot, &total, s.total)) {
     return nullptr;
+  }
+  if (!stat_outputs(a + 7, a[0], r, &m, &rs, &mean, &rstd)) return nullptr;
   Room room;
   if (!take_room(r.like.dev, 0, &room)) return nullptr;
   stage_status st;
@@ -173,7 +221,11 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   layer_norm_shape s = norm_shape(r, 0.0f);
   void *dy, *total, *gamma, *mean, *rstd, *dtotal = nullptr, *dx = nullptr, *dgamma = nullptr,
                                           *dbeta = nullptr;
-  if (!like_rows("dy", a[0], r, &dy, s.dy) || !like_rows("total", a[1], r, &total, s.total) ||
+  Tensor weights;  // gamma
+  weights.nd = 1;
+  weights.size[0] = r.width;
+  weights.stride[0] = 1;
+  if (!like_rows("dy", r.like, r, &dy, s.dy) || !like_rows("total", a[1], r, &total, s.total) ||
       !weight("gamma", a[2], r, &gamma) || !stat("mean", a[3], r, &mean) ||
       !stat("rstd", a[4], r, &rstd) ||
       (a[5] != Py_None && !like_rows("dtotal", a[5], r, &dtotal, s.dtotal)))
@@ -181,25 +233,34 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int here = on_device(r.like.dev);
   if (here <= 0) return here < 0 ? nullptr : PyLong_FromLong(r.like.dev);
   Ref x, g, b;
-  const bool makes[3] = {a[6] != Py_False, a[7] != Py_False, a[8] != Py_False};
-  Ref* const to[3] = {&x, &g, &b};
-  for (int i = 0; i < 3; ++i) {
-    if (!makes[i]) {
-      Py_INCREF(Py_None);
-      to[i]->set(Py_None);
-    } else if (i == 0 || a[6 + i] != Py_None) {
-      to[i]->set(output(a[6 + i], a[0]));
+  if (a[6] == Py_False) {
+    Py_INCREF(Py_None);
+    x.set(Py_None);
+  } else if (!rows_output("dx", a[6], a[0], r, &x, &dx, s.dx)) {
+    return nullptr;
+  }
+  Ref* const to[2] = {&g, &b};
+  void** const p[2] = {&dgamma, &dbeta};
+  for (int i = 0; i < 2; ++i) {
+    const bool none = a[7 + i] == Py_False;
+    if (none || a[7 + i] != Py_None) {
+      PyObject* given = none ? Py_None : a[7 + i];
+      Py_INCREF(given);
+      to[i]->set(given);
+      if (!weight(i ? "dbeta" : "dgamma", given, r, p[i])) return nullptr;
+    } else if (a[2] != Py_None) {
+      Tensor made;
+      to[i]->set(fresh(a[2], weights, &made));
+      if (!to[i]->p) return nullptr;
+      *p[i] = made.p;
     } else {
       Ref shape(Py_BuildValue("(L)", (long long)r.width));
       if (!shape.p) return nullptr;
       PyObject* args[3] = {a[0], shape.p, f32};
       to[i]->set(PyObject_VectorcallMethod(n_new_empty, args, 2, kw_dtype));
+      if (!to[i]->p || !weight(i ? "dbeta" : "dgamma", to[i]->p, r, p[i])) return nullptr;
     }
-    if (!to[i]->p) return nullptr;
   }
-  if ((makes[0] && !like_rows("dx", x.p, r, &dx, s.dx)) || !weight("dgamma", g.p, r, &dgamma) ||
-      !weight("dbeta", b.p, r, &dbeta))
-    return nullptr;
   size_t bytes = 0;
   if ((dgamma || dbeta) && !norm_done(norm_workspace_fn(&s, &bytes))) return nullptr;
   Room room;
@@ -216,8 +277,7 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // ---------------------------------------------------------------------------
 // Rotary positions
 // ---------------------------------------------------------------------------
-bool heads(const char* name, PyObject* x, const Tensor* like, Tensor* t, int64_t* st) {
-  if (!load(name, x, t)) return false;
+bool heads(const char* name, const Tensor* like, Tensor* t, int64_t* st) {
   if (t->nd != 4 || t->size[3] != 64 || t->dev < 0 || (t->dtype != bf16 && t->dtype != f32))
     return refuse("%s must be bfloat16 or float32 [batch, length, heads, 64] on a GPU", name);
   for (int i = 0; i < 3; ++i)
@@ -228,6 +288,20 @@ bool heads(const char* name, PyObject* x, const Tensor* like, Tensor* t, int64_t
   if (t->stride[3] != 1) return refuse("the 64 values of a head of %s must lie side by side", name);
   for (int i = 0; i < 3; ++i) st[i] = t->stride[i];
   return true;
+}
+bool heads(const char* name, PyObject* x, const Tensor* like, Tensor* t, int64_t* st) {
+  return load(name, x, t) && heads(name, like, t, st);
+}
+// The one given, or, where that is None, a new one like x, which `of` is of.
+bool heads_output(const char* name, PyObject* given, PyObject* x, const Tensor& of, const Tensor* like, Ref* out,
+                  Tensor* t, int64_t* st) {
+  if (given != Py_None) {
+    Py_INCREF(given);
+    out->set(given);
+    return heads(name, given, like, t, st);
+  }
+  out->set(fresh(x, of, t));
+  return out->p && heads(name, like, t, st);
 }
 
 // rotary(backward, freqs, q, k, pos, q_out, k_out): (q_out, k_out), or the device as above.
@@ -264,17 +338,14 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   const int here = on_device(q.dev);
   if (here <= 0) return here < 0 ? nullptr : PyLong_FromLong(q.dev);
-  Ref q_out(output(a[5], a[2])), k_out;
-  if (!q_out.p) return nullptr;
-  if (both) {
-    k_out.set(output(a[6], a[3]));
-  } else {
+  Ref q_out, k_out;
+  if (!heads_output("q_out", a[5], a[2], q, &q, &q_out, &qo, s.q_out)) return nullptr;
+  if (!both) {
     Py_INCREF(Py_None);
     k_out.set(Py_None);
-  }
-  if (!k_out.p || !heads("q_out", q_out.p, &q, &qo, s.q_out) ||
-      (both && !heads("k_out", k_out.p, &q, &ko, s.k_out)))
+  } else if (!heads_output("k_out", a[6], a[3], k, &q, &k_out, &ko, s.k_out)) {
     return nullptr;
+  }
   if (qo.size[2] != q.size[2] || (both && ko.size[2] != k.size[2]))
     return refuse("q_out and k_out must have the heads of q and k"), nullptr;
   Room room;
@@ -339,15 +410,18 @@ PyObject* adamw_call(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-// setup(addresses of the nine functions above, in their order; then as set_common())
+// setup(addresses of the nine functions above, in their order; then as set_common(); torch.empty_like)
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 17) {
-    PyErr_SetString(PyExc_TypeError, "setup takes 17 arguments");
+  if (n != 18) {
+    PyErr_SetString(PyExc_TypeError, "setup takes 18 arguments");
     return nullptr;
   }
   void* f[9];
   if (!addresses(a, 9, f)) return nullptr;
   set_common(a + 9);
+  Py_INCREF(a[17]);
+  Py_XDECREF(empty_like);
+  empty_like = a[17];
   norm_workspace_fn = (decltype(norm_workspace_fn))f[0];
   norm_forward_fn = (decltype(norm_forward_fn))f[1];
   norm_backward_fn = (decltype(norm_backward_fn))f[2];
