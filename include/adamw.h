@@ -76,8 +76,8 @@ typedef struct {
 
 /*
  * A handle for n tensors of the current device.  Allocates device memory for their addresses
- * and copies them there; returns when that is done (so not during a capture).  steps: int64 on the device, the number of
- * steps done so far.  EINVAL for n < 0, a negative numel (0 is valid), null or misaligned
+ * and copies them there; returns when that is done (so not during a capture).  steps: int64 on
+ * the device, the number of steps done so far, 0 or more.  EINVAL for n < 0, a negative numel (0 is valid), null or misaligned
  * pointers, unknown types, scales or a master copy that do not fit the types, values that are
  * not finite, or 2^40 elements or more in all.
  */
@@ -96,7 +96,8 @@ typedef struct {
  * must be the current one.  EINVAL for what the comments rule out. */
 stage_status adamw_step(adamw_t* h, const adamw_args* a, void* hip_stream);
 
-/* Frees what the handle owns (waits for the device).  NULL is a no-op. */
+/* Frees what the handle owns (waits for the device; graphs that captured a step of it may not be
+ * replayed any more).  NULL is a no-op. */
 void adamw_destroy(adamw_t* h);
 
 /* Message of this thread's last failed adamw_ call ("" if none). */

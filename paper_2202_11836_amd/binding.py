@@ -862,7 +862,8 @@ class AdamW:
     state           the states to go on with (another AdamW's .state, say), held in place; None:
                     new ones
 
-    Steps of one AdamW go one after the other; a captured step counts on with each replay.
+    Steps of one AdamW go one after the other; a captured step counts on with each replay, for which
+    the AdamW has to be there still, and open.
 
     state: a dict of lists, an entry for each tensor: "exp_avg", "exp_avg_sq" (fp32, or
     float8_e4m3fn and float8_e5m2), "exp_avg_scale", "exp_avg_sq_scale" (8 bits: fp32, one for
