@@ -745,7 +745,7 @@ def _ops_setup():
         from . import _ops_call
     except ImportError as e:
         raise RuntimeError("_ops_call is not built; run __graft_entry__.build() first "
-                           "(it needs Python's headers)") from e
+                           "(it needs Python's and torch's headers)") from e
     _ops_call.setup(*(ctypes.cast(f, ctypes.c_void_p).value
                       for f in (lib.layer_norm_workspace, lib.layer_norm_forward,
                                 lib.layer_norm_backward, lib.layer_norm_last_error,
@@ -753,7 +753,7 @@ def _ops_setup():
                                 lib.adamw_step, lib.adamw_last_error)),
                     StageError, torch.bfloat16, torch.float32, torch.uint8, torch.int32,
                     torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
-                    lambda n, dev: torch.empty(n, dtype=torch.uint8, device=dev), torch.empty_like)
+                    lambda n, dev: torch.empty(n, dtype=torch.uint8, device=dev))
     _ops_module = _ops_call
     return _ops_module
 

@@ -49,15 +49,29 @@ def _compile(src: str) -> str:
     return obj
 
 
-# Python modules of host code (csrc/py) that marshal the operators' calls.
-BINDINGS = {"_attn_call": "attn_call.cpp", "_ops_call": "ops_call.cpp"}
+# Python modules of host code (csrc/py) that marshal the operators' calls, and whether they use
+# torch's C++ objects.
+BINDINGS = {"_attn_call": ("attn_call.cpp", False), "_ops_call": ("ops_call.cpp", True)}
+
+
+def _torch_flags() -> Optional[list]:
+    """Where torch's headers and libraries are, or None (torch itself is not imported; a program
+    that loads the module has)."""
+    import importlib.util
+    spec = importlib.util.find_spec("torch")
+    at = spec.submodule_search_locations[0] if spec and spec.submodule_search_locations else ""
+    include = os.path.join(at, "include")
+    if not at or not os.path.exists(os.path.join(include, "torch", "csrc", "autograd", "python_variable.h")):
+        return None
+    return ["-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
+            "-L" + os.path.join(at, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python"]
 
 
 def build_binding() -> Optional[str]:
     """The Python modules that marshal the operators' calls (host code): by $CXX, g++ or
     hipcc; the path of the attention operators' one.  None, with no module left, where
-    Python's headers are not installed: the stage and the allocator do without, and the
-    operators' first call from Python says what is missing."""
+    Python's headers are not installed (one of torch's objects: torch's): the stage and the
+    allocator do without, and the operators' first call from Python says what is missing."""
     import sysconfig
     include = sysconfig.get_paths()["include"]
     paths = {name: os.path.join(PKG, name + ".so") for name in BINDINGS}
@@ -68,9 +82,16 @@ def build_binding() -> Optional[str]:
                 os.remove(path)
         return None
     for name, path in paths.items():
-        src = os.path.join(CSRC, "py", BINDINGS[name])
+        source, with_torch = BINDINGS[name]
+        flags = _torch_flags() if with_torch else []
+        if flags is None:
+            print(f"{name} not built: no headers of torch", file=sys.stderr)
+            if os.path.exists(path):
+                os.remove(path)
+            continue
+        src = os.path.join(CSRC, "py", source)
         cmd = [os.environ.get("CXX") or shutil.which("g++") or HIPCC, "-O2", "-std=c++17", "-fPIC",
-               "-shared", "-I" + include, src, "-o", path + ".tmp"]
+               "-shared", "-I" + include, src, "-o", path + ".tmp"] + flags
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"{src}:\n{r.stderr}")

@@ -8,6 +8,58 @@
 
 namespace {
 
+bool ints(PyObject* t, int n, int64_t* out) {
+  for (int i = 0; i < n; ++i) {
+    out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
+    if (out[i] == -1 && PyErr_Occurred()) return false;
+  }
+  return true;
+}
+
+bool load(const char* name, PyObject* t, Tensor* o, int most) {
+  Ref shape(PyObject_GetAttr(t, n_shape));
+  if (!shape.p) return false;
+  Ref stride(PyObject_CallMethodNoArgs(t, n_stride));
+  if (!stride.p) return false;
+  if (!PyTuple_Check(shape.p) || !PyTuple_Check(stride.p) ||
+      PyTuple_GET_SIZE(shape.p) != PyTuple_GET_SIZE(stride.p))
+    return refuse("%s is not a tensor", name);
+  if (PyTuple_GET_SIZE(shape.p) > most)
+    return refuse("%s has more than %s dimensions", name, most == 4 ? "four" : "eight");
+  o->nd = (int)PyTuple_GET_SIZE(shape.p);
+  if (!ints(shape.p, o->nd, o->size) || !ints(stride.p, o->nd, o->stride)) return false;
+  Ref dtype(PyObject_GetAttr(t, n_dtype));
+  if (!dtype.p) return false;
+  o->dtype = dtype.p;
+  Ref dev(PyObject_CallMethodNoArgs(t, n_get_device));
+  if (!dev.p) return false;
+  o->dev = (int)PyLong_AsLong(dev.p);
+  if (o->dev == -1 && PyErr_Occurred()) return false;
+  Ref p(PyObject_CallMethodNoArgs(t, n_data_ptr));
+  if (!p.p) return false;
+  o->p = PyLong_AsVoidPtr(p.p);
+  return o->p || !PyErr_Occurred();
+}
+
+PyObject* new_bytes(size_t n, int dev, void** p) {
+  Ref bytes(PyLong_FromSize_t(n)), on(PyLong_FromLong(dev));
+  if (!bytes.p || !on.p) return nullptr;
+  Ref t(PyObject_CallFunctionObjArgs(new_workspace, bytes.p, on.p, nullptr));
+  Ref at(t.p ? PyObject_CallMethodNoArgs(t.p, n_data_ptr) : nullptr);
+  if (!at.p) return nullptr;
+  *p = PyLong_AsVoidPtr(at.p);
+  return PyErr_Occurred() ? nullptr : t.release();
+}
+// given, or an uninitialised tensor shaped like `like` if it is None.
+PyObject* output(PyObject* given, PyObject* like) {
+  if (given != Py_None) {
+    Py_INCREF(given);
+    return given;
+  }
+  Ref shape(PyObject_GetAttr(like, n_shape));
+  return shape.p ? PyObject_CallMethodOneArg(like, n_new_empty, shape.p) : nullptr;
+}
+
 typedef decltype(&attn_workspace) WorkspaceFn;
 typedef decltype(&attn_forward) ForwardFn;
 typedef decltype(&attn_backward) BackwardFn;

@@ -1,5 +1,5 @@
-// What the modules of operators' calls share: references, errors, and what a call needs
-// to know of a tensor, by attribute.  Each module has its own copy.
+// What the modules of operators' calls share: references, errors, and checks of what a call
+// needs to know of a tensor.  Each module has its own copy.
 #pragma once
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -59,38 +59,10 @@ struct Tensor {
   void* p = nullptr;
 };
 
-bool ints(PyObject* t, int n, int64_t* out) {
-  for (int i = 0; i < n; ++i) {
-    out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
-    if (out[i] == -1 && PyErr_Occurred()) return false;
-  }
-  return true;
-}
-
-bool load(const char* name, PyObject* t, Tensor* o, int most = 4) {
-  Ref shape(PyObject_GetAttr(t, n_shape));
-  if (!shape.p) return false;
-  Ref stride(PyObject_CallMethodNoArgs(t, n_stride));
-  if (!stride.p) return false;
-  if (!PyTuple_Check(shape.p) || !PyTuple_Check(stride.p) ||
-      PyTuple_GET_SIZE(shape.p) != PyTuple_GET_SIZE(stride.p))
-    return refuse("%s is not a tensor", name);
-  if (PyTuple_GET_SIZE(shape.p) > most)
-    return refuse("%s has more than %s dimensions", name, most == 4 ? "four" : "eight");
-  o->nd = (int)PyTuple_GET_SIZE(shape.p);
-  if (!ints(shape.p, o->nd, o->size) || !ints(stride.p, o->nd, o->stride)) return false;
-  Ref dtype(PyObject_GetAttr(t, n_dtype));
-  if (!dtype.p) return false;
-  o->dtype = dtype.p;
-  Ref dev(PyObject_CallMethodNoArgs(t, n_get_device));
-  if (!dev.p) return false;
-  o->dev = (int)PyLong_AsLong(dev.p);
-  if (o->dev == -1 && PyErr_Occurred()) return false;
-  Ref p(PyObject_CallMethodNoArgs(t, n_data_ptr));
-  if (!p.p) return false;
-  o->p = PyLong_AsVoidPtr(p.p);
-  return o->p || !PyErr_Occurred();
-}
+// By each module in its own way: what there is to know of an object that has to be a tensor of at
+// most so many dimensions; an uninitialised tensor of n bytes.
+bool load(const char* name, PyObject* t, Tensor* o, int most = 4);
+PyObject* new_bytes(size_t n, int dev, void** p);
 
 const char* name_of(PyObject* dtype) {
   return dtype == bf16 ? "bfloat16" : dtype == f32 ? "float32" : dtype == u8 ? "uint8" : "int32";
@@ -145,28 +117,13 @@ bool take_room(int device, size_t bytes, Room* r) {
   if (!dev.p) return false;
   r->bytes = bytes;
   if (bytes) {
-    Ref n(PyLong_FromSize_t(bytes));
-    if (!n.p) return false;
-    r->ws.set(PyObject_CallFunctionObjArgs(new_workspace, n.p, dev.p, nullptr));
+    r->ws.set(new_bytes(bytes, device, &r->p));
     if (!r->ws.p) return false;
-    Ref p(PyObject_CallMethodNoArgs(r->ws.p, n_data_ptr));
-    if (!p.p) return false;
-    r->p = PyLong_AsVoidPtr(p.p);
   }
   Ref st(PyObject_CallOneArg(current_stream, dev.p));
   if (!st.p) return false;
   r->stream = PyLong_AsVoidPtr(st.p);
   return !PyErr_Occurred();
-}
-
-// given, or an uninitialised tensor shaped like `like` if it is None.
-PyObject* output(PyObject* given, PyObject* like) {
-  if (given != Py_None) {
-    Py_INCREF(given);
-    return given;
-  }
-  Ref shape(PyObject_GetAttr(like, n_shape));
-  return shape.p ? PyObject_CallMethodOneArg(like, n_new_empty, shape.p) : nullptr;
 }
 
 // The objects a[0 .. 7]: StageError; torch.bfloat16, float32, uint8, int32; current_device(),

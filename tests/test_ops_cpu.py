@@ -313,3 +313,19 @@ def test_adamw_python_refusals(kw):
     with pytest.raises(P.StageError) as e:
         P.AdamW([p], [p.clone()])
     assert "cuda" in str(e.value) or "on cpu" in str(e.value)
+
+
+def test_what_is_no_tensor_with_memory():
+    """The marshalling module says so of objects, sparse tensors and those without memory."""
+    import torch
+    for x in (None, 3, "x", [1.0]):
+        with pytest.raises(TypeError, match="not a tensor"):
+            P.layer_norm_forward(x)
+    for x in (torch.zeros(2, 3).to_sparse(), torch.zeros(2, 3, device="meta"), torch.zeros(2, 3),
+              torch.zeros((1,) * 9)):
+        with pytest.raises(P.StageError):
+            P.layer_norm_forward(x)
+    from paper_2202_11836_amd import _ops_call as m
+    for fn in (m.setup, m.norm_forward, m.norm_backward, m.rotary, m.adamw):
+        with pytest.raises(TypeError, match="arguments"):
+            fn()
