@@ -983,7 +983,7 @@ class AdamW:
         """The master copies as the parameters now are (after something else changed those)."""
         for p, w in zip(self.params, self.state["master"]):
             if w is not None:
-                w.copy_(p)
+                w.copy_(p.detach())
 
     def close(self):
         if getattr(self, "handle", None):

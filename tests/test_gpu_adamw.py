@@ -351,6 +351,21 @@ def test_reset_master():
     assert torch.equal(x.opt.state["master"][0], x.params[0].float())
 
 
+def test_leaves_of_a_graph():
+    """Parameters that autograd knows: the states are none of its."""
+    p = rand((5, 300), 1, "bf16").requires_grad_()
+    g = torch.zeros_like(p)
+    opt = P.AdamW([p], [g], state_bits=8)
+    (p.float() ** 2).sum().backward()
+    g.copy_(p.grad)
+    opt.step(LR)
+    opt.reset_master()
+    for n in opt.LISTS:
+        t = opt.state[n][0]
+        assert t is not None and t.grad_fn is None and not t.requires_grad, n
+    assert p.is_leaf and p.requires_grad and torch.equal(opt.state["master"][0], p.detach().float())
+
+
 def test_nothing_to_update():
     for sizes in ([], [0, 0]):
         x = Tensors(sizes)
