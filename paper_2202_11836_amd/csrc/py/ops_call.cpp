@@ -1,8 +1,8 @@
 // layer_norm_forward, layer_norm_backward, rotary_forward, rotary_backward and a step of
 // AdamW of the binding: argument checks and marshalling of torch tensors, as attn_call.cpp does
 // for the attention operators, but from torch's C++ objects: these kernels take a few us, and by
-// attribute a tensor costs 0.35 us to look at and 1.1 to 1.6 to make (32 tokens turned 5.6 -> 3.5 us a
-// call, layer norm of 8 x 1024 7.9 -> 5.7, a step of 231 x 765 15.7 -> 10.0).
+// attribute a tensor costs 0.35 us to look at and 1.1 to 1.6 to make (32 tokens turned 5.6 -> 3.5 to 4.3
+// us a call, layer norm of 8 x 1024 7.9 -> 5.7, a step of 231 x 765 15.7 -> 10.0 to 10.9).
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
