@@ -156,6 +156,25 @@ def test_in_place(width):
         assert got[0] is t[over] and all(torch.equal(a, b) for a, b in zip(got, want)), over
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [37, 1500])
+@pytest.mark.parametrize("width", [3, 13, 493, 999, 1531, 2501, 8199])
+def test_odd_rows_in_place(width, rows, dtype):
+    """A row's last values are read with some of those before them, which may be written by then."""
+    x, res, dy, dt = (rand((rows, width), i, dtype) for i in range(4))
+    ga, be = 1 + rand((width,), 5, std=0.2), rand((width,), 6)
+    want = P.layer_norm_forward(x, ga, be, res, eps=1e-5)
+    a, b = x.clone(), res.clone()
+    got = P.layer_norm_forward(a, ga, be, b, eps=1e-5, out=a, total=b)
+    assert all(torch.equal(s, t) for s, t in zip(got, want))
+    _, total, mean, rstd = want
+    want = P.layer_norm_backward(dy, total, ga, mean, rstd, dtotal=dt)
+    for over in ("dy", "total", "dt"):
+        t = {"dy": dy.clone(), "total": total.clone(), "dt": dt.clone()}
+        got = P.layer_norm_backward(t["dy"], t["total"], ga, mean, rstd, dtotal=t["dt"], dx=t[over])
+        assert all(torch.equal(s, t) for s, t in zip(got, want)), over
+
+
 @pytest.mark.parametrize("rows", [1, 5, 3000])
 def test_left_out(rows):
     x, dy = rand((rows, 300), 1), rand((rows, 300), 2)
