@@ -7,8 +7,8 @@
 // x (and the residual) and writes out (and the sum), backward reads dy, z and dtotal and
 // writes dx, while every thread adds up dy xh and dy of its columns over the rows of its
 // work-group, which leaves one partial row a work-group to a second launch.  bf16 rows of
-// 1024, 16384 of them, with residual: forward 27.4 us (4.9 TB/s), backward 28.5 (4.7) and
-// 4.7 for the sums; 5000 rows of 5120: 27.2 (3.8), 36.6 (4.2), 5.4.
+// 1024, 16384 of them, with residual: forward 27.3 us (4.9 TB/s), backward 27.5 (5.0) and
+// 4.6 for the sums; 5000 rows of 5120: 27.2 (3.8), 36.0 (4.9 with the partial rows), 5.4.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -335,6 +335,10 @@ __device__ __forceinline__ void column_sums(const BwdArgs& g, int col0) {
   }
 }
 
+// Values of a row of the partial sums in LDS: whole chunks.
+__host__ __device__ __forceinline__ int red_row(int w) { return (w + 7) & ~7; }
+typedef f32x4_t __attribute__((aligned(4))) any_f32x4_t;
+
 // What becomes of dy xh and dy: nothing, a partial row of each work-group's, or the sums at once by
 // work-groups behind those of the rows, each for 64 columns (few rows, read twice from cache: one
 // launch less).
@@ -451,7 +455,10 @@ __global__ __launch_bounds__(MAX_THREADS) void bwd_kernel(const BwdArgs g) {
   if constexpr (GRADS) {
     // The work-group's rows side by side: lanes of a wavefront first, then slots in order, one
     // sum after the other through LDS.
-    extern __shared__ float red[];  // [TPR 0: slot, else wavefront][w]
+    // (LDS rows are whole chunks, so that all of it goes 16 bytes at a time: with rows of w values and
+    // one at a time 1200 x 2048 took 10.5 us in bf16, 7.6 so, 5.4 without the sums.)
+    extern __shared__ __attribute__((aligned(16))) float red[];  // [TPR 0: slot, else wavefront][wp]
+    const int wp = red_row(g.w);
     constexpr bool WAVES = TPR > 0;
     float* const part = gridDim.x == 1 && g.dgamma ? nullptr : g.part + (int64_t)blockIdx.x * 2 * g.w;
     if constexpr (WAVES && TPR < 64) {
@@ -475,18 +482,36 @@ __global__ __launch_bounds__(MAX_THREADS) void bwd_kernel(const BwdArgs g) {
 #pragma unroll
           for (int i = 0; i < NC; ++i) {
             const int at = 8 * (lane + threads * i);
-            Chunk<float> c;
-            c.set(which ? pb[i] : pg[i]);
-            store_n(c, red + mine * g.w + at, left<NC>(g.w, at, i));
+            if (at >= g.w) continue;
+            const float* v = which ? pb[i] : pg[i];
+            f32x4_t* to_lds = (f32x4_t*)(red + mine * wp + at);
+            to_lds[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+            to_lds[1] = f32x4_t{v[4], v[5], v[6], v[7]};
           }
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < g.w; e += blockDim.x) {
-          float t = red[e];
-          for (int j = 1; j < rows; ++j) t += red[j * g.w + e];
-          to[e] = t;
+        for (int e = 4 * threadIdx.x; e < g.w; e += 4 * blockDim.x) {
+          const f32x4_t* from = (const f32x4_t*)(red + e);
+          f32x4_t t = from[0];
+          if constexpr (WAVES) {
+#pragma unroll
+            for (int j = 1; j < BWD_GROUP / 64; ++j) t += from[j * wp / 4];
+          } else {  // (two or four)
+            t += from[wp / 4];
+            if (rows > 2) {
+              t += from[2 * wp / 4];
+              t += from[3 * wp / 4];
+            }
+          }
+          if (e + 4 <= g.w) {
+            *(any_f32x4_t*)(to + e) = t;
+          } else {
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+              if (e + k < g.w) to[e + k] = t[k];
+          }
         }
-        __syncthreads();
+        if (which == 0) __syncthreads();
       } else {
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
@@ -563,14 +588,17 @@ int bwd_group(int w) {
 }
 // Work-groups, which leave a partial row each: one to a CU, or two where their registers let
 // two live there (one chunk a thread, or bf16 rows of more than one wavefront).  us with one and
-// two, bf16: 30000 x 512 30.6 / 24.9, 16384 x 1280 46.1 / 36.6, 5000 x 5120 59 / 46.6; one
-// is better for 16384 x 1024, 28.6 / 29.4, and fp32 8192 x 2048, 50.1 / 54.5.
+// two, bf16: 16384 x 1280 43.3 / 33.9, 3000 x 5120 38.5 / 32.5, 2000 x 2048 13.0 / 14.4; rows of up to 1024
+// gain or lose 4% with two, and fp32 rows of more than one wavefront lose, 8192 x 2048 50.1 / 54.5.
 int bwd_most(int w, stage_dtype dt) {
   return w <= 512 || (w > BWD_NARROW && w <= BWD_MIDDLE && dt == STAGE_BF16) ? 512 : 256;
 }
-// Up to so many rows the sums are made by work-groups of columns in the same launch: 231 x 768 in bf16
-// 10.5 -> 7.6 us, 231 x 5120 15 -> 7.6, 1024 x 1024 10.6 -> 9.4; 2000 x 1024 10.9 -> 15.5.
-constexpr int FEW_ROWS = 1024;
+// Up to so many rows the sums are made by work-groups of columns in the same launch, of more by partial
+// rows and a launch to sum them: a column's time grows with the rows, that of partial rows with the
+// width.  us by columns / partial rows, bf16: 550 x 512 6.3 / 7.8, 650 x 1024 7.3 / 7.8, 800 x 768
+// 7.8 / 7.3; 700 x 1280 7.7 / 8.4, 1000 x 1280 9.8 / 9.1; 1100 x 4096 13.2 / 17.0, 1600 x 5120 22.4 / 22.9,
+// 2000 x 5120 28.9 / 26.3; fp32 1000 x 1024 10.6 / 8.7, 1100 x 4096 19.3 / 21.4, 1400 x 4096 25.6 / 24.5.
+int few_rows(int w) { return w <= BWD_NARROW ? 700 : w < 4096 ? 900 : 1300; }
 struct BwdPlan {
   int blocks, rpb;
 };
@@ -612,7 +640,7 @@ template <typename T, int TPR, int MAX_THREADS, int NC>
 void launch_bwd(const BwdArgs& g, int blocks, Grads grads, hipStream_t st) {
   const dim3 grid((unsigned)blocks), block(bwd_group(g.w));
   const int rows = TPR ? BWD_GROUP / 64 : (int)block.x / g.threads;
-  const size_t lds = rows > 1 ? (size_t)rows * g.w * 4 : 0;
+  const size_t lds = rows > 1 ? (size_t)rows * red_row(g.w) * 4 : 0;
   if (grads == PARTIAL) {
     hipLaunchKernelGGL((bwd_kernel<T, TPR, MAX_THREADS, NC, 1, PARTIAL>), grid, block, lds, st, g);
   } else if (grads == NONE) {
@@ -832,7 +860,7 @@ stage_status layer_norm_backward(const layer_norm_shape* s, const void* dy, cons
       if (s->dtype == STAGE_BF16) backward<bf16_t>(g, blocks, how, st);
       else backward<float>(g, blocks, how, st);
     };
-    if (grads && rows <= FEW_ROWS) {
+    if (grads && rows <= few_rows(s->width)) {
       // Work-groups of columns read dy and z while those of rows write dx: over one of them, the
       // columns go first.
       grads = COLUMNS;

@@ -51,6 +51,13 @@ def test_rows(rows, dtype):
         run((rows, width), dtype, seed=rows + width, residual=True, dtotal=True)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,width", [(700, 1024), (701, 1024), (900, 2048), (901, 2048), (901, 4095), (1300, 4096),
+                                        (1301, 4096), (1301, 5123)])
+def test_weights_gradients_by_columns_and_by_partial_rows(rows, width, dtype):
+    run((rows, width), dtype, seed=rows, dtotal=True)
+
+
 @pytest.mark.parametrize("gamma", [False, True])
 @pytest.mark.parametrize("beta", [False, True])
 def test_without_weights(gamma, beta):
