@@ -574,10 +574,21 @@ constexpr int BWD_MIDDLE = 8192;                      // of eight
 
 int round64(int n) { return (n + 63) / 64 * 64; }
 // Threads of a row: a wavefront or less while its row fits (no barriers), then as many
-// wavefronts as the row fills with two chunks a thread.
-int fwd_threads(int w) {
+// wavefronts as the row fills with two chunks a thread.  bf16 rows that would leave a third of the lanes
+// without a value, or half of the second chunks, have three chunks a thread instead: their instructions
+// bound them.  us so / with 64 threads: forward 30000 x 300 11.3 / 17.3, 30000 x 384 13.2 / 15.4, 16384 x
+// 768 14.0 / 14.9 (fp32: 21.0 / 21.3, 22.4 / 21.6, 24.0 / 24.2, so it keeps its 64).
+bool by_threes(int w, stage_dtype dt) {
+  return dt == STAGE_BF16 && ((w > 256 && w <= 384) || (w > 512 && w <= 768));
+}
+int fwd_threads(int w, stage_dtype dt) {
+  if (by_threes(w, dt)) return w <= 384 ? 16 : 32;
   return w <= 64 ? 8 : w <= 128 ? 16 : w <= 256 ? 32 : w <= FWD_NARROW ? 64 : round64((w + 15) / 16);
 }
+// In the backward pass they take 178 registers for 125, which pays for many rows of the wider ones:
+// 40000 x 768 44.2 / 49.0, 22500 x 598 27.1 / 30.7, 16384 x 768 22.9 / 24.0; but 6000 x 768 12.7 / 12.0,
+// 30000 x 384 26.8 / 22.9.
+bool bwd_by_threes(int rows, int w, stage_dtype dt) { return w > 512 && rows >= 8192 && by_threes(w, dt); }
 int bwd_threads(int w) {
   return w <= 64 ? 8 : w <= 128 ? 16 : w <= 256 ? 32 : w <= BWD_NARROW ? 64 : round64((w + 15) / 16);
 }
@@ -603,7 +614,7 @@ struct BwdPlan {
   int blocks, rpb;
 };
 BwdPlan bwd_plan(int rows, int w, stage_dtype dt) {
-  const int step = bwd_group(w) / bwd_threads(w);  // rows at a time
+  const int step = bwd_by_threes(rows, w, dt) ? BWD_GROUP / 32 : bwd_group(w) / bwd_threads(w);  // rows at a time
   const int blocks = std::min(bwd_most(w, dt), (rows + step - 1) / step);
   const int rpb = ((rows + blocks - 1) / blocks + step - 1) / step * step;
   return {(rows + rpb - 1) / rpb, rpb};
@@ -612,10 +623,10 @@ BwdPlan bwd_plan(int rows, int w, stage_dtype dt) {
 template <typename T, int TPR, int NC>
 void launch_fwd(const FwdArgs& g, hipStream_t st) {
   constexpr int RPB = TPR ? 256 / (TPR ? TPR : 1) : 1;
-  const dim3 grid((unsigned)((g.rows + RPB - 1) / RPB)), block(TPR ? 256 : fwd_threads(g.w));
+  const dim3 grid((unsigned)((g.rows + RPB - 1) / RPB)), block(TPR ? 256 : round64((g.w + 15) / 16));
   // Early while all rows run at once: 2000 x 1024 in bf16 5.7 -> 5.1 us; 16384 x 1024 16.7 -> 17.1,
   // in fp32 29.4 -> 32.5.
-  const bool early = (int64_t)g.rows * fwd_threads(g.w) <= 2560 * 64;
+  const bool early = (int64_t)g.rows * (NC == 3 ? 64 : block.x / RPB) <= 2560 * 64;
   if (g.res.p) {
     if (early) hipLaunchKernelGGL((fwd_kernel<T, TPR, NC, true, true>), grid, block, 0, st, g);
     else hipLaunchKernelGGL((fwd_kernel<T, TPR, NC, true, false>), grid, block, 0, st, g);
@@ -627,6 +638,12 @@ void launch_fwd(const FwdArgs& g, hipStream_t st) {
 template <typename T>
 void forward(const FwdArgs& g, hipStream_t st) {
   const int w = g.w;
+  if constexpr (sizeof(T) == 2)
+    if (by_threes(w, STAGE_BF16)) {
+      if (w <= 384) launch_fwd<T, 16, 3>(g, st);
+      else launch_fwd<T, 32, 3>(g, st);
+      return;
+    }
   if (w <= 64) launch_fwd<T, 8, 1>(g, st);
   else if (w <= 128) launch_fwd<T, 16, 1>(g, st);
   else if (w <= 256) launch_fwd<T, 32, 1>(g, st);
@@ -653,6 +670,12 @@ void launch_bwd(const BwdArgs& g, int blocks, Grads grads, hipStream_t st) {
 template <typename T>
 void backward(const BwdArgs& g, int blocks, Grads grads, hipStream_t st) {
   const int w = g.w;
+  if constexpr (sizeof(T) == 2)
+    if (grads == PARTIAL && bwd_by_threes(g.rows, w, STAGE_BF16)) {
+      hipLaunchKernelGGL((bwd_kernel<T, 32, BWD_GROUP, 3, 1, PARTIAL>), dim3((unsigned)blocks), dim3(BWD_GROUP),
+                         BWD_GROUP / 64 * red_row(w) * 4, st, g);
+      return;
+    }
   if (w <= 64) launch_bwd<T, 8, BWD_GROUP, 1>(g, blocks, grads, st);
   else if (w <= 128) launch_bwd<T, 16, BWD_GROUP, 1>(g, blocks, grads, st);
   else if (w <= 256) launch_bwd<T, 32, BWD_GROUP, 1>(g, blocks, grads, st);
@@ -687,7 +710,7 @@ stage_status check_shape(const layer_norm_shape* s) {
   if (s->width < 1 || s->width > LAYER_NORM_MAX_WIDTH)
     return bad(STAGE_EINVAL, "width must be 1 .. %d", LAYER_NORM_MAX_WIDTH);
   // A launch holds fewer than 2^32 threads.
-  if ((int64_t)s->batch * s->seq > 4294967040LL / fwd_threads(s->width))
+  if ((int64_t)s->batch * s->seq > 4294967040LL / fwd_threads(s->width, s->dtype))
     return bad(STAGE_EINVAL, "batch * seq too large");
   return STAGE_OK;
 }

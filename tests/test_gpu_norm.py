@@ -52,6 +52,13 @@ def test_rows(rows, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,width", [(9, 258), (9, 383), (2600, 384), (3001, 385), (9, 640), (8191, 514), (8192, 514),
+                                        (8203, 599), (20000, 640), (8200, 767), (8192, 768), (8193, 769)])
+def test_rows_in_three_chunks(rows, width, dtype):
+    run((rows, width), dtype, seed=width, residual=rows % 2 == 1, dtotal=width % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,width", [(700, 1024), (701, 1024), (900, 2048), (901, 2048), (901, 4095), (1300, 4096),
                                         (1301, 4096), (1301, 5123)])
 def test_weights_gradients_by_columns_and_by_partial_rows(rows, width, dtype):
