@@ -10,6 +10,7 @@ built, loading fails with an error.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 import struct
@@ -853,7 +854,9 @@ class AdamW:
     in grads, in place, in one launch (two with max_norm).
 
     params, grads   lists of contiguous fp32 or bf16 tensors of one GPU; the gradients' memory
-                    is read by every step
+                    is read by every step.  A step is refused once one of the tensors (or of
+                    the states) is of other memory (its .data set, its module cast): make
+                    another AdamW then, of this one's .state
     weight_decay, lr_scale   a number, or one for each tensor
     state_bits      32 or 8, or a list of them: fp32 states, or e4m3 and e5m2 with a scale for
                     each 256 elements
@@ -897,10 +900,20 @@ class AdamW:
             self._fits(f"grads[{i}]", g, p.shape, types)
         self.state = self._new_state(bool(master)) if state is None else self._given_state(state)
         self.norm = torch.zeros(1, device=self.device)
-        # (the handle has their addresses, whatever becomes of the lists)
-        self._held = self.params + self.grads + [t for n in self.LISTS for t in self.state[n]] + \
-            [self.state["steps"]]
+        self._hold()
         self._make(decay, scale)
+
+    def _hold(self):
+        """The handle has addresses: their memory stays, whatever becomes of the lists or of a tensor's
+        .data, and step() looks at the tensors themselves, whether they still are of that memory."""
+        named = [(f"{n}[{i}]", t) for n, ts in [("params", self.params), ("grads", self.grads)] +
+                 [(n, self.state[n]) for n in self.LISTS] for i, t in enumerate(ts) if t is not None]
+        named.append(("steps", self.state["steps"]))
+        self._held = [t.detach() for _, t in named]
+        self._names = [n for n, t in named if t.numel()]
+        given = tuple(t for _, t in named if t.numel())
+        places = array.array("Q", [v for t in given for v in (t.untyped_storage().data_ptr(), t.storage_offset())])
+        self._given = given, places.tobytes()
 
     def _fits(self, name, t, shape, types):
         if t.dtype not in types or t.device != self.device or not t.is_cuda or not t.is_contiguous() or \
@@ -973,8 +986,10 @@ class AdamW:
         global norm; returns that norm before clipping (fp32 [1] on the GPU, the same tensor for
         every step), else None.  With max_norm a step whose norm is not finite changes nothing."""
         fn, dev = (_ops_module or _ops_setup()).adamw, self.device.index
-        a = (self.handle or 0, dev, lr, self.betas[0], self.betas[1], self.eps, max_norm, self.norm)
+        a = (self.handle or 0, dev, lr, self.betas[0], self.betas[1], self.eps, max_norm, self.norm, *self._given)
         r = fn(*a)
+        if r.__class__ is tuple:
+            raise StageError(STAGE_EINVAL, f"{self._names[r[0]]} has other memory than when the AdamW was made")
         if r is not None:
             _attn_on(r, fn, *a)
         return None if max_norm is None else self.norm

@@ -8,6 +8,7 @@
 
 #include <ATen/ops/empty.h>
 #include <cmath>
+#include <cstring>
 
 #include "../../../include/adamw.h"
 #include "../../../include/norm.h"
@@ -363,13 +364,48 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // ---------------------------------------------------------------------------
 // AdamW
 // ---------------------------------------------------------------------------
-// adamw(handle, device, lr, beta1, beta2, eps, max_norm, norm): None, or the device as above.  lr: a
-// number, or fp32 of one element on the device; max_norm None: no clipping (norm is then not
-// written).
+// The first of the tensors `given` that is no longer at its place, the address of its storage's memory
+// and its offset there (-1: none, -2: an error): .data of a tensor can be set, its storage can be given
+// up or made anew.  Straight from the objects, 3 ns a tensor: 24 weights with their gradients and states
+// 0.3 us, 640 of them 8 us.
+Py_ssize_t moved(PyObject* given, PyObject* places) {
+  struct Place {
+    uint64_t memory, offset;
+  } was;
+  if (!PyTuple_Check(given) || !PyBytes_Check(places) ||
+      PyBytes_GET_SIZE(places) != (Py_ssize_t)sizeof(Place) * PyTuple_GET_SIZE(given)) {
+    PyErr_SetString(PyExc_TypeError, "the tensors and their places are not as many");
+    return -2;
+  }
+  for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(given); ++i) {
+    PyObject* const t = PyTuple_GET_ITEM(given, i);
+    memcpy(&was, PyBytes_AS_STRING(places) + sizeof(Place) * i, sizeof(Place));
+    try {
+      if (!THPVariable_Check(t)) {
+        PyErr_SetString(PyExc_TypeError, "not a tensor");
+        return -2;
+      }
+      const c10::TensorImpl* const now = THPVariable_Unpack(t).unsafeGetTensorImpl();
+      const c10::StorageImpl* const memory = now->unsafe_storage().unsafeGetStorageImpl();
+      if (!memory || (uint64_t)(uintptr_t)memory->data_ptr().get() != was.memory ||
+          (uint64_t)now->storage_offset() != was.offset)
+        return i;
+    } catch (const std::exception&) {  // (memory that is not to be had)
+      return PyErr_Occurred() ? -2 : i;
+    }
+  }
+  return -1;
+}
+
+// adamw(handle, device, lr, beta1, beta2, eps, max_norm, norm, given, places): None, or the device as above,
+// or (i,), with nothing launched, where tensor i of `given` has moved.  lr: a number, or fp32 of one
+// element on the device; max_norm None: no clipping (norm is then not written).
 PyObject* adamw_call(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!wants("adamw", n, 8)) return nullptr;
+  if (!wants("adamw", n, 10)) return nullptr;
   adamw_t* h = (adamw_t*)PyLong_AsVoidPtr(a[0]);
   if (!h) return PyErr_Occurred() ? nullptr : (refuse("the optimizer is closed"), nullptr);
+  const Py_ssize_t i = moved(a[8], a[9]);
+  if (i != -1) return i < 0 ? nullptr : Py_BuildValue("(n)", i);
   const int dev = (int)PyLong_AsLong(a[1]);
   if (dev == -1 && PyErr_Occurred()) return nullptr;
   adamw_args g = {};

@@ -448,3 +448,35 @@ def test_two_at_once():
         for _ in range(5):
             y.opt.step(LR, max_norm=1.0)
         assert all(torch.equal(a, b) for a, b in zip(x.all(), y.all()))
+
+
+def test_tensors_that_move():
+    """A step is refused while a tensor is of other memory, and nothing is written to the old or the new."""
+    x = Tensors([5000, 300], "bf16", "bf16", 8)
+    x.opt.step(LR)
+    for t in (x.params[0], x.grads[1], x.opt.state["master"][1], x.opt.state["exp_avg_scale"][0]):
+        back, other = t.data, torch.full_like(t, 3)
+        t.data = other
+        was = copies(x.opt._held)
+        with pytest.raises(P.StageError) as e:
+            x.opt.step(LR, max_norm=1.0)
+        assert e.value.status == 1 and "other memory" in str(e.value)
+        torch.cuda.synchronize()
+        assert (other == 3).all()
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(was, x.opt._held))
+        t.data = back
+    net = torch.nn.Linear(64, 32, device="cuda")
+    for p in net.parameters():
+        p.grad = torch.ones_like(p)
+    opt = P.AdamW(list(net.parameters()), [p.grad for p in net.parameters()])
+    opt.step(LR)
+    net.bfloat16()
+    with pytest.raises(P.StageError) as e:
+        opt.step(LR)
+    assert "params[0]" in str(e.value)
+    assert opt.state["steps"].item() == 1
+    y = Tensors([5000, 300], "bf16", "bf16", 8)
+    for _ in range(2):
+        y.opt.step(LR)
+    x.opt.step(LR)
+    assert all(torch.equal(a, b) for a, b in zip(x.all(), y.all()))

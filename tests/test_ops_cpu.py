@@ -329,3 +329,60 @@ def test_what_is_no_tensor_with_memory():
     for fn in (m.setup, m.norm_forward, m.norm_backward, m.rotary, m.adamw):
         with pytest.raises(TypeError, match="arguments"):
             fn()
+
+
+def adamw_of_cpu_tensors(monkeypatch, params, grads, **kw):
+    """An AdamW over tensors of the CPU, without a handle: what it holds, and the marshalling of its step."""
+    monkeypatch.setattr(P.AdamW, "_fits", lambda *a: None)
+    monkeypatch.setattr(P.AdamW, "_make", lambda *a: None)
+    return P.AdamW(params, grads, **kw)
+
+
+def test_adamw_holds_memory_not_objects(monkeypatch):
+    """What a module's cast or a new .data takes from a tensor stays the optimizer's memory."""
+    net = torch.nn.Linear(300, 70)
+    params, grads = list(net.parameters()), [torch.randn_like(p) for p in net.parameters()]
+    opt = adamw_of_cpu_tensors(monkeypatch, params, grads)
+    every = params + grads + opt.state["exp_avg"] + opt.state["exp_avg_sq"] + [opt.state["steps"]]
+    at, was = [t.data_ptr() for t in every], [t.detach().clone() for t in every]
+    net.double()
+    for t in every[2:]:
+        t.data = torch.full_like(t, 7)
+    junk = [torch.full_like(t, 9) for t in was for _ in range(20)]
+    held = {t.data_ptr(): t for t in opt._held}
+    for a, w in zip(at, was):
+        assert a in held and torch.equal(held[a], w)
+    assert all((j == 9).all() for j in junk)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="a handle that is none")
+@pytest.mark.parametrize("name,i", [("params", 0), ("params", 1), ("grads", 1), ("exp_avg", 0), ("exp_avg_sq", 1),
+                                    ("exp_avg_scale", 0), ("master", 1), ("steps", None)])
+@pytest.mark.parametrize("how", ["data", "offset", "resized"])
+def test_adamw_step_of_moved_tensors(name, i, how, monkeypatch):
+    """Refused before the handle is looked at, and no longer once the memory is back."""
+    params = [torch.randn(300).bfloat16(), torch.randn(40, 20).bfloat16()]
+    opt = adamw_of_cpu_tensors(monkeypatch, params, [torch.randn_like(p) for p in params], state_bits=8)
+    opt.device = torch.device("cuda", 0)
+    block = ctypes.create_string_buffer(4096)
+    opt.handle = ctypes.addressof(block)
+    own = {"params": opt.params, "grads": opt.grads, "steps": [opt.state["steps"]]}
+    t = own.get(name, opt.state.get(name))[i or 0]
+    back = t.data
+    if how == "data":
+        t.data = t.data.clone()
+    elif how == "offset":
+        t.data = t.data.view(-1)[1:]
+    else:
+        t.untyped_storage().resize_(0)
+    try:
+        with pytest.raises(P.StageError) as e:
+            opt.step(1e-3)
+        assert e.value.status == 1 and (name if i is None else f"{name}[{i}]") + " has other memory" in str(e.value)
+        if how != "resized":
+            t.data = back
+            with pytest.raises((RuntimeError, AssertionError)) as e:  # (no device here)
+                opt.step(1e-3)
+            assert not isinstance(e.value, P.StageError)
+    finally:
+        opt.handle = None
