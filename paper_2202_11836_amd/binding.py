@@ -1019,12 +1019,19 @@ class _StageAdamW(AdamW):
         self.stage, self.names, self._tables = stage, names, stage._tables
         super().__init__(params, grads, **kw)
 
-    def step(self, lr, max_norm=None):
+    def _of_use(self):
         if not self.stage.handle:
             raise StageError(STAGE_ESTATE, "the stage is closed")
         if self.stage._tables != self._tables:
             raise StageError(STAGE_ESTATE, "the stage's bias table is another one since")
+
+    def step(self, lr, max_norm=None):
+        self._of_use()
         return super().step(lr, max_norm)
+
+    def reset_master(self):
+        self._of_use()
+        super().reset_master()
 
 
 # ---------------------------------------------------------------------------

@@ -302,3 +302,15 @@ def test_adamw_of_a_stage_that_is_gone():
     with pytest.raises(StageError) as e:
         st.adamw()
     assert e.value.status == 2 and "closed" in str(e.value)
+
+
+def test_master_copies_of_a_stage_that_is_gone():
+    st = Stage(1, 64, 1, 64, seed=2)
+    opt = st.adamw()
+    st.set_param(0, 0, st.param(0, 0) + 1)
+    opt.reset_master()
+    assert all(w is None or torch.equal(w, p.float()) for p, w in zip(opt.params, opt.state["master"]))
+    st.close()
+    with pytest.raises(StageError) as e:
+        opt.reset_master()
+    assert e.value.status == 2 and "closed" in str(e.value)

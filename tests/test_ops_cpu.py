@@ -386,3 +386,23 @@ def test_adamw_step_of_moved_tensors(name, i, how, monkeypatch):
             assert not isinstance(e.value, P.StageError)
     finally:
         opt.handle = None
+
+
+def test_adamw_of_a_stage_that_is_gone():
+    """Neither a step nor new master copies read a closed stage's memory, or an earlier bias table's."""
+    class Gone:
+        handle, _tables = None, 1
+
+    opt = Bn._StageAdamW.__new__(Bn._StageAdamW)
+    opt.stage, opt._tables, opt.handle = Gone(), 1, None
+    opt.params, opt.state = [torch.ones(4).bfloat16()], {"master": [torch.zeros(4)]}
+    for handle, tables, word in ((None, 1, "closed"), (5, 2, "table")):
+        Gone.handle, Gone._tables = handle, tables
+        for call in (opt.reset_master, lambda: opt.step(1e-3)):
+            with pytest.raises(P.StageError) as e:
+                call()
+            assert e.value.status == 2 and word in str(e.value)
+    assert (opt.state["master"][0] == 0).all()
+    Gone._tables = 1
+    opt.reset_master()
+    assert (opt.state["master"][0] == 1).all()
