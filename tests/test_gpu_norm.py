@@ -317,3 +317,10 @@ def test_graph_and_streams(shape):
                 results.append(call())
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for r in results for a, b in zip(r, want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,width", [(1301, 8193), (1301, 8200), (1400, 16384), (2053, 12345)])
+def test_wide_rows_by_partial_rows(rows, width, dtype):
+    """Rows of more than 8192 values, more of them than the sums by columns take."""
+    run((rows, width), dtype, seed=rows, dtotal=True)
