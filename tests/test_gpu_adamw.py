@@ -480,3 +480,24 @@ def test_tensors_that_move():
         y.opt.step(LR)
     x.opt.step(LR)
     assert all(torch.equal(a, b) for a, b in zip(x.all(), y.all()))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("master", [False, True])
+@pytest.mark.parametrize("pattern", [0x7fc00000, 0x7fffffff, -1, 0x7f800001, 0x7fbfffff, -0x400001])
+def test_any_nan_reaches_its_weight(pattern, master, bits):
+    """NaN with any low bits, in a gradient or in a weight, whatever the draw of its rounding."""
+    n = 20000
+    x, y = (Tensors([n], "bf16", "f32", bits, master) for _ in range(2))
+    hit = torch.zeros(n, dtype=torch.bool, device="cuda")
+    hit[3::37] = True
+    x.grads[0].view(torch.int32)[hit] = pattern
+    x.opt.step(LR)
+    y.opt.step(LR)
+    assert x.params[0][hit].isnan().all() and torch.equal(x.params[0][~hit], y.params[0][~hit])
+    if bits == 32:
+        assert x.opt.state["exp_avg"][0][hit].isnan().all() and x.opt.state["exp_avg_sq"][0][hit].isnan().all()
+    z = Tensors([n], "bf16", "f32", bits, False)
+    z.params[0].view(torch.int16)[hit] = pattern >> 16 | 0x40  # (a bf16 NaN, quiet)
+    z.opt.step(LR)
+    assert z.params[0][hit].isnan().all() and z.params[0][~hit].isfinite().all()
