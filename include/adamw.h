@@ -87,7 +87,7 @@ typedef struct {
   float lr;             /* used if lr_ptr is NULL */
   const float* lr_ptr;  /* one fp32 value on the device, read by the step */
   double beta1, beta2;  /* 0 <= beta < 1 */
-  float eps;            /* > 0 */
+  float eps;            /* 1e-30 or more, finite */
   float max_norm;       /* > 0: clip; 0: do not */
   float* norm;          /* receives the norm before clipping (fp32), or NULL; needs max_norm > 0 */
 } adamw_args;

@@ -857,6 +857,7 @@ class AdamW:
                     is read by every step.  A step is refused once one of the tensors (or of
                     the states) is of other memory (its .data set, its module cast): make
                     another AdamW then, of this one's .state
+    eps             1e-30 or more
     weight_decay, lr_scale   a number, or one for each tensor
     state_bits      32 or 8, or a list of them: fp32 states, or e4m3 and e5m2 with a scale for
                     each 256 elements

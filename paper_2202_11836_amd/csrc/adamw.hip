@@ -261,6 +261,10 @@ struct Step {  // what all elements of a step share
   float lr, lr_bias;           // lr, lr / (1 - beta1^t)
   float inv_root;              // 1 / sqrt(1 - beta2^t)
   float eps;
+  // The device's square root of a subnormal is 0.  Roots of those are below 2^-63, and where eps is
+  // 2^24 times what inv_root makes of that they do not count.  us with / without, 50M weights with 8-bit
+  // states: 102.2 / 96.8 (bf16 alone), 150.3 / 149.0 (a master copy).
+  bool small_roots;
   uint32_t t;
 };
 
@@ -307,10 +311,18 @@ __device__ __forceinline__ void update8(const Tensor& x, int64_t i, const Step& 
   drop<R>(g, gone);
   new_states(g, s, m, v);
   const float keep = 1.0f - s.lr * x.lr_scale * x.decay, rate = s.lr_bias * x.lr_scale;
+  float root[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) root[k] = __builtin_amdgcn_sqrtf(v[k]);
+  if (s.small_roots) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (v[k] < 0x1p-126f) root[k] = __builtin_amdgcn_sqrtf(v[k] * 0x1p64f) * 0x1p-32f;
+  }
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     // (square root and reciprocal of 1 ulp: a change of w, not w, is off by that)
-    const float den = fmaf(__builtin_amdgcn_sqrtf(v[k]), s.inv_root, s.eps);
+    const float den = fmaf(root[k], s.inv_root, s.eps);
     w[k] = fmaf(w[k], keep, -(rate * m[k] * __builtin_amdgcn_rcpf(den)));
   }
   uint32_t r[8];
@@ -452,6 +464,7 @@ __global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
   s.lr_bias = (float)(lr / (1.0 - power(a.beta1, t)));
   s.inv_root = (float)(1.0 / sqrt(1.0 - power(a.beta2, t)));
   s.eps = a.eps;
+  s.small_roots = __builtin_amdgcn_readfirstlane(s.inv_root > a.eps * 0x1p39f);
   s.t = (uint32_t)t;
   for (int c = blockIdx.x; go && c < a.n_chunks; c += gridDim.x) {
     const Chunk next = chunk_at(a, min(c + (int)gridDim.x, a.n_chunks - 1));

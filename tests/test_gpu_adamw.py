@@ -501,3 +501,36 @@ def test_any_nan_reaches_its_weight(pattern, master, bits):
     z.params[0].view(torch.int16)[hit] = pattern >> 16 | 0x40  # (a bf16 NaN, quiet)
     z.opt.step(LR)
     assert z.params[0][hit].isnan().all() and z.params[0][~hit].isfinite().all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("eps", [1e-30, 1e-20, 1e-17, 1e-8])
+def test_subnormal_second_moments(eps, dtype, bits):
+    """Gradients whose squares are subnormal in v: it is held as such and has its root, so an eps far
+    below that root leaves updates of the usual size.  Weights of 0, so that w is the update: off
+    by the roundings of rate, rate m, root, its product, the sum, reciprocal (1 EPS each, root and
+    reciprocal 2) and the last product, 9 EPS, from the states in fp32 as they are defined."""
+    n = 4096
+    w = torch.zeros(n, device="cuda")
+    p = w.to(DT[dtype])
+    g = rand((n,), 1) * torch.exp(rand((n,), 2) * 2.0) * 1e-18
+    g[::5] = 0
+    g[1::64] = 3e-12  # (among others whose squares are not subnormal)
+    zero = torch.zeros(n, device="cuda")
+    opt = P.AdamW([p], [g], betas=BETAS, eps=eps, weight_decay=0.0, state_bits=bits)
+    opt.step(LR)
+    m, v = states32(g, zero, zero, BETAS)
+    tiny = (v > 0) & (v < torch.finfo(torch.float32).tiny)
+    assert tiny.sum() > n // 4 and (v >= torch.finfo(torch.float32).tiny).any()
+    if bits == 32:
+        assert torch.equal(opt.state["exp_avg"][0], m) and torch.equal(opt.state["exp_avg_sq"][0], v)
+    up = LR * (m.double() / (1 - BETAS[0])) / ((v.double() / (1 - BETAS[1])).sqrt() + eps)
+    got = p if dtype == "f32" else opt.state["master"][0]
+    within("w", got, -up, 9 * EPS * up.abs() + 2.0 ** -149)
+    if eps == 1e-30:
+        # An update of the size of the rate.  Of v above 2^-140 the rounding, 2^-150, is 2^-10 of it and 2^-11
+        # of its root, g^2's before, 2^-150 of some 1000 v, less; eps is below 1e-10 of sqrt(v / 0.001).  (For
+        # 1e-20 it is up to 0.4 of that root, which the bound above has and this one had not.)
+        some = tiny & (v > 2.0 ** -140)
+        assert some.any() and ((got[some].abs() - LR).abs() < LR * 2.0 ** -9).all()

@@ -406,3 +406,22 @@ def test_adamw_of_a_stage_that_is_gone():
     Gone._tables = 1
     opt.reset_master()
     assert (opt.state["master"][0] == 1).all()
+
+
+class AdamWArgs(ctypes.Structure):
+    _fields_ = [("lr", f32), ("lr_ptr", vp), ("beta1", f64), ("beta2", f64), ("eps", f32), ("max_norm", f32), ("norm", vp)]
+
+
+@pytest.mark.parametrize("kw,word", [(dict(eps=0.0), "eps"), (dict(eps=9e-31), "eps"), (dict(eps=-1e-8), "eps"),
+                                     (dict(eps=math.inf), "eps"), (dict(eps=math.nan), "eps"),
+                                     (dict(beta2=1.0), "betas"), (dict(beta1=math.nan), "betas"),
+                                     (dict(max_norm=-1.0), "max_norm"), (dict(max_norm=math.nan), "max_norm"),
+                                     (dict(lr=math.inf), "lr"), (dict(lr_ptr=6), "lr_ptr"), (dict(norm=64), "norm")], ids=str)
+def test_adamw_step_refusals(kw, word):
+    """(before the handle is looked at)"""
+    lib, handle = P.load_library(), ctypes.create_string_buffer(4096)
+    lib.adamw_step.restype = i32
+    a = AdamWArgs(**dict(dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8), **kw))
+    assert lib.adamw_step(handle, ctypes.byref(a), None) == 1
+    msg = lib.adamw_last_error().decode()
+    assert word in msg, msg
