@@ -1001,6 +1001,9 @@ class AdamW:
             if w is not None:
                 w.copy_(p.detach())
 
+    def __reduce__(self):  # (two of one handle would both free it)
+        raise TypeError("an AdamW is not copied or pickled: make another one, of copies of its .state")
+
     def close(self):
         if getattr(self, "handle", None):
             load_library().adamw_destroy(self.handle)

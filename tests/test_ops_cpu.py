@@ -425,3 +425,16 @@ def test_adamw_step_refusals(kw, word):
     assert lib.adamw_step(handle, ctypes.byref(a), None) == 1
     msg = lib.adamw_last_error().decode()
     assert word in msg, msg
+
+
+def test_adamw_is_not_copied(monkeypatch):
+    """A copy would share the handle, which both would free."""
+    freed, p = [], torch.ones(4)
+    opt = adamw_of_cpu_tensors(monkeypatch, [p], [p.clone()])
+    monkeypatch.setattr(P.AdamW, "close", lambda self: freed.append(self.handle))
+    opt.handle = 1 << 20
+    for how in (copy.copy, copy.deepcopy, pickle.dumps):
+        with pytest.raises(TypeError, match="state"):
+            how(opt)
+    del opt
+    assert freed == [1 << 20]
