@@ -364,7 +364,7 @@ Group group_of(int batch, int S, int64_t per_token) {
   double most = 0.0;
   for (int p = 1; p <= MAX_P && p <= S; ++p) {
     const int64_t items = p * per_token, threads = (items + 63) / 64 * 64;
-    if (p > 1 && (threads > 320 || (int64_t)batch * ((S + p - 1) / p) < 1024)) break;
+    if (p > 1 && (threads > 320 || batch * (((int64_t)S + p - 1) / p) < 1024)) break;
     // (a few more idle threads rather than work-groups of one or two wavefronts)
     const double used = (double)items / threads * std::min(1.0, 0.7 + threads / 640.0);
     if (threads <= MOST_THREADS && used > most) {
@@ -431,7 +431,7 @@ stage_status apply(const rotary_shape* s, const rotary_freqs* f, bool backward, 
   }
   const Group group = group_of(batch, g.S, (int64_t)g.HG * g.items);
   g.P = group.tokens;
-  g.nblk = (g.S + g.P - 1) / g.P;
+  g.nblk = (int)(((int64_t)g.S + g.P - 1) / g.P);
   g.inv_hg = inverse(g.HG);
   g.inv_items = inverse(g.items);
   const int64_t grid = (int64_t)batch * g.nblk;
