@@ -3,7 +3,8 @@
 // the C ABI.
 //
 // A few operations a value, so HBM bounds it.  A row stays in the registers of its TPR
-// threads (8 to 1024 of them by its width) from its one read to its one write: forward reads
+// threads (8 to 1024 of them by its width; of fp32 rows beyond 8192 the backward pass that leaves partial
+// rows keeps 12 bytes a thread in scratch) from its one read to its one write: forward reads
 // x (and the residual) and writes out (and the sum), backward reads dy, z and dtotal and
 // writes dx, while every thread adds up dy xh and dy of its columns over the rows of its
 // work-group, which leaves one partial row a work-group to a second launch.  bf16 rows of
@@ -344,10 +345,9 @@ typedef f32x4_t __attribute__((aligned(4))) any_f32x4_t;
 // launch less).
 enum Grads { NONE, PARTIAL, COLUMNS };
 
-// U rows of a row's threads at a time, so that the loads of all are on their way together.
-template <typename T, int TPR, int MAX_THREADS, int NC, int U, Grads G>
+template <typename T, int TPR, int MAX_THREADS, int NC, Grads G>
 __global__ __launch_bounds__(MAX_THREADS) void bwd_kernel(const BwdArgs g) {
-  __shared__ float lds[TPR ? 1 : 4 * U * MOST_WAVES];
+  __shared__ float lds[TPR ? 1 : 4 * MOST_WAVES];
   constexpr bool GRADS = G == PARTIAL;
   if constexpr (G == COLUMNS)
     if ((int)blockIdx.x >= g.row_groups) {
@@ -373,82 +373,68 @@ __global__ __launch_bounds__(MAX_THREADS) void bwd_kernel(const BwdArgs g) {
   }
   int turn = 0;
   // (the same number of passes for all wavefronts of a row)
-  for (int first = r0; first < r1; first += slots * U) {
-    Chunk<T> dy[U][NC], z[U][NC], dt[U][NC];
-    float mean[U], rstd[U];
+  for (int first = r0; first < r1; first += slots) {
+    Chunk<T> dy[NC], z[NC], dt[NC];
+    const int row = first + slot;
+    const bool live = row < r1;
+    const T* pd = live ? row_at<T>(g.dy, g.batch, g.seq, row) : nullptr;
+    const T* pz = live ? row_at<T>(g.z, g.batch, g.seq, row) : nullptr;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int row = first + slot + slots * u;
-      const bool live = row < r1;
-      const T* pd = live ? row_at<T>(g.dy, g.batch, g.seq, row) : nullptr;
-      const T* pz = live ? row_at<T>(g.z, g.batch, g.seq, row) : nullptr;
+    for (int i = 0; i < NC; ++i) {
+      const int at = 8 * (lane + threads * i), n = live ? left<NC>(g.w, at, i) : 0;
+      load_n<TPR == 8>(dy[i], pd, at, n);
+      load_n<TPR == 8>(z[i], pz, at, n);
+    }
+    if (g.dtotal.p) {
+      const T* pt = live ? row_at<T>(g.dtotal, g.batch, g.seq, row) : nullptr;
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
-        const int at = 8 * (lane + threads * i), n = live ? left<NC>(g.w, at, i) : 0;
-        load_n<TPR == 8>(dy[u][i], pd, at, n);
-        load_n<TPR == 8>(z[u][i], pz, at, n);
+        const int at = 8 * (lane + threads * i);
+        load_n<TPR == 8>(dt[i], pt, at, live ? left<NC>(g.w, at, i) : 0);
       }
-      if (g.dtotal.p) {
-        const T* pt = live ? row_at<T>(g.dtotal, g.batch, g.seq, row) : nullptr;
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-          const int at = 8 * (lane + threads * i);
-          load_n<TPR == 8>(dt[u][i], pt, at, live ? left<NC>(g.w, at, i) : 0);
-        }
-      }
-      mean[u] = live ? g.mean[row] : 0.0f;
-      rstd[u] = live ? g.rstd[row] : 0.0f;
     }
+    const float mean = live ? g.mean[row] : 0.0f, rstd = live ? g.rstd[row] : 0.0f;
     if (g.w & 7)
 #pragma unroll
-      for (int ui = 0; ui < U * NC; ++ui) {
-        const int u = ui / NC, i = ui % NC;
+      for (int i = 0; i < NC; ++i) {
         const int at = 8 * (lane + threads * i), n = left<NC>(g.w, at, i);
-        trim(dy[u][i], at, n);
-        trim(z[u][i], at, n);
-        if (g.dtotal.p) trim(dt[u][i], at, n);
+        trim(dy[i], at, n);
+        trim(z[i], at, n);
+        if (g.dtotal.p) trim(dt[i], at, n);
       }
-    float s[2 * U];
-#pragma unroll
-    for (int u = 0; u < 2 * U; ++u) s[u] = 0.0f;
+    float s[2] = {0.0f, 0.0f};
     // (behind a row's end dy is 0, and so is all that comes of it)
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int i = 0; i < NC; ++i)
 #pragma unroll
-      for (int i = 0; i < NC; ++i)
+      for (int k = 0; k < 8; ++k) {
+        const float d = dy[i].get(k), xh = (z[i].get(k) - mean) * rstd;
+        const float dg = d * gm[i][k];
+        s[0] += dg;
+        s[1] += dg * xh;
+        if constexpr (GRADS) {
+          pg[i][k] += d * xh;
+          pb[i][k] += d;
+        }
+      }
+    if (g.dx.p) {
+      row_sums<TPR, 2>(s, lds, turn, threads / 64, slot);
+      turn ^= 1;
+      if (!live) continue;
+      T* px = row_at<T>(g.dx, g.batch, g.seq, row);
+      const float a = s[0] * inv_w, b = s[1] * inv_w;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        const int at = 8 * (lane + threads * i);
+        float v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const float d = dy[u][i].get(k), xh = (z[u][i].get(k) - mean[u]) * rstd[u];
-          const float dg = d * gm[i][k];
-          s[2 * u] += dg;
-          s[2 * u + 1] += dg * xh;
-          if constexpr (GRADS) {
-            pg[i][k] += d * xh;
-            pb[i][k] += d;
-          }
+          const float xh = (z[i].get(k) - mean) * rstd;
+          v[k] = rstd * (dy[i].get(k) * gm[i][k] - a - xh * b);
+          if (g.dtotal.p) v[k] += dt[i].get(k);
         }
-    if (g.dx.p) {
-      row_sums<TPR, 2 * U>(s, lds, turn, threads / 64, slot);
-      turn ^= 1;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int row = first + slot + slots * u;
-        if (row >= r1) continue;
-        T* px = row_at<T>(g.dx, g.batch, g.seq, row);
-        const float a = s[2 * u] * inv_w, b = s[2 * u + 1] * inv_w;
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-          const int at = 8 * (lane + threads * i);
-          float v[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float xh = (z[u][i].get(k) - mean[u]) * rstd[u];
-            v[k] = rstd[u] * (dy[u][i].get(k) * gm[i][k] - a - xh * b);
-            if (g.dtotal.p) v[k] += dt[u][i].get(k);
-          }
-          dy[u][i].set(v);
-          store_n(dy[u][i], px + at, left<NC>(g.w, at, i));
-        }
+        dy[i].set(v);
+        store_n(dy[i], px + at, left<NC>(g.w, at, i));
       }
     }
   }
@@ -460,7 +446,7 @@ __global__ __launch_bounds__(MAX_THREADS) void bwd_kernel(const BwdArgs g) {
     extern __shared__ __attribute__((aligned(16))) float red[];  // [TPR 0: slot, else wavefront][wp]
     const int wp = red_row(g.w);
     constexpr bool WAVES = TPR > 0;
-    float* const part = gridDim.x == 1 && g.dgamma ? nullptr : g.part + (int64_t)blockIdx.x * 2 * g.w;
+    float* const part = g.part + (int64_t)blockIdx.x * 2 * g.w;
     if constexpr (WAVES && TPR < 64) {
 #pragma unroll
       for (int i = 0; i < NC; ++i)
@@ -475,8 +461,7 @@ __global__ __launch_bounds__(MAX_THREADS) void bwd_kernel(const BwdArgs g) {
     const int rows = WAVES ? BWD_GROUP / 64 : slots, mine = WAVES ? threadIdx.x >> 6 : slot;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-      float* const to = part ? part + which * g.w : which ? g.dbeta : g.dgamma;
-      if (!to) continue;  // (uniform)
+      float* const to = part + which * g.w;
       if (rows > 1) {
         if (!WAVES || (threadIdx.x & 63) < TPR) {
 #pragma unroll
@@ -659,12 +644,12 @@ void launch_bwd(const BwdArgs& g, int blocks, Grads grads, hipStream_t st) {
   const int rows = TPR ? BWD_GROUP / 64 : (int)block.x / g.threads;
   const size_t lds = rows > 1 ? (size_t)rows * red_row(g.w) * 4 : 0;
   if (grads == PARTIAL) {
-    hipLaunchKernelGGL((bwd_kernel<T, TPR, MAX_THREADS, NC, 1, PARTIAL>), grid, block, lds, st, g);
+    hipLaunchKernelGGL((bwd_kernel<T, TPR, MAX_THREADS, NC, PARTIAL>), grid, block, lds, st, g);
   } else if (grads == NONE) {
-    hipLaunchKernelGGL((bwd_kernel<T, TPR, MAX_THREADS, NC, 1, NONE>), grid, block, 0, st, g);
+    hipLaunchKernelGGL((bwd_kernel<T, TPR, MAX_THREADS, NC, NONE>), grid, block, 0, st, g);
   } else {
     const dim3 both((unsigned)(blocks + (g.w + 63) / 64));
-    hipLaunchKernelGGL((bwd_kernel<T, TPR, MAX_THREADS, NC, 1, COLUMNS>), both, block, 0, st, g);
+    hipLaunchKernelGGL((bwd_kernel<T, TPR, MAX_THREADS, NC, COLUMNS>), both, block, 0, st, g);
   }
 }
 template <typename T>
@@ -672,7 +657,7 @@ void backward(const BwdArgs& g, int blocks, Grads grads, hipStream_t st) {
   const int w = g.w;
   if constexpr (sizeof(T) == 2)
     if (grads == PARTIAL && bwd_by_threes(g.rows, w, STAGE_BF16)) {
-      hipLaunchKernelGGL((bwd_kernel<T, 32, BWD_GROUP, 3, 1, PARTIAL>), dim3((unsigned)blocks), dim3(BWD_GROUP),
+      hipLaunchKernelGGL((bwd_kernel<T, 32, BWD_GROUP, 3, PARTIAL>), dim3((unsigned)blocks), dim3(BWD_GROUP),
                          BWD_GROUP / 64 * red_row(w) * 4, st, g);
       return;
     }
@@ -894,7 +879,7 @@ stage_status layer_norm_backward(const layer_norm_shape* s, const void* dy, cons
     } else {
       run(plan.blocks, grads);
     }
-    if (grads == PARTIAL && !(plan.blocks == 1 && dgamma))
+    if (grads == PARTIAL)
       hipLaunchKernelGGL(reduce_kernel, dim3((2 * s->width + RED_COLS - 1) / RED_COLS), dim3(1024), 0, st,
                          (const float*)workspace, plan.blocks, s->width, dgamma, dbeta);
   }
