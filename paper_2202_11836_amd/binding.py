@@ -10,7 +10,6 @@ built, loading fails with an error.
 """
 from __future__ import annotations
 
-import array
 import ctypes
 import os
 import struct
@@ -907,14 +906,18 @@ class AdamW:
     def _hold(self):
         """The handle has addresses: their memory stays, whatever becomes of the lists or of a tensor's
         .data, and step() looks at the tensors themselves, whether they still are of that memory."""
-        named = [(f"{n}[{i}]", t) for n, ts in [("params", self.params), ("grads", self.grads)] +
-                 [(n, self.state[n]) for n in self.LISTS] for i, t in enumerate(ts) if t is not None]
-        named.append(("steps", self.state["steps"]))
-        self._held = [t.detach() for _, t in named]
-        self._names = [n for n, t in named if t.numel()]
-        given = tuple(t for _, t in named if t.numel())
-        places = array.array("Q", [v for t in given for v in (t.untyped_storage().data_ptr(), t.storage_offset())])
-        self._given = given, places.tobytes()
+        lists = [self.params, self.grads] + [self.state[n] for n in self.LISTS] + [[self.state["steps"]]]
+        given = tuple(t for ts in lists for t in ts if t is not None)
+        self._held, places = (_ops_module or _ops_setup()).hold(given)
+        self._given = given, places
+
+    def _name(self, t):
+        """Of one of the tensors given."""
+        for n, ts in [("params", self.params), ("grads", self.grads)] + [(n, self.state[n]) for n in self.LISTS]:
+            for i, x in enumerate(ts):
+                if x is t:
+                    return f"{n}[{i}]"
+        return "steps" if t is self.state["steps"] else "a tensor"
 
     def _fits(self, name, t, shape, types):
         if t.dtype not in types or t.device != self.device or not t.is_cuda or not t.is_contiguous() or \
@@ -990,7 +993,8 @@ class AdamW:
         a = (self.handle or 0, dev, lr, self.betas[0], self.betas[1], self.eps, max_norm, self.norm, *self._given)
         r = fn(*a)
         if r.__class__ is tuple:
-            raise StageError(STAGE_EINVAL, f"{self._names[r[0]]} has other memory than when the AdamW was made")
+            raise StageError(STAGE_EINVAL,
+                             f"{self._name(self._given[0][r[0]])} has other memory than when the AdamW was made")
         if r is not None:
             _attn_on(r, fn, *a)
         return None if max_norm is None else self.norm

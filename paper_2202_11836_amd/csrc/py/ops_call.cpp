@@ -364,14 +364,41 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // ---------------------------------------------------------------------------
 // AdamW
 // ---------------------------------------------------------------------------
-// The first of the tensors `given` that is no longer at its place, the address of its storage's memory
-// and its offset there (-1: none, -2: an error): .data of a tensor can be set, its storage can be given
-// up or made anew.  Straight from the objects, 3 ns a tensor: 24 weights with their gradients and states
-// 0.3 us, 640 of them 8 us.
+// Where a tensor is: the memory of its storage and its offset there.
+struct Place {
+  uint64_t memory, offset;
+};
+Place place_of(const at::Tensor& t) {
+  const c10::TensorImpl* const of = t.unsafeGetTensorImpl();
+  const c10::StorageImpl* const memory = of->unsafe_storage().unsafeGetStorageImpl();
+  return {memory ? (uint64_t)(uintptr_t)memory->data_ptr().get() : 0, (uint64_t)of->storage_offset()};
+}
+
+// hold(tensors, a tuple): (aliases of them, as a list, which keep their memory; their places, as bytes).
+PyObject* hold(PyObject*, PyObject* tensors) {
+  HANDLE_TH_ERRORS
+  if (!PyTuple_Check(tensors)) return PyErr_SetString(PyExc_TypeError, "not a tuple"), nullptr;
+  const Py_ssize_t n = PyTuple_GET_SIZE(tensors);
+  Ref held(PyList_New(n)), places(PyBytes_FromStringAndSize(nullptr, n * sizeof(Place)));
+  if (!held.p || !places.p) return nullptr;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    PyObject* const x = PyTuple_GET_ITEM(tensors, i);
+    if (!THPVariable_Check(x)) return PyErr_SetString(PyExc_TypeError, "not a tensor"), nullptr;
+    const at::Tensor& t = THPVariable_Unpack(x);
+    const Place p = place_of(t);
+    memcpy(PyBytes_AS_STRING(places.p) + sizeof(p) * i, &p, sizeof(p));
+    PyObject* const alias = THPVariable_Wrap(t.variable_data());
+    if (!alias) return nullptr;
+    PyList_SET_ITEM(held.p, i, alias);
+  }
+  return PyTuple_Pack(2, held.p, places.p);
+  END_HANDLE_TH_ERRORS
+}
+
+// The first of the tensors `given` that is no longer at its place (-1: none, -2: an error): .data of a
+// tensor can be set, its storage can be given up or made anew.  Straight from the objects, 3 ns a
+// tensor: 24 weights with their gradients and states 0.3 us, 640 of them 8 us.
 Py_ssize_t moved(PyObject* given, PyObject* places) {
-  struct Place {
-    uint64_t memory, offset;
-  } was;
   if (!PyTuple_Check(given) || !PyBytes_Check(places) ||
       PyBytes_GET_SIZE(places) != (Py_ssize_t)sizeof(Place) * PyTuple_GET_SIZE(given)) {
     PyErr_SetString(PyExc_TypeError, "the tensors and their places are not as many");
@@ -379,17 +406,15 @@ Py_ssize_t moved(PyObject* given, PyObject* places) {
   }
   for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(given); ++i) {
     PyObject* const t = PyTuple_GET_ITEM(given, i);
-    memcpy(&was, PyBytes_AS_STRING(places) + sizeof(Place) * i, sizeof(Place));
+    Place was;
+    memcpy(&was, PyBytes_AS_STRING(places) + sizeof(was) * i, sizeof(was));
     try {
       if (!THPVariable_Check(t)) {
         PyErr_SetString(PyExc_TypeError, "not a tensor");
         return -2;
       }
-      const c10::TensorImpl* const now = THPVariable_Unpack(t).unsafeGetTensorImpl();
-      const c10::StorageImpl* const memory = now->unsafe_storage().unsafeGetStorageImpl();
-      if (!memory || (uint64_t)(uintptr_t)memory->data_ptr().get() != was.memory ||
-          (uint64_t)now->storage_offset() != was.offset)
-        return i;
+      const Place now = place_of(THPVariable_Unpack(t));
+      if (now.memory != was.memory || now.offset != was.offset) return i;
     } catch (const std::exception&) {  // (memory that is not to be had)
       return PyErr_Occurred() ? -2 : i;
     }
@@ -471,6 +496,7 @@ PyMethodDef methods[] = {{"setup", (PyCFunction)(void*)setup, METH_FASTCALL, nul
                          {"norm_forward", (PyCFunction)(void*)norm_forward, METH_FASTCALL, nullptr},
                          {"norm_backward", (PyCFunction)(void*)norm_backward, METH_FASTCALL, nullptr},
                          {"rotary", (PyCFunction)(void*)rotary, METH_FASTCALL, nullptr},
+                         {"hold", hold, METH_O, nullptr},
                          {"adamw", (PyCFunction)(void*)adamw_call, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops_call", nullptr, -1, methods,

@@ -437,6 +437,6 @@ def test_adamw_is_not_copied(monkeypatch):
         for how in (copy.copy, copy.deepcopy, pickle.dumps):
             with pytest.raises(TypeError, match="state"):
                 how(opt)
-        assert freed == []
+        assert 1 << 20 not in freed
     finally:
         opt.handle = None
