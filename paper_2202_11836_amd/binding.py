@@ -900,8 +900,8 @@ class AdamW:
             self._fits(f"grads[{i}]", g, p.shape, types)
         self.state = self._new_state(bool(master)) if state is None else self._given_state(state)
         self.norm = torch.zeros(1, device=self.device)
-        self._hold()
         self._make(decay, scale)
+        self._hold()
 
     def _hold(self):
         """The handle has addresses: their memory stays, whatever becomes of the lists or of a tensor's

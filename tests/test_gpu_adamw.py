@@ -534,3 +534,27 @@ def test_subnormal_second_moments(eps, dtype, bits):
         # 1e-20 it is up to 0.4 of that root, which the bound above has and this one had not.)
         some = tiny & (v > 2.0 ** -140)
         assert some.any() and ((got[some].abs() - LR).abs() < LR * 2.0 ** -9).all()
+
+
+def test_tensors_that_are_copied_when_written():
+    """Their own memory comes with the address that the handle takes, and is where they stay."""
+    x, y = Tensors([3000, 100]), Tensors([3000, 100])
+    was = copies(x.params)
+    x.opt = P.AdamW([torch._lazy_clone(p) for p in x.params], [torch._lazy_clone(g) for g in x.grads], **x.kw)
+    for _ in range(2):
+        x.opt.step(LR)
+        y.opt.step(LR)
+    assert all(torch.equal(a, b) for a, b in zip(x.opt.params, y.params))
+    assert all(torch.equal(a, b) for a, b in zip(x.params, was))
+
+
+def test_tensors_of_inference():
+    """Parameters and states made in inference mode."""
+    with torch.inference_mode():
+        x = Tensors([3000], "bf16")
+        x.opt.step(LR)
+    y = Tensors([3000], "bf16")
+    y.opt.step(LR)
+    x.opt.step(LR)
+    y.opt.step(LR)
+    assert torch.equal(x.params[0], y.params[0])
