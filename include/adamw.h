@@ -13,7 +13,7 @@
  *   - param: fp32, or bf16.  A bf16 parameter with a master copy (fp32) takes w from
  *     it and becomes its value rounded to nearest; one without takes w from itself and
  *     becomes one of w's two neighbours at random in proportion (nearest would lose every
- *     update below 2^-9 of the weight).
+ *     update below 2^-9 of the weight), or NaN if w is.
  *   - grad: fp32 or bf16.
  *   - m, v: fp32 (state_bits 32), or 8 bits in blocks of 256 elements with an fp32 scale
  *     each (state_bits 8): m = scale * e4m3, scale = max |m| / 448, and v = scale * e5m2,

@@ -22,7 +22,8 @@
  *     total itself, with its strides; apart from that no output may overlap an input.
  *   - gamma and beta [width], mean and rstd [batch, seq], dgamma and dbeta are fp32,
  *     contiguous.  gamma NULL: 1.  beta NULL: 0.
- *   - Sums and statistics are fp32; what is stored is rounded once.
+ *   - Sums and statistics are fp32; what is stored is rounded once.  A row whose sum or
+ *     whose mean times rstd is beyond fp32's range may become NaN.
  *   - width is 1 .. 16384; a call has at most 2^32 / 1024 (width 8193 on) to 2^32 / 8 (width
  *     64 or less) rows, by the threads that a row takes.
  *   - All device work is enqueued on hip_stream (NULL = default stream) of the

@@ -867,8 +867,8 @@ class AdamW:
 
     Steps of one AdamW go one after the other; a captured step counts on with each replay, for which
     the AdamW has to be there still, and open.  Autograd's version counters do not see a step: a
-    backward pass through a parameter's earlier value is not refused, as with torch's in-place
-    operations, but takes the new one.
+    backward pass that needs a parameter's earlier value takes the new one, where after an in-place
+    operation of torch's it were refused.
 
     state: a dict of lists, an entry for each tensor: "exp_avg", "exp_avg_sq" (fp32, or
     float8_e4m3fn and float8_e5m2), "exp_avg_scale", "exp_avg_sq_scale" (8 bits: fp32, one for
